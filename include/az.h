@@ -382,6 +382,137 @@ int az_eval_batch_compact_noalloc(az_net* net, const float* planes, const uint8_
                                   int32_t max_legal, float* policy, int32_t* legal_count, float* value,
                                   void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Matrices in 8 bits, and the policy from logits: the operators of a dense layer
+ * outside the fused network (a policy head over a trunk's flattened features, a
+ * layer that is trained with 8-bit activations).  They use no network handle,
+ * run asynchronously on `stream` (a hipStream_t of the current device, which
+ * also holds every buffer; NULL is its null stream), allocate nothing, never
+ * synchronise and can be captured into a HIP graph.  Two calls may run at once
+ * on any streams unless one writes what the other touches.  Input values are
+ * not checked; sizes, alignment and NULL pointers are, before the device is
+ * touched.
+ *
+ * A coded matrix holds OCP e4m3 codes with one scale 2^(s - 127), s a byte, for
+ * each block of 128 consecutive columns of one row (scale_rows 1, activations)
+ * or of 128 x 128 entries (scale_rows 128, weights).  The last block of a row or
+ * column may be short.  An entry stands for code * 2^(s - 127).
+ * az_codes_quantize writes s in 10..246, for which every such value is zero or a
+ * normal finite float that fp32 and bf16 hold exactly; the operators take these
+ * bytes, and 255, which makes its block NaN.  Other bytes are outside the format.
+ *
+ * Powers of two lose nothing against other scales but where a block's smallest
+ * entries become sub-normal codes, and the matrix instruction applies them
+ * itself.
+ *   codes       device, [rows][ld] bytes, 16-byte aligned.
+ *   scales      device, [ceil(rows / scale_rows)][ceil(cols / 128)] bytes.
+ *   rows, cols  rows 0..2^31-1, cols 1..2^30; at most 2^31-1 rows times blocks of a row.
+ *   ld          bytes from row to row, a multiple of 16 and >= cols.  The bytes
+ *               past cols are never written, and their values never matter.
+ *   scale_rows  1 or 128. */
+#define AZ_CODE_BLOCK 128
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t rows, cols, ld;
+  int32_t scale_rows;
+} az_code_matrix;
+
+/* Codes of x [q->rows][q->cols] (dtype AZ_F32 or AZ_BF16; ldx elements from row to
+ * row, aligned to its element): for each block with a = max |x| over its finite
+ * entries, e = ceil(log2(a / 448)) clamped to -117..119 (0 if a = 0), s = e + 127
+ * and code = sat(rne(x * 2^-e)), |code| <= 448.  An infinity or NaN in x becomes
+ * the NaN code 0x7f, so that it is seen in what is computed from it.  This is
+ * also how an activation is saved in 8 bits for the backward pass.
+ *   qt  NULL, or (scale_rows 128 in both) a second matrix [q->cols][q->rows] that
+ *       receives the transposed codes and scales: the operand of the input's
+ *       gradient, dx = dy W = az_codes_matmul(dy, Wt).
+ * Returns AZ_OK, AZ_ERR_INVALID_ARG, AZ_ERR_UNSUPPORTED (sizes past the limits) or
+ * AZ_ERR_DEVICE.  No rows: AZ_OK, nothing is launched. */
+int az_codes_quantize(const void* x, int32_t dtype, int64_t ldx, const az_code_matrix* q,
+                      const az_code_matrix* qt, void* stream);
+
+/* x[i][j] = the value of entry (i, j) of q, in AZ_F32 or AZ_BF16 (exact in both):
+ * restores a saved activation.  Layout and errors as for az_codes_quantize. */
+int az_codes_dequantize(const az_code_matrix* q, void* x, int32_t dtype, int64_t ldx, void* stream);
+
+/* out[m][n] = bias[n] + sum_k a[m][k] b[n][k]: a is [M][K] (activations), b [N][K]
+ * (a layer's weights, one row per output); either may have scale_rows 1 or 128.
+ *   bias  device, [N] fp32, or NULL.
+ *   out   device, [M][N], dtype AZ_BF16 or AZ_F32, ld_out elements from row to row,
+ *         aligned to its element.
+ * AZ_BF16 multiplies on the scaled e4m3 matrix instruction, which cuts products
+ * that are far below the largest one next to them (about 1.5e-5 of the result's
+ * norm, a hundredth of a bf16 rounding) and accumulates in fp32.  AZ_F32 multiplies on
+ * the bf16 instruction: every product is exact, sums are fp32.  Sums have a fixed
+ * order: equal calls give equal bits.
+ * M = 0 or N = 0 (rows): AZ_OK, nothing is launched.  Errors as above. */
+int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b, const float* bias, void* out,
+                    int32_t dtype, int64_t ld_out, void* stream);
+
+/* The weight's and bias's gradients of y = x W^T + bias, x as it was saved in 8
+ * bits (scale_rows 1):
+ *   dw[n][k] = sum_m dy[m][n] x[m][k],   db[n] = sum_m dy[m][n]
+ * (accumulate != 0: added to what dw and db hold).
+ *   dy  device, bf16 [x->rows][N], ld_dy elements from row to row; 16-byte aligned rows
+ *       (dy and ld_dy) take a faster path.
+ *   dw  device, [N][x->cols], dtype AZ_F32 or AZ_BF16, ld_dw elements from row to
+ *       row.  db  device, [N] fp32, or NULL.
+ * Products are exact, sums fp32 in a fixed order.  x->rows = 0 clears dw and db (or,
+ * accumulating, leaves them).
+ *   workspace  device, 16-byte aligned, at least az_codes_weight_grad_workspace
+ *              bytes (which may be 0; then it may be NULL).  It holds sums over
+ *              parts of the rows, is written before it is read, and must not be
+ *              shared by two calls that may run at once.
+ * Errors as above. */
+size_t az_codes_weight_grad_workspace(int64_t rows, int32_t n, int64_t cols);
+int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, const az_code_matrix* x, void* dw,
+                         int32_t dtype, int64_t ld_dw, float* db, int32_t accumulate, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Logits, what is allowed, and what has been chosen before. */
+typedef enum { AZ_MASK_NONE = 0, AZ_MASK_BYTES = 1, AZ_MASK_BITS = 2 } az_mask_kind;
+typedef struct {
+  const void* logits;   /* device, [rows][vocab], AZ_F32 or AZ_BF16 */
+  int32_t dtype;
+  int32_t rows, vocab;  /* rows 0..2^20, vocab 1..2^24 */
+  int64_t ld;           /* elements from row to row, >= vocab */
+  const void* mask;     /* device; AZ_MASK_BYTES: [rows][vocab] bytes, nonzero = allowed, as
+                           az_eval_batch's legal; AZ_MASK_BITS: [rows][ceil(vocab / 32)] 32-bit words,
+                           bit v % 32 of word v / 32; NULL with AZ_MASK_NONE: all are allowed */
+  int32_t mask_kind;
+  int64_t ld_mask;      /* bytes (words) from row to row */
+  const float* bias;    /* device, added to the logits, or NULL; */
+  int64_t ld_bias;      /* elements from row to row, or 0: one row for all */
+  const int32_t* history;    /* device, [rows][ld_history]: entries chosen before, or NULL;
+                                values outside 0..vocab-1 are ignored */
+  int64_t ld_history;
+  int32_t max_history;       /* 0..ld_history */
+  const int32_t* lengths;    /* device, [rows]: entries of each row, clamped to 0..max_history; NULL: max_history */
+  const float* penalties;    /* device, [rows][3] (needed with history): repetition r > 0 (1: none),
+                                frequency f and presence p (0: none) */
+} az_logits;
+
+/* Per row, with c[v] = how often v stands in the row's history:
+ *   l = logits[v];  if c[v] > 0:  l = (l > 0 ? l / r : l * r) - (f * c[v] + p);
+ *   l += bias[v];   l = -inf where v is not allowed
+ * probabilities = 0: out[v] = l.  probabilities = 1: the policy, as the network's:
+ * out[v] = exp(l[v] - max l) / sum exp(l - max l), exactly 0.0f where v is not
+ * allowed; a row in which nothing is allowed (or every allowed l is -inf) is all
+ * zero.  What the logits hold where v is not allowed, NaN or infinities, does
+ * not matter.  A NaN or +inf that is allowed makes the row's allowed entries NaN.
+ *   out        device, [rows][vocab] fp32, ld_out elements from row to row.  It may be
+ *              the logits' own buffer (AZ_F32, ld_out = ld), and may not overlap any
+ *              input otherwise.
+ *   workspace  device, 16-byte aligned, at least az_logits_policy_workspace
+ *              bytes (which may be 0; then it may be NULL), written before it is
+ *              read; not shared by two calls that may run at once.
+ * All arithmetic is fp32, sums in a fixed order.  Buffers are aligned to their
+ * elements.  rows = 0: AZ_OK, nothing is launched.  Errors as above. */
+size_t az_logits_policy_workspace(int32_t rows, int32_t vocab);
+int az_logits_policy(const az_logits* in, int32_t probabilities, float* out, int64_t ld_out, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 /* Failure-handling test support.  az_debug_fail_allocation(n), n >= 1: the
  * n-th device or pinned-host allocation the library attempts from now on
  * (weights in az_net_load, buffers in az_pipeline_create) fails as if the

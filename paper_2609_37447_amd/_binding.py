@@ -29,6 +29,8 @@ EXPORTS = ("az_weight_count", "az_net_load", "az_eval_batch", "az_eval_batch_wdl
            "az_pipeline_create", "az_pipeline_slot", "az_pipeline_submit", "az_pipeline_query",
            "az_pipeline_wait", "az_pipeline_drive", "az_pipeline_free", "az_debug_fail_allocation",
            "az_debug_live_allocations", "az_eval_batch_compact_noalloc",
+           "az_codes_quantize", "az_codes_dequantize", "az_codes_matmul", "az_codes_weight_grad",
+           "az_codes_weight_grad_workspace", "az_logits_policy", "az_logits_policy_workspace",
            "az_status_string", "az_last_error")
 
 
@@ -47,6 +49,23 @@ class az_layer_spec(ctypes.Structure):
 class az_layer_spec_v1(ctypes.Structure):
     """The version-1 layout (the first nine fields), as older callers pass it."""
     _fields_ = az_layer_spec._fields_[:9]
+
+
+AZ_CODE_BLOCK = 128
+AZ_MASK_NONE, AZ_MASK_BYTES, AZ_MASK_BITS = 0, 1, 2
+
+
+class az_code_matrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("scale_rows", ctypes.c_int32)]
+
+
+class az_logits(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("ld", ctypes.c_int64), ("mask", ctypes.c_void_p),
+                ("mask_kind", ctypes.c_int32), ("ld_mask", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("ld_bias", ctypes.c_int64), ("history", ctypes.c_void_p), ("ld_history", ctypes.c_int64),
+                ("max_history", ctypes.c_int32), ("lengths", ctypes.c_void_p), ("penalties", ctypes.c_void_p)]
 
 
 class AzError(RuntimeError):
@@ -101,6 +120,17 @@ def lib():
         L.az_pipeline_drive.restype = ctypes.c_int
         L.az_eval_batch_compact_noalloc.argtypes = [P, P, P, I32, I32, P, P, P, P]
         L.az_eval_batch_compact_noalloc.restype = ctypes.c_int
+        M, I64 = ctypes.POINTER(az_code_matrix), ctypes.c_int64
+        L.az_codes_quantize.argtypes = [P, I32, I64, M, M, P]
+        L.az_codes_dequantize.argtypes = [M, P, I32, I64, P]
+        L.az_codes_matmul.argtypes = [M, M, P, P, I32, I64, P]
+        L.az_codes_weight_grad.argtypes = [P, I64, I32, M, P, I32, I64, P, I32, P, SZ, P]
+        L.az_logits_policy.argtypes = [ctypes.POINTER(az_logits), I32, P, I64, P, SZ, P]
+        for f in (L.az_codes_quantize, L.az_codes_dequantize, L.az_codes_matmul, L.az_codes_weight_grad,
+                  L.az_logits_policy):
+            f.restype = ctypes.c_int
+        L.az_codes_weight_grad_workspace.argtypes, L.az_codes_weight_grad_workspace.restype = [I64, I32, I64], SZ
+        L.az_logits_policy_workspace.argtypes, L.az_logits_policy_workspace.restype = [I32, I32], SZ
         L.az_debug_fail_allocation.argtypes, L.az_debug_fail_allocation.restype = [I32], None
         L.az_debug_live_allocations.argtypes, L.az_debug_live_allocations.restype = [], ctypes.c_int64
         L.az_status_string.argtypes, L.az_status_string.restype = [ctypes.c_int], ctypes.c_char_p
@@ -284,6 +314,245 @@ def validate(net_test, net_ref, planes, legal, min_top1: float = 0.8, max_kl: fl
     dv = float(r[:, 2].max())
     return {"top1": top1, "kl": kl, "dv_max": dv, "rows": r,
             "passed": top1 >= min_top1 and kl <= max_kl and dv <= max_dv}
+
+
+# --------------------------------------------------------------------------- #
+# Coded matrices and the policy from logits, on torch device tensors
+# --------------------------------------------------------------------------- #
+def az_codes_quantize(x, dtype: int, ldx: int, q: az_code_matrix, qt=None, stream: int = 0,
+                      raise_on_error: bool = True) -> int:
+    st = lib().az_codes_quantize(x, dtype, ldx, q, qt, stream)
+    return _check(st, "az_codes_quantize") if raise_on_error else st
+
+
+def az_codes_dequantize(q: az_code_matrix, x, dtype: int, ldx: int, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_codes_dequantize(q, x, dtype, ldx, stream)
+    return _check(st, "az_codes_dequantize") if raise_on_error else st
+
+
+def az_codes_matmul(a: az_code_matrix, b: az_code_matrix, bias, out, dtype: int, ld_out: int, stream: int = 0,
+                    raise_on_error: bool = True) -> int:
+    st = lib().az_codes_matmul(a, b, bias, out, dtype, ld_out, stream)
+    return _check(st, "az_codes_matmul") if raise_on_error else st
+
+
+def az_codes_weight_grad_workspace(rows: int, n: int, cols: int) -> int:
+    return int(lib().az_codes_weight_grad_workspace(rows, n, cols))
+
+
+def az_codes_weight_grad(dy, ld_dy: int, n: int, x: az_code_matrix, dw, dtype: int, ld_dw: int, db=None,
+                         accumulate: bool = False, workspace=None, workspace_bytes: int = 0, stream: int = 0,
+                         raise_on_error: bool = True) -> int:
+    st = lib().az_codes_weight_grad(dy, ld_dy, n, x, dw, dtype, ld_dw, db, int(accumulate), workspace,
+                                    workspace_bytes, stream)
+    return _check(st, "az_codes_weight_grad") if raise_on_error else st
+
+
+def az_logits_policy_workspace(rows: int, vocab: int) -> int:
+    return int(lib().az_logits_policy_workspace(rows, vocab))
+
+
+def az_logits_policy(logits: az_logits, probabilities: bool, out, ld_out: int, workspace=None, workspace_bytes: int = 0,
+                     stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_logits_policy(logits, int(probabilities), out, ld_out, workspace, workspace_bytes, stream)
+    return _check(st, "az_logits_policy") if raise_on_error else st
+
+
+def _rows_of(name, t, dtypes):
+    """(rows, columns, elements from row to row) of a two-dimensional device tensor."""
+    if not t.is_cuda or t.dtype not in dtypes or t.dim() != 2:
+        raise ValueError(f"{name} must be a two-dimensional device tensor of {' or '.join(map(str, dtypes))}")
+    rows, cols = t.shape
+    step, inner = t.stride()
+    if cols > 1 and inner != 1 or rows > 1 and step < cols:
+        raise ValueError(f"{name} must hold its rows one behind the other, each without gaps")
+    return rows, cols, step if rows > 1 else max(step, cols)
+
+
+def _vector_of(name, t, dtype, n):
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be a contiguous device tensor of {dtype} [{n}]")
+
+
+class CodeMatrix:
+    """A matrix of e4m3 codes with a power-of-two scale for each block of 128 columns of a
+    row (scale_rows 1) or of 128 x 128 entries (scale_rows 128), on torch device tensors:
+    codes uint8 [rows][columns or more], rows a multiple of 16 bytes apart, and scales uint8
+    [ceil(rows / scale_rows)][ceil(cols / 128)].  Keeps its tensors alive."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "scale_rows", "device", "c")
+
+    def __init__(self, codes, scales, cols=None, scale_rows: int = 1):
+        import torch
+        rows, width, ld = _rows_of("codes", codes, (torch.uint8,))
+        cols = width if cols is None else int(cols)
+        if not 0 < cols <= width:
+            raise ValueError(f"cols {cols} is not in 1..{width}")
+        if scale_rows not in (1, AZ_CODE_BLOCK):
+            raise ValueError("scale_rows is 1 or 128")
+        if rows <= 1:
+            ld = -(-ld // 16) * 16  # one row: only its whole 16-byte chunks have to be there
+            if rows == 1 and codes.untyped_storage().nbytes() - codes.storage_offset() < -(-cols // 16) * 16:
+                raise ValueError("codes needs whole chunks of 16 bytes")
+        want = (-(-rows // scale_rows), -(-cols // AZ_CODE_BLOCK))
+        if not scales.is_cuda or scales.dtype != torch.uint8 or tuple(scales.shape) != want or not scales.is_contiguous():
+            raise ValueError(f"scales must be a contiguous uint8 device tensor {list(want)}")
+        if scales.device != codes.device:
+            raise ValueError("codes and scales are on different devices")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self.scale_rows, self.device = scale_rows, codes.device
+        self.c = az_code_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, scale_rows)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, scale_rows: int = 1, device="cuda"):
+        """A matrix of these sizes on memory of its own, codes and scales not yet written."""
+        import torch
+        codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device)
+        scales = torch.empty((-(-rows // scale_rows), -(-cols // AZ_CODE_BLOCK)), dtype=torch.uint8, device=device)
+        return cls(codes, scales, cols, scale_rows)
+
+
+class _On:
+    """The device that all operands share made the current one for a call, and the stream (torch's
+    current one by default) as the library takes it."""
+
+    def __init__(self, stream, first, *others):
+        import torch
+        for t in others:
+            if t is not None and t.device != first:
+                raise ValueError("the operands are on different devices")
+        self.guard = torch.cuda.device(first) if first.index != torch.cuda.current_device() else None
+        self.s = torch.cuda.current_stream(first) if stream is None else stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.s.cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _workspace(given, need, device, stream):
+    """(pointer, bytes) of a call's workspace; made for the call on its stream where none is given."""
+    if given is not None:
+        if not given.is_cuda or not given.is_contiguous() or given.device != device:
+            raise ValueError("workspace must be a contiguous tensor on the operands' device")
+        return given.data_ptr(), given.numel() * given.element_size(), given
+    if need == 0:
+        return None, 0, None
+    import torch
+    if stream is None:
+        t = torch.empty((need,), dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(stream):
+            t = torch.empty((need,), dtype=torch.uint8, device=device)
+    return t.data_ptr(), need, t
+
+
+def _float_type(t) -> int:
+    import torch
+    return AZ_BF16 if t.dtype == torch.bfloat16 else AZ_F32
+
+
+def quantize_tensors(x, q: CodeMatrix, transposed: CodeMatrix = None, stream=None) -> int:
+    """az_codes_quantize of x (float32 or bfloat16 [rows][cols]) into q and, for matrices with
+    scale_rows 128, its transposed copy; stream defaults to torch's current one."""
+    import torch
+    rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
+    if (rows, cols) != (q.rows, q.cols):
+        raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
+    with _On(stream, x.device, q, transposed) as s:
+        return az_codes_quantize(x.data_ptr(), _float_type(x), ld, q.c, transposed.c if transposed is not None else None, s)
+
+
+def dequantize_tensors(q: CodeMatrix, x, stream=None) -> int:
+    """az_codes_dequantize of q into x (float32 or bfloat16 [rows][cols])."""
+    import torch
+    rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
+    if (rows, cols) != (q.rows, q.cols):
+        raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
+    with _On(stream, x.device, q) as s:
+        return az_codes_dequantize(q.c, x.data_ptr(), _float_type(x), ld, s)
+
+
+def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, stream=None) -> int:
+    """az_codes_matmul: out [a.rows][b.rows] (bfloat16 or float32) = a b^T + bias (float32 [b.rows])."""
+    import torch
+    m, n, ld = _rows_of("out", out, (torch.float32, torch.bfloat16))
+    if (m, n) != (a.rows, b.rows):
+        raise ValueError(f"out is {[m, n]}, the product {[a.rows, b.rows]}")
+    if bias is not None:
+        _vector_of("bias", bias, torch.float32, n)
+    with _On(stream, out.device, a, b, bias) as s:
+        return az_codes_matmul(a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), _float_type(out), ld, s)
+
+
+def weight_grad_tensors(dy, x: CodeMatrix, dw, db=None, accumulate: bool = False, workspace=None, stream=None) -> int:
+    """az_codes_weight_grad: dw [n][x.cols] (float32 or bfloat16) and db (float32 [n]) from dy
+    (bfloat16 [x.rows][n]) and the layer's saved input x.  A workspace is made for the call
+    (torch's allocator, on the call's stream) unless a tensor is given."""
+    import torch
+    m, n, ldy = _rows_of("dy", dy, (torch.bfloat16,))
+    if m != x.rows:
+        raise ValueError(f"dy has {m} rows, x {x.rows}")
+    wn, wk, ldw = _rows_of("dw", dw, (torch.float32, torch.bfloat16))
+    if (wn, wk) != (n, x.cols):
+        raise ValueError(f"dw is {[wn, wk]}, the gradient {[n, x.cols]}")
+    if db is not None:
+        _vector_of("db", db, torch.float32, n)
+    with _On(stream, dw.device, dy, x, db) as s:
+        ws, size, keep = _workspace(workspace, az_codes_weight_grad_workspace(m, n, x.cols), dw.device, stream)
+        return az_codes_weight_grad(dy.data_ptr(), ldy, n, x.c, dw.data_ptr(), _float_type(dw), ldw,
+                                    db.data_ptr() if db is not None else None, accumulate, ws, size, s)
+
+
+def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None, penalties=None,
+                   probabilities: bool = True, workspace=None, stream=None) -> int:
+    """az_logits_policy of logits (float32 or bfloat16 [rows][vocab]) into out (float32): the policy over
+    what the mask allows, or the adjusted logits.  mask: uint8 or bool [rows][vocab] (nonzero =
+    allowed) or int32 [rows][ceil(vocab / 32)] of bits; bias: float32 [vocab], [1][vocab] or
+    [rows][vocab]; history: int32 [rows][entries] with lengths int32 [rows] (default: all) and penalties
+    float32 [rows][3] (repetition, frequency, presence)."""
+    import torch
+    b, v, ld = _rows_of("logits", logits, (torch.float32, torch.bfloat16))
+    ob, ov, ldo = _rows_of("out", out, (torch.float32,))
+    if (ob, ov) != (b, v):
+        raise ValueError(f"out is {[ob, ov]}, the logits {[b, v]}")
+    kind, ldm = AZ_MASK_NONE, 0
+    if mask is not None:
+        mb, mv, ldm = _rows_of("mask", mask, (torch.uint8, torch.bool, torch.int32))
+        kind = AZ_MASK_BITS if mask.dtype == torch.int32 else AZ_MASK_BYTES
+        if (mb, mv) != (b, -(-v // 32) if kind == AZ_MASK_BITS else v):
+            raise ValueError(f"mask {[mb, mv]} does not fit logits {[b, v]}")
+    ldb = 0
+    if bias is not None:
+        if bias.dim() == 1:
+            bias = bias.unsqueeze(0)
+        bb, bv, ldb = _rows_of("bias", bias, (torch.float32,))
+        if bv != v or bb not in (1, b):
+            raise ValueError(f"bias {[bb, bv]} does not fit logits {[b, v]}")
+        ldb = ldb if bb == b and b > 1 else 0
+    t, ldh = 0, 0
+    if history is not None:
+        hb, t, ldh = _rows_of("history", history, (torch.int32,))
+        if hb != b:
+            raise ValueError(f"history has {hb} rows, the logits {b}")
+        if penalties is None:
+            raise ValueError("a history needs penalties")
+        if not penalties.is_cuda or penalties.dtype != torch.float32 or tuple(penalties.shape) != (b, 3) or not penalties.is_contiguous():
+            raise ValueError(f"penalties must be a contiguous float32 device tensor [{b}, 3]")
+        if lengths is not None:
+            _vector_of("lengths", lengths, torch.int32, b)
+    elif lengths is not None or penalties is not None:
+        raise ValueError("lengths and penalties come with a history")
+    with _On(stream, logits.device, out, mask, bias, history, lengths, penalties) as s:
+        ws, size, keep = _workspace(workspace, az_logits_policy_workspace(b, v), logits.device, stream)
+        p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
+        return az_logits_policy(az_logits(p(logits), _float_type(logits), b, v, ld, p(mask), kind, ldm, p(bias), ldb,
+                                          p(history), ldh, t, p(lengths), p(penalties)), probabilities, out.data_ptr(), ldo,
+                                ws, size, s)
 
 
 AZ_PIPE_GRAPHS = 1
