@@ -90,20 +90,15 @@ __device__ __forceinline__ uint32_t code_pair_bf16(uint32_t w, float scale) {
 
 // 16 bytes of codes of a row from column c on; bytes at and past `cols` read as
 // zero codes.  c is a multiple of 16, and a row holds a multiple of 16 bytes, so
-// that every chunk that begins before cols can be read.
+// that every chunk that begins before cols can be read; one that does not reads the last
+// such chunk and keeps nothing of it.
 __device__ __forceinline__ cm_i32x4 code_chunk(const uint8_t* row, int c, int cols) {
-  cm_i32x4 v = {0, 0, 0, 0};
-  if (c < cols) {
-    v = *reinterpret_cast<const cm_i32x4*>(row + c);
-    const int left = cols - c;
-    if (left < 16) {
+  cm_i32x4 v = *reinterpret_cast<const cm_i32x4*>(row + min(c, (cols - 1) & ~15));
+  const int left = cols - c;
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const int n = left - 4 * i;  // bytes of this word that count
-        if (n <= 0) v[i] = 0;
-        else if (n < 4) v[i] &= (int)((1u << (8 * n)) - 1u);
-      }
-    }
+  for (int i = 0; i < 4; i++) {
+    const int n = max(left - 4 * i, 0);  // bytes of this word that count
+    v[i] &= n >= 4 ? -1 : (int)((1u << (8 * n)) - 1u);
   }
   return v;
 }
