@@ -454,6 +454,7 @@ int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b, const floa
  * bits (scale_rows 1):
  *   dw[n][k] = sum_m dy[m][n] x[m][k],   db[n] = sum_m dy[m][n]
  * (accumulate != 0: added to what dw and db hold).
+ *   x   ld below 2^25.
  *   dy  device, bf16 [x->rows][N], ld_dy elements from row to row; 16-byte aligned rows
  *       (dy and ld_dy) take a faster path.
  *   dw  device, [N][x->cols], dtype AZ_F32 or AZ_BF16, ld_dw elements from row to

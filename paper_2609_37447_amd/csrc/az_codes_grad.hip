@@ -1,15 +1,28 @@
 // The weight's and bias's gradients of a dense layer whose input was saved as
 // codes: dw[n][k] = sum_m dy[m][n] x[m][k], db[n] = sum_m dy[m][n].
 //
-// The summed dimension runs down the rows of both operands.  A saved value is a bf16
-// number exactly, and dy is bf16, so the product runs on the bf16 matrix
-// instruction with exact terms.
+// A saved value is a bf16 number exactly, and dy is bf16, so the product runs on the
+// bf16 matrix instruction with exact terms and fp32 sums.  The summed dimension runs
+// down the rows of both operands: tiles stay in LDS as they lie in memory, and the
+// transposing LDS read gives a lane four rows of its column.
+//
+// Four waves own T = 64 W rows of dw and as many columns, a wave a quarter of them (W x W
+// blocks of 32 x 32), and step through 64 rows of dy and x at a time, two steps' tiles in
+// turn in LDS.  dy is copied straight into LDS (through registers if its rows are not 16-byte
+// aligned); the codes become bf16 on their way through registers, once for the whole workgroup.
+// A wave reads the fragments of half a step while the matrix unit works on the half before.
+//
+// LDS rows hold T bf16 in 16-byte chunks, exchanged by the row (chunk ^ 4 (row % 4)): the four
+// rows that a transposing read takes at a time then lie in different banks.
 #include "az_codes_common.h"
 
 namespace {
 
-constexpr int NT = 256, TN = 64, TK = 64, BM = 64;
-constexpr int LROW = BM + 8;  // LDS row of one n or k: BM bf16 and a pad that spreads the banks
+constexpr int NT = 256;
+constexpr int MS = 64;  // rows of a step
+
+typedef __attribute__((address_space(3))) uint8_t lds_bytes;
+typedef __attribute__((ext_vector_type(4))) __bf16 cm_bf16x4;
 
 template <bool F32>
 __device__ __forceinline__ void put(void* p, int64_t at, float v, bool add) {
@@ -22,84 +35,325 @@ __device__ __forceinline__ void put(void* p, int64_t at, float v, bool add) {
   }
 }
 
-// 64 columns of dy summed by one workgroup: four groups of rows, joined in order.
-__device__ void bias_columns(const uint16_t* __restrict__ dy, int64_t ldy, int n, int m, int n0, float* db, bool add) {
-  __shared__ float sums[4][64];
-  const int c = n0 + (threadIdx.x & 63), q = threadIdx.x >> 6;
-  float s = 0.0f;
-  if (c < n)
-    for (int i = q; i < m; i += 4) s += f32_of_bf16(dy[i * ldy + c]);
-  sums[q][threadIdx.x & 63] = s;
+// Eight bf16 of a row from column c on, zero at and past n; any alignment.
+__device__ __forceinline__ cm_i32x4 row8(const uint16_t* row, int c, int n) {
+  cm_i32x4 v = {0, 0, 0, 0};
+  if (c + 8 <= n) {
+    __builtin_memcpy(&v, row + c, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if (c + i < n) v[i >> 1] |= (int)((uint32_t)row[c + i] << (16 * (i & 1)));
+  }
+  return v;
+}
+
+// 64 columns of dy summed by one workgroup: 32 groups of rows, joined in order.
+__device__ void bias_columns(const uint16_t* __restrict__ dy, int64_t ldy, int n, int m, int n0, float* db, bool add, float* sums) {
+  const int c = (threadIdx.x & 7) * 8, q = threadIdx.x >> 3;
+  float s[8] = {};
+#pragma unroll 8
+  for (int i = q; i < m; i += 32) {
+    const cm_i32x4 v = row8(dy + i * ldy, n0 + c, n);
+#pragma unroll
+    for (int e = 0; e < 8; e++) s[e] += f32_of_bf16(((uint32_t)v[e >> 1] >> (16 * (e & 1))) & 0xffffu);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e++) sums[q * 64 + c + e] = s[e];
   __syncthreads();
-  if (q == 0 && c < n) {
-    const float v = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
-    db[c] = add ? db[c] + v : v;
+  const int t = threadIdx.x;
+  if (t < 64 && n0 + t < n) {
+    float v = 0.0f;
+    for (int i = 0; i < 32; i++) v += sums[i * 64 + t];
+    db[n0 + t] = add ? db[n0 + t] + v : v;
   }
 }
 
-template <bool F32>
-__global__ __launch_bounds__(NT) void az_weight_grad(const uint16_t* __restrict__ dy, int64_t ldy, int n, CodeView x,
-                                                     void* __restrict__ dw, int64_t ldw, float* __restrict__ db,
-                                                     int tiles, int add) {
-  if ((int)blockIdx.x >= tiles) {
-    bias_columns(dy, ldy, n, x.rows, ((int)blockIdx.x - tiles) * 64, db, add);
+template <int W, bool COPY>
+struct Grad {
+  static constexpr int T = 64 * W;
+  static constexpr int ROW = 2 * T;            // LDS bytes of a row
+  static constexpr int TILE = MS * ROW;        // of one operand's step
+  static constexpr int STAGE = 2 * TILE;       // of both
+  static constexpr int YROWS = 1024 / ROW;     // rows that one copy instruction of a wave fills
+  static constexpr int YCOPIES = MS / (4 * YROWS);
+  static constexpr int XCHUNKS = MS * T / 16 / NT;  // 16-code chunks of a thread
+
+  struct Frag {
+    cm_bf16x8 y[2][W], x[2][W];  // two sums of 16 rows
+  };
+
+  // A thread's chunks of a step of dy, straight into LDS; `rows` bytes lie between their rows.
+  static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, lds_bytes* to, uint32_t off, int rows) {
+#pragma unroll
+    for (int j = 0; j < YCOPIES; j++) __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * 4 * YROWS * ROW, 16, off, j * rows, 0, 0);
+  }
+  static __device__ __forceinline__ cm_bf16x8 transposed(const uint8_t* p) {
+    typedef __attribute__((address_space(3))) cm_bf16x4 lds4;
+    const cm_bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)p);
+    const cm_bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 4 * ROW));
+    return cm_bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  }
+  // Fragments of half a step; yo, xo: the lane's places of the W blocks in the half's first rows.
+  static __device__ __forceinline__ void read(Frag& f, const uint8_t* smem, const uint32_t (&yo)[W], const uint32_t (&xo)[W], uint32_t at) {
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+#pragma unroll
+      for (int i = 0; i < W; i++) {
+        f.y[q][i] = transposed(smem + (yo[i] + at) + q * 16 * ROW);
+        f.x[q][i] = transposed(smem + (xo[i] + at) + q * 16 * ROW + TILE);
+      }
+  }
+  static __device__ __forceinline__ void multiply(cm_f32x16 (&acc)[W][W], const Frag& f) {
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+#pragma unroll
+      for (int i = 0; i < W; i++)
+#pragma unroll
+        for (int j = 0; j < W; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.y[q][i], f.x[q][j], acc[i][j], 0, 0, 0);
+  }
+  // Spreads half a step's LDS reads, loads and writes over its matrix instructions, reads first.
+  template <int READS>
+  static __device__ __forceinline__ void interleave() {
+#pragma unroll
+    for (int i = 0; i < 2 * W * W; i++) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i < 8 * W / READS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+      else {
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+      }
+    }
+  }
+};
+
+// Blocks 0..bias-1 sum dy's columns; the others own a tile of dw each, for rows
+// part * rows_of_part on of blockIdx.y = part (sums over several parts go to
+// dw + part * part_stride of a workspace).
+template <int W, bool F32, bool COPY>
+__global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint16_t* __restrict__ dy, int64_t ldy, int n, CodeView x,
+                                                                     void* __restrict__ dw, int64_t ldw, float* __restrict__ db,
+                                                                     int bias, int add, int part_rows, int64_t part_stride, int add_bias) {
+  using G = Grad<W, COPY>;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  if ((int)blockIdx.x < bias) {
+    if (blockIdx.y == 0) bias_columns(dy, ldy, n, x.rows, (int)blockIdx.x * 64, db, add_bias, reinterpret_cast<float*>(smem));
     return;
   }
-  __shared__ uint16_t ys[TN * LROW], xs[TK * LROW];
-  const int kt = (x.cols + TK - 1) / TK;
-  const int n0 = (int)(blockIdx.x / kt) * TN, k0 = (int)(blockIdx.x % kt) * TK;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int wn = (wave & 1) * 32, wk = (wave >> 1) * 32, r = lane & 31, h = lane >> 5;
-  cm_f32x16 acc = {};
-  for (int m0 = 0; m0 < x.rows; m0 += BM) {
-    // A thread takes one row's 16 columns of both operands and writes them as columns.
-    const int mr = t >> 2, c = (t & 3) * 16, m = m0 + mr;
-    uint16_t yv[16], xv[16];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const uint32_t kt = (uint32_t)(x.cols + G::T - 1) / G::T, id = blockIdx.x - bias;
+  const int n0 = (int)(id / kt) * G::T, k0 = (int)(id % kt) * G::T;
+  const int mb = (int)blockIdx.y * part_rows, me = min(mb + part_rows, x.rows);
+
+  // dy, copied: a wave fills YROWS rows at a time, a lane one chunk.
+  const int yr = G::YROWS * wave + lane / (G::T / 8), yp = lane % (G::T / 8), yc = yp ^ ((yr & 3) << 2);
+  const uint32_t yoff = (uint32_t)yr * (uint32_t)ldy * 2u + (uint32_t)yc * 16u;
+  lds_bytes* const ylds = (lds_bytes*)smem + G::YROWS * wave * G::ROW;
+  cm_i32x4 yv[COPY ? 1 : G::YCOPIES];
+  auto copy_y = [&](int m, int stage) {
+    // (past the last row: nothing is in range, and zeros are read)
+    const int rows = min(me - m, MS), first = min(m, me - 1);
+    const uint32_t bytes = (((uint32_t)max(rows, 1) - 1u) * (uint32_t)ldy + (uint32_t)(n - n0)) * 2u;
+    const __amdgpu_buffer_rsrc_t buf =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(dy + first * ldy + n0), 0, (int)(bytes & (uint32_t)-(int)(rows > 0)), 0x00027000);
+    G::copy(buf, ylds + stage, yoff, 4 * G::YROWS * (int)ldy * 2);
+  };
+  auto load_y = [&](int m) {
 #pragma unroll
-    for (int i = 0; i < 16; i++) yv[i] = m < x.rows && n0 + c + i < n ? dy[m * ldy + n0 + c + i] : (uint16_t)0;
-    cm_i32x4 w = {0, 0, 0, 0};
-    float s = 0.0f;
-    if (m < x.rows && k0 + c < x.cols) {
-      w = code_chunk(x.codes + m * x.ld, k0 + c, x.cols);
-      s = scale_value(x.scales[(int64_t)(m >> x.shift) * x.nb + (k0 + c) / CB]);
+    for (int j = 0; j < G::YCOPIES; j++) {
+      const int row = m + yr + j * 4 * G::YROWS;
+      yv[COPY ? 0 : j] = row < me ? row8(dy + row * ldy, n0 + 8 * yc, n) : cm_i32x4{0, 0, 0, 0};
     }
+  };
+  auto store_y = [&](int stage) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const uint32_t lo = code_pair_bf16<false>((uint32_t)w[i], s), hi = code_pair_bf16<true>((uint32_t)w[i], s);
-      xv[4 * i] = (uint16_t)lo;
-      xv[4 * i + 1] = (uint16_t)(lo >> 16);
-      xv[4 * i + 2] = (uint16_t)hi;
-      xv[4 * i + 3] = (uint16_t)(hi >> 16);
+    for (int j = 0; j < G::YCOPIES; j++)
+      *reinterpret_cast<cm_i32x4*>(smem + stage + (yr + j * 4 * G::YROWS) * G::ROW + yp * 16) = yv[COPY ? 0 : j];
+  };
+
+  // x: a thread's chunks of 16 codes, one of each NT * 16 / T rows.
+  constexpr int XR = NT * 16 / G::T;
+  const int xr = t / (G::T / 16), xk = k0 + 16 * (t % (G::T / 16)), xb = min(xk / CB, x.nb - 1);
+  const uint32_t xoff = (uint32_t)xr * (uint32_t)x.ld + (xk < x.cols ? xk : 0);  // (other columns: of no output)
+  const uint32_t soff = (uint32_t)xr * (uint32_t)x.nb + xb;
+  uint8_t* const xlds = smem + G::TILE + xr * G::ROW + (((t % (G::T / 16)) * 2) ^ ((xr & 3) << 2)) * 16;
+  cm_i32x4 xv[G::XCHUNKS];
+  uint32_t xs[G::XCHUNKS];
+  auto load_x = [&](int m) {
+    const int rows = min(me - m, MS), first = min(m, me - 1), some = -(int)(rows > 0);
+    const uint32_t bytes = ((uint32_t)max(rows, 1) - 1u) * (uint32_t)x.ld + (((uint32_t)x.cols + 15u) & ~15u);
+    const __amdgpu_buffer_rsrc_t codes =
+        __builtin_amdgcn_make_buffer_rsrc(x.codes + first * x.ld, 0, (int)(bytes & (uint32_t)some), 0x00027000);
+    const __amdgpu_buffer_rsrc_t scales =
+        __builtin_amdgcn_make_buffer_rsrc(x.scales + (int64_t)first * x.nb, 0, (max(rows, 0) * x.nb) & some, 0x00027000);
+#pragma unroll
+    for (int j = 0; j < G::XCHUNKS; j++) {
+      xv[j] = __builtin_bit_cast(cm_i32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, xoff, j * XR * (int)x.ld, 0));
+      xs[j] = __builtin_amdgcn_raw_buffer_load_b8(scales, soff, j * XR * x.nb, 0);
     }
+  };
+  auto store_x = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < G::XCHUNKS; j++) {
+      const float s = scale_value(xs[j]);
+      cm_i32x4 w[2];
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        w[i >> 1][2 * (i & 1)] = (int)code_pair_bf16<false>((uint32_t)xv[j][i], s);
+        w[i >> 1][2 * (i & 1) + 1] = (int)code_pair_bf16<true>((uint32_t)xv[j][i], s);
+      }
+      cm_i32x4* to = reinterpret_cast<cm_i32x4*>(xlds + stage + j * XR * G::ROW);
+      to[0] = w[0];
+      to[1] = w[1];
+    }
+  };
+
+  // Reading: lane l of 16 takes row l / 4 of four, columns 4 (l % 4) on, and gets its own column.
+  const int wn = (wave & 1) * 32 * W, wk = (wave >> 1) * 32 * W;
+  const int i16 = lane & 15, g = lane >> 4, rr = 8 * (g >> 1) + (i16 >> 2);
+  uint32_t yo[W], xo[W];
+#pragma unroll
+  for (int i = 0; i < W; i++) {
+    const uint32_t in = rr * G::ROW + (2 * (g & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+    yo[i] = in + (((wn / 32 + i) ^ (i16 >> 2)) * 64);
+    xo[i] = in + (((wk / 32 + i) ^ (i16 >> 2)) * 64);
+  }
+  cm_f32x16 acc[W][W];
+#pragma unroll
+  for (int i = 0; i < W; i++)
+#pragma unroll
+    for (int j = 0; j < W; j++) acc[i][j] = cm_f32x16{};
+
+  typename G::Frag f0, f1;
+  load_x(mb);
+  if constexpr (COPY) {
+    copy_y(mb, 0);
+  } else {
+    load_y(mb);
+    store_y(0);
+    load_y(mb + MS);
+  }
+  store_x(0);
+  load_x(mb + MS);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if constexpr (COPY) {
+    copy_y(mb + MS, G::STAGE);
+  } else {
+    store_y(G::STAGE);
+    load_y(mb + 2 * MS);
+  }
+  store_x(G::STAGE);
+  load_x(mb + 2 * MS);
+  G::read(f0, smem, yo, xo, 0);
+  uint32_t stage = 0;
+  for (int m = mb; m < me; m += MS, stage ^= G::STAGE) {
+    G::read(f1, smem, yo, xo, stage + 32 * G::ROW);
+    G::multiply(acc, f0);
+    G::template interleave<2>();
+    __builtin_amdgcn_sched_barrier(0);
+    // This wave's reads of the step are done and its part of the next step's tiles is in LDS; after
+    // the barrier that holds for every wave.
+    __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
+    G::read(f0, smem, yo, xo, stage ^ G::STAGE);
+    if constexpr (COPY) copy_y(m + 2 * MS, (int)stage);
+    else store_y((int)stage);
+    store_x((int)stage);
+    if constexpr (!COPY) load_y(m + 3 * MS);
+    load_x(m + 3 * MS);
+    G::multiply(acc, f1);
+    G::template interleave<2>();
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // no copy into LDS is under way when the workgroup ends
+
+  // D: rows are n, columns are k
+  const int r = lane & 31, h = lane >> 5;
+  const int64_t out = (int64_t)blockIdx.y * part_stride;
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      ys[(c + i) * LROW + mr] = yv[i];
-      xs[(c + i) * LROW + mr] = xv[i];
-    }
-    __syncthreads();
+  for (int j = 0; j < W; j++) {
+    const int k = k0 + wk + 32 * j + r;
+    if (k >= x.cols) continue;
 #pragma unroll
-    for (int q = 0; q < BM / 16; q++) {
-      const cm_bf16x8 fx = *reinterpret_cast<const cm_bf16x8*>(xs + (wk + r) * LROW + 16 * q + 8 * h);
-      const cm_bf16x8 fy = *reinterpret_cast<const cm_bf16x8*>(ys + (wn + r) * LROW + 16 * q + 8 * h);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx, fy, acc, 0, 0, 0);
+    for (int i = 0; i < W; i++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const int nn = n0 + wn + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+        if (nn < n) put<F32>(dw, out + nn * ldw + k, acc[i][j][e], add);
+      }
+  }
+}
+
+// dw from the sums over parts, in the order of the parts.
+template <bool F32>
+__global__ __launch_bounds__(NT) void az_join_parts(const float* __restrict__ parts, int count, int n, int cols,
+                                                    void* __restrict__ dw, int64_t ldw, int add) {
+  const int64_t total = (int64_t)n * cols;
+  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < total; i += (int64_t)gridDim.x * NT) {
+    float v = 0.0f;
+    for (int p = 0; p < count; p++) v += parts[p * total + i];
+    const int64_t r = i / cols;
+    put<F32>(dw, r * ldw + (i - r * cols), v, add);
+  }
+}
+
+// How a gradient is cut: tiles of 64 W, and `parts` parts of the rows.
+struct Cut {
+  int w, parts, part_rows;
+};
+
+// The cheapest cut by an estimate of its time in units of a quarter of a compute unit's
+// matrix work on a 64-row step of a 256 tile: rounds of workgroups times their steps
+// (and four steps' worth of start and end), plus the parts' way through memory (written,
+// read: about 50 outputs a unit).
+Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
+  const int64_t steps = rows > 0 ? (rows + MS - 1) / MS : 1;
+  Cut best = {2, 1, (int)(steps * MS)};
+  double least = 0;
+  for (int w = 4; w >= 2; w -= 2) {
+    const int64_t t = 64 * w, tiles = ((n + t - 1) / t) * ((cols + t - 1) / t);
+    const int64_t slots = w == 4 ? 256 : 512;
+    for (int64_t parts = 1; parts <= 64 && (parts == 1 || parts * 4 <= steps); parts *= 2) {
+      const int64_t per = (steps + parts - 1) / parts;
+      const double rounds = (double)((tiles * parts + slots - 1) / slots);
+      const double cost = rounds * (double)(per + 4) * (w == 4 ? 4.0 : 2.2) +
+                          (parts > 1 ? 8.0 + (double)(parts * n * cols) / 50000.0 : 0.0);
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = {w, (int)((steps + per - 1) / per), (int)(per * MS)};
+      }
     }
   }
-  // D: rows are k, columns are n
-  const int nn = n0 + wn + r;
-  if (nn >= n) return;
-#pragma unroll
-  for (int i = 0; i < 16; i++) {
-    const int k = k0 + wk + 8 * (i >> 2) + 4 * h + (i & 3);
-    if (k < x.cols) put<F32>(dw, nn * ldw + k, acc[i], add);
-  }
+  return best;
+}
+
+template <int W, bool F32, bool COPY>
+void launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add, int add_bias,
+            const Cut& cut, int64_t part_stride, hipStream_t s) {
+  using G = Grad<W, COPY>;
+  constexpr int LDS = 2 * G::STAGE;
+  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_weight_grad<W, F32, COPY>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  (void)once;
+  const int bias = db ? (n + 63) / 64 : 0;
+  const int64_t tiles = (int64_t)((n + G::T - 1) / G::T) * ((x.cols + G::T - 1) / G::T);
+  hipLaunchKernelGGL((az_weight_grad<W, F32, COPY>), dim3((unsigned)(bias + tiles), (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
+                     dw, ldw, db, bias, add, cut.part_rows, part_stride, add_bias);
+}
+
+template <int W, bool F32>
+void launch_copy(bool copy, const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
+                 int add_bias, const Cut& cut, int64_t part_stride, hipStream_t s) {
+  if (copy) launch<W, F32, true>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
+  else launch<W, F32, false>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
 }
 
 }  // namespace
 
 extern "C" size_t az_codes_weight_grad_workspace(int64_t rows, int32_t n, int64_t cols) {
-  (void)rows, (void)n, (void)cols;
-  return 0;
+  if (rows <= 0 || n <= 0 || cols <= 0) return 0;
+  const Cut cut = choose_cut(rows, n, cols);
+  return cut.parts > 1 ? (size_t)cut.parts * (size_t)n * (size_t)cols * sizeof(float) : 0;
 }
 
 extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, const az_code_matrix* x, void* dw,
@@ -109,6 +363,7 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   int st = code_check(x, who);
   if (st != AZ_OK) return st;
   if (x->scale_rows != 1) return code_fail(AZ_ERR_INVALID_ARG, who, "x needs scale_rows 1");
+  if (x->ld >= (1 << 25)) return code_fail(AZ_ERR_UNSUPPORTED, who, "rows of x of 2^25 bytes or more");  // 64 rows in 32-bit offsets
   if (n < 0) return code_fail(AZ_ERR_INVALID_ARG, who, "n < 0");
   if (n == 0) return AZ_OK;
   if ((st = dense_check(dw, dtype, ld_dw, x->cols, who)) != AZ_OK) return st;
@@ -118,15 +373,34 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
   if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
   const CodeView v = code_view(*x);
-  const int64_t tiles = ((int64_t)n + TN - 1) / TN * ((x->cols + TK - 1) / TK);
-  const int64_t blocks = tiles + (db ? ((int64_t)n + 63) / 64 : 0);
-  if (blocks > (1 << 30)) return code_fail(AZ_ERR_UNSUPPORTED, who, "a gradient past the size limits");
+  if ((((int64_t)n + 127) / 128) * ((x->cols + 127) / 128) > (1 << 30))
+    return code_fail(AZ_ERR_UNSUPPORTED, who, "a gradient past the size limits");
+  const Cut cut = choose_cut(x->rows, n, x->cols);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint16_t* y = static_cast<const uint16_t*>(dy);
+  // straight into LDS: whole 16-byte chunks, and a step's offsets below 2^31
+  const bool copy = x->rows > 0 && rows_aligned16(dy, ld_dy, 2) && ld_dy < (1 << 23);
+  const int add = accumulate != 0;
   (void)hipGetLastError();
-  if (dtype == AZ_F32)
-    hipLaunchKernelGGL((az_weight_grad<true>), dim3((unsigned)blocks), dim3(NT), 0, s, y, ld_dy, n, v, dw, ld_dw, db, (int)tiles, accumulate != 0);
-  else
-    hipLaunchKernelGGL((az_weight_grad<false>), dim3((unsigned)blocks), dim3(NT), 0, s, y, ld_dy, n, v, dw, ld_dw, db, (int)tiles, accumulate != 0);
+  const bool direct = cut.parts == 1;
+  void* to = direct ? dw : workspace;
+  const int64_t ld = direct ? ld_dw : x->cols, stride = direct ? 0 : (int64_t)n * x->cols;
+  const int add_here = direct ? add : 0;
+  if (dtype == AZ_F32 || !direct) {
+    if (cut.w == 4) launch_copy<4, true>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    else launch_copy<2, true>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+  } else {
+    if (cut.w == 4) launch_copy<4, false>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    else launch_copy<2, false>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+  }
+  if (!direct) {
+    const int64_t groups = ((int64_t)n * x->cols + NT - 1) / NT;
+    const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
+    if ((st = launch_status(who)) != AZ_OK) return st;
+    if (dtype == AZ_F32)
+      hipLaunchKernelGGL((az_join_parts<true>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, add);
+    else
+      hipLaunchKernelGGL((az_join_parts<false>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, add);
+  }
   return launch_status(who);
 }
