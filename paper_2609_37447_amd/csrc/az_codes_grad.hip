@@ -35,16 +35,33 @@ __device__ __forceinline__ void put(void* p, int64_t at, float v, bool add) {
   }
 }
 
-// Eight bf16 of a row from column c on, zero at and past n; any alignment.
-__device__ __forceinline__ cm_i32x4 row8(const uint16_t* row, int c, int n) {
-  cm_i32x4 v = {0, 0, 0, 0};
-  if (c + 8 <= n) {
-    __builtin_memcpy(&v, row + c, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (c + i < n) v[i >> 1] |= (int)((uint32_t)row[c + i] << (16 * (i & 1)));
+// Eight bf16 of a row of n from column c on, zeros past its end, at any alignment: where the row
+// ends before they do, the row's last eight are read and moved down.  Rows of fewer than
+// eight are read one by one (in kernels that are instantiated for them).
+struct Chunk8 {
+  int at, down;
+  __device__ __forceinline__ Chunk8(int c, int n) : at(min(c, n - 8)), down(min(c - min(c, n - 8), 8) * 16) {}
+  __device__ __forceinline__ cm_i32x4 load(const uint16_t* row) const {
+    cm_i32x4 v;
+    __builtin_memcpy(&v, row + at, 16);
+    return v;
   }
+  __device__ __forceinline__ cm_i32x4 place(const cm_i32x4& v) const {
+    typedef __attribute__((ext_vector_type(2))) uint64_t u64x2;
+    const u64x2 w = __builtin_bit_cast(u64x2, v);
+    u64x2 o;
+    o[0] = down < 64 ? (w[0] >> down) | ((w[1] << 1) << (63 - down)) : w[1] >> (down & 63);
+    o[1] = down < 64 ? w[1] >> down : 0;
+    if (down >= 128) o[0] = 0;
+    return __builtin_bit_cast(cm_i32x4, o);
+  }
+};
+
+__device__ __forceinline__ cm_i32x4 short_row(const uint16_t* row, int c, int n) {
+  cm_i32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    if (c + i < n) v[i >> 1] |= (int)((uint32_t)row[c + i] << (16 * (i & 1)));
   return v;
 }
 
@@ -52,11 +69,23 @@ __device__ __forceinline__ cm_i32x4 row8(const uint16_t* row, int c, int n) {
 __device__ void bias_columns(const uint16_t* __restrict__ dy, int64_t ldy, int n, int m, int n0, float* db, bool add, float* sums) {
   const int c = (threadIdx.x & 7) * 8, q = threadIdx.x >> 3;
   float s[8] = {};
-#pragma unroll 8
-  for (int i = q; i < m; i += 32) {
-    const cm_i32x4 v = row8(dy + i * ldy, n0 + c, n);
+  auto more = [&](const cm_i32x4& v) {
 #pragma unroll
     for (int e = 0; e < 8; e++) s[e] += f32_of_bf16(((uint32_t)v[e >> 1] >> (16 * (e & 1))) & 0xffffu);
+  };
+  if (n >= 8) {
+    const Chunk8 k(n0 + c, n);
+    int i = q;
+    for (; i + 7 * 32 < m; i += 8 * 32) {
+      cm_i32x4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; u++) v[u] = k.load(dy + (i + u * 32) * ldy);
+#pragma unroll
+      for (int u = 0; u < 8; u++) more(k.place(v[u]));
+    }
+    for (; i < m; i += 32) more(k.place(k.load(dy + i * ldy)));
+  } else {
+    for (int i = q; i < m; i += 32) more(short_row(dy + i * ldy, n0 + c, n));
   }
 #pragma unroll
   for (int e = 0; e < 8; e++) sums[q * 64 + c + e] = s[e];
@@ -69,7 +98,11 @@ __device__ void bias_columns(const uint16_t* __restrict__ dy, int64_t ldy, int n
   }
 }
 
-template <int W, bool COPY>
+// How a workgroup gets dy's tiles into LDS: copied (16-byte aligned rows), through registers at
+// any alignment, or element by element (rows of fewer than eight).
+enum { COPY = 0, MOVE = 1, SHORT = 2 };
+
+template <int W>
 struct Grad {
   static constexpr int T = 64 * W;
   static constexpr int ROW = 2 * T;            // LDS bytes of a row
@@ -130,11 +163,11 @@ struct Grad {
 // Blocks 0..bias-1 sum dy's columns; the others own a tile of dw each, for rows
 // part * rows_of_part on of blockIdx.y = part (sums over several parts go to
 // dw + part * part_stride of a workspace).
-template <int W, bool F32, bool COPY>
+template <int W, bool F32, int FEED>
 __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint16_t* __restrict__ dy, int64_t ldy, int n, CodeView x,
                                                                      void* __restrict__ dw, int64_t ldw, float* __restrict__ db,
                                                                      int bias, int add, int part_rows, int64_t part_stride, int add_bias) {
-  using G = Grad<W, COPY>;
+  using G = Grad<W>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   if ((int)blockIdx.x < bias) {
     if (blockIdx.y == 0) bias_columns(dy, ldy, n, x.rows, (int)blockIdx.x * 64, db, add_bias, reinterpret_cast<float*>(smem));
@@ -149,7 +182,6 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   const int yr = G::YROWS * wave + lane / (G::T / 8), yp = lane % (G::T / 8), yc = yp ^ ((yr & 3) << 2);
   const uint32_t yoff = (uint32_t)yr * (uint32_t)ldy * 2u + (uint32_t)yc * 16u;
   lds_bytes* const ylds = (lds_bytes*)smem + G::YROWS * wave * G::ROW;
-  cm_i32x4 yv[COPY ? 1 : G::YCOPIES];
   auto copy_y = [&](int m, int stage) {
     // (past the last row: nothing is in range, and zeros are read)
     const int rows = min(me - m, MS), first = min(m, me - 1);
@@ -158,17 +190,23 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
         __builtin_amdgcn_make_buffer_rsrc((void*)(dy + first * ldy + n0), 0, (int)(bytes & (uint32_t)-(int)(rows > 0)), 0x00027000);
     G::copy(buf, ylds + stage, yoff, 4 * G::YROWS * (int)ldy * 2);
   };
+  const Chunk8 yk(n0 + 8 * yc, n);
+  cm_i32x4 yv[FEED == COPY ? 1 : G::YCOPIES];
   auto load_y = [&](int m) {
 #pragma unroll
     for (int j = 0; j < G::YCOPIES; j++) {
-      const int row = m + yr + j * 4 * G::YROWS;
-      yv[COPY ? 0 : j] = row < me ? row8(dy + row * ldy, n0 + 8 * yc, n) : cm_i32x4{0, 0, 0, 0};
+      const uint16_t* row = dy + min(m + yr + j * 4 * G::YROWS, me - 1) * ldy;
+      yv[FEED == COPY ? 0 : j] = FEED == SHORT ? short_row(row, n0 + 8 * yc, n) : yk.load(row);
     }
   };
-  auto store_y = [&](int stage) {
+  auto store_y = [&](int m, int stage) {
 #pragma unroll
-    for (int j = 0; j < G::YCOPIES; j++)
-      *reinterpret_cast<cm_i32x4*>(smem + stage + (yr + j * 4 * G::YROWS) * G::ROW + yp * 16) = yv[COPY ? 0 : j];
+    for (int j = 0; j < G::YCOPIES; j++) {
+      cm_i32x4 v = yv[FEED == COPY ? 0 : j];
+      if constexpr (FEED == MOVE) v = yk.place(v);
+      if (m + yr + j * 4 * G::YROWS >= me) v = cm_i32x4{0, 0, 0, 0};
+      *reinterpret_cast<cm_i32x4*>(smem + stage + (yr + j * 4 * G::YROWS) * G::ROW + yp * 16) = v;
+    }
   };
 
   // x: a thread's chunks of 16 codes, one of each NT * 16 / T rows.
@@ -226,21 +264,21 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
 
   typename G::Frag f0, f1;
   load_x(mb);
-  if constexpr (COPY) {
+  if constexpr (FEED == COPY) {
     copy_y(mb, 0);
   } else {
     load_y(mb);
-    store_y(0);
+    store_y(mb, 0);
     load_y(mb + MS);
   }
   store_x(0);
   load_x(mb + MS);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  if constexpr (COPY) {
+  if constexpr (FEED == COPY) {
     copy_y(mb + MS, G::STAGE);
   } else {
-    store_y(G::STAGE);
+    store_y(mb + MS, G::STAGE);
     load_y(mb + 2 * MS);
   }
   store_x(G::STAGE);
@@ -257,10 +295,10 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     G::read(f0, smem, yo, xo, stage ^ G::STAGE);
-    if constexpr (COPY) copy_y(m + 2 * MS, (int)stage);
-    else store_y((int)stage);
+    if constexpr (FEED == COPY) copy_y(m + 2 * MS, (int)stage);
+    else store_y(m + 2 * MS, (int)stage);
     store_x((int)stage);
-    if constexpr (!COPY) load_y(m + 3 * MS);
+    if constexpr (FEED != COPY) load_y(m + 3 * MS);
     load_x(m + 3 * MS);
     G::multiply(acc, f1);
     G::template interleave<2>();
@@ -310,7 +348,7 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
   const int64_t steps = rows > 0 ? (rows + MS - 1) / MS : 1;
   Cut best = {2, 1, (int)(steps * MS)};
   double least = 0;
-  for (int w = 4; w >= 2; w -= 2) {
+  for (int w = n < 8 ? 2 : 4; w >= 2; w -= 2) {  // (rows of fewer than eight are read by the small tile alone)
     const int64_t t = 64 * w, tiles = ((n + t - 1) / t) * ((cols + t - 1) / t);
     const int64_t slots = w == 4 ? 256 : 512;
     for (int64_t parts = 1; parts <= 64 && (parts == 1 || parts * 4 <= steps); parts *= 2) {
@@ -327,25 +365,26 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
   return best;
 }
 
-template <int W, bool F32, bool COPY>
+template <int W, bool F32, int FEED>
 void launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add, int add_bias,
             const Cut& cut, int64_t part_stride, hipStream_t s) {
-  using G = Grad<W, COPY>;
+  using G = Grad<W>;
   constexpr int LDS = 2 * G::STAGE;
-  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_weight_grad<W, F32, COPY>),
+  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_weight_grad<W, F32, FEED>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   (void)once;
   const int bias = db ? (n + 63) / 64 : 0;
   const int64_t tiles = (int64_t)((n + G::T - 1) / G::T) * ((x.cols + G::T - 1) / G::T);
-  hipLaunchKernelGGL((az_weight_grad<W, F32, COPY>), dim3((unsigned)(bias + tiles), (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
+  hipLaunchKernelGGL((az_weight_grad<W, F32, FEED>), dim3((unsigned)(bias + tiles), (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
                      dw, ldw, db, bias, add, cut.part_rows, part_stride, add_bias);
 }
 
 template <int W, bool F32>
-void launch_copy(bool copy, const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
+void launch_feed(int feed, const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
                  int add_bias, const Cut& cut, int64_t part_stride, hipStream_t s) {
-  if (copy) launch<W, F32, true>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
-  else launch<W, F32, false>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
+  if (feed == COPY) launch<W, F32, COPY>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
+  else if (feed == MOVE) launch<W, F32, MOVE>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
+  else if constexpr (W == 2) launch<W, F32, SHORT>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
 }
 
 }  // namespace
@@ -378,8 +417,8 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   const Cut cut = choose_cut(x->rows, n, x->cols);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint16_t* y = static_cast<const uint16_t*>(dy);
-  // straight into LDS: whole 16-byte chunks, and a step's offsets below 2^31
-  const bool copy = x->rows > 0 && rows_aligned16(dy, ld_dy, 2) && ld_dy < (1 << 23);
+  // straight into LDS: whole 16-byte chunks, and a step's offsets below 2^31 (no rows: nothing is read)
+  const int feed = x->rows == 0 || (rows_aligned16(dy, ld_dy, 2) && ld_dy < (1 << 23)) ? COPY : n >= 8 ? MOVE : SHORT;
   const int add = accumulate != 0;
   (void)hipGetLastError();
   const bool direct = cut.parts == 1;
@@ -387,11 +426,11 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   const int64_t ld = direct ? ld_dw : x->cols, stride = direct ? 0 : (int64_t)n * x->cols;
   const int add_here = direct ? add : 0;
   if (dtype == AZ_F32 || !direct) {
-    if (cut.w == 4) launch_copy<4, true>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
-    else launch_copy<2, true>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    if (cut.w == 4) launch_feed<4, true>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    else launch_feed<2, true>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
   } else {
-    if (cut.w == 4) launch_copy<4, false>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
-    else launch_copy<2, false>(copy, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    if (cut.w == 4) launch_feed<4, false>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    else launch_feed<2, false>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
   }
   if (!direct) {
     const int64_t groups = ((int64_t)n * x->cols + NT - 1) / NT;
