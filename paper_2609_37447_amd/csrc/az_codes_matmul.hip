@@ -132,32 +132,6 @@ __device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, in
   tn = (int)(in / high);
 }
 
-// Four neighbouring results of a row, n..n+3.  vec: rows are aligned for one store.
-template <bool F32>
-__device__ __forceinline__ void store4(void* out, int64_t at, int n, int rows, const float* v, bool vec) {
-  if constexpr (F32) {
-    float* o = (float*)out + at;
-    if (vec && n + 4 <= rows) {
-      *reinterpret_cast<cm_f32x4*>(o) = cm_f32x4{v[0], v[1], v[2], v[3]};
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; e++)
-      if (n + e < rows) o[e] = v[e];
-  } else {
-    uint16_t* o = (uint16_t*)out + at;
-    if (vec && n + 4 <= rows) {
-      const cm_i32x2 w = {(int)((uint32_t)bf16_of(v[0]) | ((uint32_t)bf16_of(v[1]) << 16)),
-                          (int)((uint32_t)bf16_of(v[2]) | ((uint32_t)bf16_of(v[3]) << 16))};
-      *reinterpret_cast<cm_i32x2*>(o) = w;
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; e++)
-      if (n + e < rows) o[e] = bf16_of(v[e]);
-  }
-}
-
 typedef __attribute__((address_space(3))) uint8_t lds_bytes;
 
 // Large products.  Four waves own a square tile of 64 W rows of each operand, a wave a
@@ -168,33 +142,35 @@ typedef __attribute__((address_space(3))) uint8_t lds_bytes;
 // LDS rows are 128 bytes, their 16-byte chunks exchanged by the row's place (chunk ^ (row /
 // 2) % 8), which spreads the 16 rows that are read together over all banks.  The copy into
 // LDS puts lanes side by side, so that the exchange is made on the source address.
-template <int W, bool F32>
+template <int W, int NW, bool F32>
 struct Tiled {
   static constexpr int T = 64 * W;           // rows of a and of b of a tile
   static constexpr int STEP = T * CB;        // LDS bytes of one operand's step
   static constexpr int SCALES = 2 * STEP;    // where a word of scale bytes for each row of a, then of b, begins
   static constexpr int STAGE = 2 * STEP + 2 * T * 4;
-  static constexpr int CHUNKS = T / 32;      // 16-byte chunks a thread copies of one operand's step
+  static constexpr int ROWS = 8 * NW;        // rows that one copy instruction of the workgroup fills
+  static constexpr int CHUNKS = T / ROWS;
+  static constexpr int FA = W, FB = 4 * W / NW;  // 32-row blocks of a wave
 
   struct Frag {
-    cm_i32x8 a[W], b[W];
+    cm_i32x8 a[FA], b[FB];
   };
 
-  // A thread's chunks of a step, one of each 32 rows: `off` within the step's first rows, `at`
+  // A thread's chunks of a step, one of each ROWS rows: `off` within the step's first rows, `at`
   // the step's place in the tile.
   static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, int ld, uint32_t off, int at, lds_bytes* to) {
 #pragma unroll
     for (int j = 0; j < CHUNKS; j++)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * 32 * CB, 16, off, at + j * 32 * ld, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * ROWS * CB, 16, off, at + j * ROWS * ld, 0, 0);
   }
   // Spreads half a step's LDS reads (of the next half's fragments) and loads over its matrix
   // instructions, reads first, so that they are back before the half ends.
   static __device__ __forceinline__ void interleave() {
     if constexpr (!F32) {
 #pragma unroll
-      for (int i = 0; i < W * W; i++) {
+      for (int i = 0; i < FA * FB; i++) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
-        if (i < 2 * W) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // LDS reads
+        if (i < FA + FB) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // LDS reads
         else __builtin_amdgcn_sched_group_barrier(0x020, 3, 0);  // copies
       }
     }
@@ -205,31 +181,29 @@ struct Tiled {
   }
   static __device__ __forceinline__ void read(Frag& f, const uint8_t* a0, const uint8_t* a1, const uint8_t* b0, const uint8_t* b1) {
 #pragma unroll
-    for (int i = 0; i < W; i++) {
-      f.a[i] = fragment(a0 + i * 32 * CB, a1 + i * 32 * CB);
-      f.b[i] = fragment(b0 + i * 32 * CB, b1 + i * 32 * CB);
-    }
+    for (int i = 0; i < FA; i++) f.a[i] = fragment(a0 + i * 32 * CB, a1 + i * 32 * CB);
+#pragma unroll
+    for (int j = 0; j < FB; j++) f.b[j] = fragment(b0 + j * 32 * CB, b1 + j * 32 * CB);
   }
-  static __device__ __forceinline__ void multiply(cm_f32x16 (&acc)[W][W], const Frag& f, const uint32_t (&sa)[W], const uint32_t (&sb)[W]) {
+  static __device__ __forceinline__ void multiply(cm_f32x16 (&acc)[FA][FB], const Frag& f, const uint32_t (&sa)[FA], const uint32_t (&sb)[FB]) {
     if constexpr (!F32) {
 #pragma unroll
-      for (int i = 0; i < W; i++)
+      for (int i = 0; i < FA; i++)
 #pragma unroll
-        for (int j = 0; j < W; j++)
+        for (int j = 0; j < FB; j++)
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j], f.a[i], acc[i][j], 0, 0, 0, (int)sb[j], 0, (int)sa[i]);
     } else {
 #pragma unroll
       for (int q = 0; q < 4; q++) {
-        cm_bf16x8 va[W], vb[W];
+        cm_bf16x8 va[FA], vb[FB];
 #pragma unroll
-        for (int i = 0; i < W; i++) {
-          va[i] = fragment_bf16(f.a[i], q, scale_value(sa[i]));
-          vb[i] = fragment_bf16(f.b[i], q, scale_value(sb[i]));
-        }
+        for (int i = 0; i < FA; i++) va[i] = fragment_bf16(f.a[i], q, scale_value(sa[i]));
 #pragma unroll
-        for (int i = 0; i < W; i++)
+        for (int j = 0; j < FB; j++) vb[j] = fragment_bf16(f.b[j], q, scale_value(sb[j]));
 #pragma unroll
-          for (int j = 0; j < W; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j], va[i], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < FA; i++)
+#pragma unroll
+          for (int j = 0; j < FB; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j], va[i], acc[i][j], 0, 0, 0);
       }
     }
   }
@@ -248,10 +222,10 @@ struct ScaleWords {
   __device__ __forceinline__ uint32_t place(const CodeView& m, int row) const { return skip + (uint32_t)(row >> m.shift) * (uint32_t)m.nb; }
 };
 
-template <int W, bool F32>
-__global__ __launch_bounds__(256, W == 4 ? 1 : 2) void az_matmul_tiled(CodeView a, CodeView b, const float* __restrict__ bias,
-                                                                       void* __restrict__ out, int64_t ldo, int mt, int nt, int vec) {
-  using K = Tiled<W, F32>;
+template <int W, int NW, bool F32>
+__global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_tiled(CodeView a, CodeView b, const float* __restrict__ bias,
+                                                                       void* __restrict__ out, int64_t ldo, int mt, int nt) {
+  using K = Tiled<W, NW, F32>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   int tm, tn;
@@ -267,11 +241,12 @@ __global__ __launch_bounds__(256, W == 4 ? 1 : 2) void az_matmul_tiled(CodeView 
   const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, K::T * (int)b.ld, 0x00027000);
   lds_bytes* const lds0 = (lds_bytes*)smem + 8 * wave * CB;
   const int whole = a.cols / CB;  // steps that fill their columns
-  // Scales: a thread's row of a (T = 256: also of b; 128: the upper half of the threads, of b instead).
+  // Scales: a thread's row of a and of b, or of a for half of the threads and of b for the others.
   const ScaleWords aw(a), bw(b);
-  const bool half = K::T == 128 && wave >= 2;
-  const uint32_t srow = half ? bw.place(b, n0 + (t & 127)) : aw.place(a, m0 + (t & (K::T - 1)));
-  const uint32_t srow2 = K::T == 256 ? bw.place(b, n0 + t) : 0u;
+  constexpr bool BOTH = 64 * NW == K::T;
+  const bool half = !BOTH && wave >= NW / 2;
+  const uint32_t srow = half ? bw.place(b, n0 + (t & (K::T - 1))) : aw.place(a, m0 + (t & (K::T - 1)));
+  const uint32_t srow2 = BOTH ? bw.place(b, n0 + t) : 0u;
   lds_bytes* const slds = (lds_bytes*)smem + K::SCALES + wave * 64 * 4;
   // (past the last step: that step again, which nothing reads)
   auto fetch = [&](int kb) {
@@ -280,37 +255,35 @@ __global__ __launch_bounds__(256, W == 4 ? 1 : 2) void az_matmul_tiled(CodeView 
     K::copy(abuf, (int)a.ld, aoff, kb * CB, lds0 + stage);
     K::copy(bbuf, (int)b.ld, boff, kb * CB, lds0 + stage + K::STEP);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(half ? bw.words : aw.words, slds + stage, 4, (srow + kb) & ~3u, 0, 0, 0);
-    if constexpr (K::T == 256)
+    if constexpr (BOTH)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(bw.words, slds + stage + K::T * 4, 4, (srow2 + kb) & ~3u, 0, 0, 0);
   };
 
   // Reading: a lane holds row l % 32 of a block, columns 32 (l / 32) + 64 s on of half s.
-  const int r = lane & 31, h = lane >> 5, wm = (wave & 1) * 32 * W, wn = (wave >> 1) * 32 * W;
+  const int r = lane & 31, h = lane >> 5, wm = (wave & 1) * 32 * K::FA, wn = (wave >> 1) * 32 * K::FB;
   const int sw = (r >> 1) & 7;
   const uint8_t* ap = smem + (wm + r) * CB;
   const uint8_t* bp = smem + K::STEP + (wn + r) * CB;
   const int at[2][2] = {{((2 * h) ^ sw) * 16, ((2 * h + 1) ^ sw) * 16}, {((2 * h + 4) ^ sw) * 16, ((2 * h + 5) ^ sw) * 16}};
-  uint32_t ac[W], bc[W];  // places of the lane's rows' scales
+  uint32_t ac[K::FA], bc[K::FB];  // places of the lane's rows' scales
 #pragma unroll
-  for (int i = 0; i < W; i++) {
-    ac[i] = aw.place(a, m0 + wm + 32 * i + r);
-    bc[i] = bw.place(b, n0 + wn + 32 * i + r);
-  }
-  uint32_t sa[W], sb[W], na[W], nb[W];
-  auto scales = [&](uint32_t (&pa)[W], uint32_t (&pb)[W], int kb) {
+  for (int i = 0; i < K::FA; i++) ac[i] = aw.place(a, m0 + wm + 32 * i + r);
+#pragma unroll
+  for (int j = 0; j < K::FB; j++) bc[j] = bw.place(b, n0 + wn + 32 * j + r);
+  uint32_t sa[K::FA], sb[K::FB], na[K::FA], nb[K::FB];
+  auto scales = [&](uint32_t (&pa)[K::FA], uint32_t (&pb)[K::FB], int kb) {
     const uint8_t* from = smem + (kb & 1) * K::STAGE + K::SCALES + r * 4;
 #pragma unroll
-    for (int i = 0; i < W; i++) {
-      pa[i] = from[(wm + 32 * i) * 4 + ((ac[i] + kb) & 3u)];
-      pb[i] = from[(K::T + wn + 32 * i) * 4 + ((bc[i] + kb) & 3u)];
-    }
+    for (int i = 0; i < K::FA; i++) pa[i] = from[(wm + 32 * i) * 4 + ((ac[i] + kb) & 3u)];
+#pragma unroll
+    for (int j = 0; j < K::FB; j++) pb[j] = from[(K::T + wn + 32 * j) * 4 + ((bc[j] + kb) & 3u)];
   };
 
-  cm_f32x16 acc[W][W];
+  cm_f32x16 acc[K::FA][K::FB];
 #pragma unroll
-  for (int i = 0; i < W; i++)
+  for (int i = 0; i < K::FA; i++)
 #pragma unroll
-    for (int j = 0; j < W; j++) acc[i][j] = cm_f32x16{};
+    for (int j = 0; j < K::FB; j++) acc[i][j] = cm_f32x16{};
   typename K::Frag f0, f1;
   if (whole > 0) {
     fetch(0);
@@ -337,41 +310,65 @@ __global__ __launch_bounds__(256, W == 4 ? 1 : 2) void az_matmul_tiled(CodeView 
     K::multiply(acc, f1, sa, sb);
     K::interleave();
 #pragma unroll
-    for (int i = 0; i < W; i++) {
-      sa[i] = na[i];
-      sb[i] = nb[i];
-    }
+    for (int i = 0; i < K::FA; i++) sa[i] = na[i];
+#pragma unroll
+    for (int j = 0; j < K::FB; j++) sb[j] = nb[j];
   }
   __builtin_amdgcn_s_waitcnt(0);  // no copy into LDS is under way when the workgroup ends
   if (whole < a.nb) {  // the columns that do not fill a step, straight from memory
 #pragma unroll
-    for (int i = 0; i < W; i++) {
-      sa[i] = a.scales[ac[i] - aw.skip + whole];
-      sb[i] = b.scales[bc[i] - bw.skip + whole];
-    }
+    for (int i = 0; i < K::FA; i++) sa[i] = a.scales[ac[i] - aw.skip + whole];
+#pragma unroll
+    for (int j = 0; j < K::FB; j++) sb[j] = b.scales[bc[j] - bw.skip + whole];
 #pragma unroll
     for (int s = 0; s < 2; s++) {
 #pragma unroll
-      for (int i = 0; i < W; i++) {
-        f0.a[i] = row_fragment(a.codes + (m0 + wm + 32 * i + r) * a.ld, whole * CB + 64 * s + 32 * h, a.cols);
-        f0.b[i] = row_fragment(b.codes + (n0 + wn + 32 * i + r) * b.ld, whole * CB + 64 * s + 32 * h, a.cols);
-      }
+      for (int i = 0; i < K::FA; i++) f0.a[i] = row_fragment(a.codes + (m0 + wm + 32 * i + r) * a.ld, whole * CB + 64 * s + 32 * h, a.cols);
+#pragma unroll
+      for (int j = 0; j < K::FB; j++) f0.b[j] = row_fragment(b.codes + (n0 + wn + 32 * j + r) * b.ld, whole * CB + 64 * s + 32 * h, a.cols);
       K::multiply(acc, f0, sa, sb);
     }
   }
+  // Results leave through LDS, so that whole rows of the tile are written: a lane's four neighbours
+  // would be 16 bytes of each of 32 rows.  Chunks are exchanged by the row, as above.
+  constexpr int ES = F32 ? 4 : 2, OROW = K::T * ES;
+  constexpr int PASSES = 2 * K::STAGE >= K::T * OROW ? 1 : 2;  // fp32: half of each wave's rows at a time
+  constexpr int PF = K::FA / PASSES, PROWS = K::T / PASSES;
 #pragma unroll
-  for (int i = 0; i < W; i++) {
-    const int m = m0 + wm + 32 * i + r;
+  for (int p = 0; p < PASSES; p++) {
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < W; j++)
+    for (int j = 0; j < K::FB; j++)
 #pragma unroll
       for (int q = 0; q < 4; q++) {
-        const int n = n0 + wn + 32 * j + 8 * q + 4 * h;
-        float v[4];
+        const int n = wn + 32 * j + 8 * q + 4 * h;
+        cm_f32x4 add = {0, 0, 0, 0};
+        if (bias) __builtin_memcpy(&add, bias + n0 + n, 16);
 #pragma unroll
-        for (int e = 0; e < 4; e++) v[e] = acc[i][j][4 * q + e] + (bias ? bias[n + e] : 0.0f);
-        store4<F32>(out, m * ldo + n, n, b.rows, v, vec);
+        for (int i = 0; i < PF; i++) {
+          const int row = (wave & 1) * 32 * PF + 32 * i + r;
+          cm_f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; e++) v[e] = acc[PF * p + i][j][4 * q + e] + add[e];
+          if constexpr (F32) {
+            *reinterpret_cast<cm_f32x4*>(smem + row * OROW + (((n >> 2) ^ r) * 16)) = v;
+          } else {
+            const cm_i32x2 w = {(int)((uint32_t)bf16_of(v[0]) | ((uint32_t)bf16_of(v[1]) << 16)),
+                                (int)((uint32_t)bf16_of(v[2]) | ((uint32_t)bf16_of(v[3]) << 16))};
+            *reinterpret_cast<cm_i32x2*>(smem + row * OROW + (((n >> 3) ^ (r & (OROW / 16 - 1))) * 16) + (n & 4) * 2) = w;
+          }
+        }
       }
+    __syncthreads();
+    constexpr int RC = OROW / 16;  // chunks of a row
+#pragma unroll 8
+    for (int c = t; c < PROWS * RC; c += 64 * NW) {
+      const int row = c / RC, in = c % RC;
+      const cm_i32x4 v = *reinterpret_cast<const cm_i32x4*>(smem + row * OROW + ((in ^ (row & 31 & (RC - 1))) * 16));
+      // rows of the two halves of the waves lie FA blocks apart
+      const int m = m0 + row / (32 * PF) * (32 * K::FA) + p * 32 * PF + row % (32 * PF);
+      __builtin_memcpy((uint8_t*)out + ((int64_t)m * ldo + n0) * ES + in * 16, &v, 16);
+    }
   }
 }
 
@@ -381,23 +378,21 @@ void launch_direct(const CodeView& a, const CodeView& b, const float* bias, void
   hipLaunchKernelGGL((az_matmul_direct<FM, FN, NW, F32>), g, dim3(NW * 64), 0, s, a, b, bias, out, ldo);
 }
 
-template <int W, bool F32>
+template <int W, int NW, bool F32>
 void launch_tiled(const CodeView& a, const CodeView& b, const float* bias, void* out, int64_t ldo, hipStream_t s) {
-  using K = Tiled<W, F32>;
-  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<W, F32>),
+  using K = Tiled<W, NW, F32>;
+  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<W, NW, F32>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, 2 * K::STAGE);
   (void)once;
   const int mt = (a.rows + K::T - 1) / K::T, nt = (b.rows + K::T - 1) / K::T;
-  const int esz = F32 ? 4 : 2;
-  const int vec = ((uintptr_t)out % (4 * esz)) == 0 && ldo % 4 == 0;
-  hipLaunchKernelGGL((az_matmul_tiled<W, F32>), dim3((unsigned)mt * (unsigned)nt), dim3(256), 2 * K::STAGE, s, a, b, bias, out, ldo, mt, nt, vec);
+  hipLaunchKernelGGL((az_matmul_tiled<W, NW, F32>), dim3((unsigned)mt * (unsigned)nt), dim3(64 * NW), 2 * K::STAGE, s, a, b, bias, out, ldo, mt, nt);
 }
 
 template <bool F32>
 void launch(const CodeView& a, const CodeView& b, const float* bias, void* out, int64_t ldo, hipStream_t s) {
   const bool fits = a.ld < (1 << 22) && b.ld < (1 << 22);  // a tile's offsets stay below 2^30
-  if (fits && a.rows >= 1024 && b.rows >= 256) { launch_tiled<4, F32>(a, b, bias, out, ldo, s); return; }
-  if (fits && a.rows >= 128 && b.rows >= 128) { launch_tiled<2, F32>(a, b, bias, out, ldo, s); return; }
+  if (fits && a.rows >= 1024 && b.rows >= 256) { launch_tiled<4, 4, F32>(a, b, bias, out, ldo, s); return; }
+  if (fits && a.rows >= 128 && b.rows >= 128) { launch_tiled<2, 4, F32>(a, b, bias, out, ldo, s); return; }
   if (a.rows <= 16) launch_direct<1, 1, 8, F32>(a, b, bias, out, ldo, s);
   else if (a.rows <= 64) launch_direct<4, 1, 8, F32>(a, b, bias, out, ldo, s);
   else launch_direct<4, 4, 4, F32>(a, b, bias, out, ldo, s);
