@@ -501,7 +501,7 @@ typedef struct {
  * out[v] = exp(l[v] - max l) / sum exp(l - max l), exactly 0.0f where v is not
  * allowed; a row in which nothing is allowed (or every allowed l is -inf) is all
  * zero.  What the logits hold where v is not allowed, NaN or infinities, does
- * not matter.  A NaN or +inf that is allowed makes the row's allowed entries NaN.
+ * not matter.  A NaN or +inf that is allowed makes every allowed l above -inf NaN.
  *   out        device, [rows][vocab] fp32, ld_out elements from row to row.  It may be
  *              the logits' own buffer (AZ_F32, ld_out = ld), and may not overlap any
  *              input otherwise.
