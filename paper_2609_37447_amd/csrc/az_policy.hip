@@ -14,8 +14,10 @@
 
 namespace {
 
-constexpr int PER = 16;           // entries of a thread, in two groups of eight
-constexpr int MOST = 1024 * PER;  // entries of a workgroup
+constexpr int GROUPS = 4;               // a thread's groups of four entries
+constexpr int PER = 4 * GROUPS;         // entries of a thread
+constexpr int THREADS = 1024;           // of the largest workgroup
+constexpr int MOST = THREADS * PER;     // entries of a workgroup
 constexpr float LOG2E = 1.44269504088896340736f;
 
 struct PolicyView {
@@ -34,79 +36,146 @@ struct PolicyView {
 // exp(l - m); 0 for l = -inf where m is finite.
 __device__ __forceinline__ float exp_below(float l, float m) { return __builtin_amdgcn_exp2f((l - m) * LOG2E); }
 
-// (maximum, sum of exp(l - maximum)) of two parts; a part without an entry above -inf
-// has maximum -inf and sum 0, or NaN where it holds one.
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2);
-  s = top == -INFINITY ? s + s2 : s * exp_below(m, top) + s2 * exp_below(m2, top);
-  m = top;
+// Maximum (of what is not NaN) and sum over a wave, in every lane, by lane exchanges of the
+// vector unit.
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float x) {
+  const int i = __float_as_int(x);
+  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, CTRL, 0xf, 0xf, false));
 }
+template <class F>
+__device__ __forceinline__ float wave_all(float x, F&& f) {
+  x = f(x, lane_move<0xb1>(x));   // lane ^ 1
+  x = f(x, lane_move<0x4e>(x));   // lane ^ 2
+  x = f(x, lane_move<0x141>(x));  // the other four of eight
+  x = f(x, lane_move<0x140>(x));  // the other eight of sixteen
+  x = f(x, __shfl_xor(x, 16));
+  return f(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float wave_top(float x) { return wave_all(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_total(float x) { return wave_all(x, [](float a, float b) { return a + b; }); }
 
-// Eight entries from v on, adjusted; -inf where they are not allowed and past the vocabulary.
-template <bool HIST>
-__device__ __forceinline__ void load8(const PolicyView& p, int64_t b, int v, const uint32_t* count, float rep, float freq, float pres,
-                                      float (&l)[8]) {
-  if (v + 8 <= p.vocab) {
-    if (p.bf16) {
-      cm_i32x4 w;
-      __builtin_memcpy(&w, (const uint16_t*)p.logits + b * p.ld + v, 16);
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        l[2 * i] = __uint_as_float((uint32_t)w[i] << 16);
-        l[2 * i + 1] = __uint_as_float((uint32_t)w[i] & 0xffff0000u);
-      }
+// A row's penalties.  l / r is a product with 1 / r and one correction, which gives the
+// quotient to the last place; where 1 / r is not a normal number, it is divided.
+struct Penalties {
+  float r, inv, f, p;
+  bool divide;
+  __device__ __forceinline__ Penalties() {}
+  __device__ __forceinline__ explicit Penalties(const float* x) : r(x[0]), inv(1.0f / x[0]), f(x[1]), p(x[2]) {
+    divide = !(inv >= 0x1p-126f && inv <= 0x1p126f);
+  }
+  __device__ __forceinline__ float of(float l, uint32_t c) const {
+    float q;
+    if (divide) {
+      q = l / r;
     } else {
-      __builtin_memcpy(l, (const float*)p.logits + b * p.ld + v, 32);
+      const float q0 = l * inv;
+      q = fmaf(fmaf(-q0, r, l), inv, q0);
+      if (fabsf(q0) == INFINITY) q = q0;
     }
-    float add[8] = {};
-    if (p.bias) __builtin_memcpy(add, p.bias + b * p.ld_bias + v, 32);
-    uint32_t ok = 0xffu;
+    return (l > 0.0f ? q : l * r) - fmaf(f, (float)c, p);
+  }
+};
+
+// Four entries from v on.  They are loaded as they lie in memory and looked at later, so that a
+// thread's loads are on their way together; a group past the vocabulary's end reads its last four.
+struct Entries {
+  cm_f32x4 l, add;
+  uint32_t ok;
+
+  // The adjusted logits, -inf where they are not allowed and past the vocabulary.
+  template <bool HIST>
+  __device__ __forceinline__ void adjust(const PolicyView& p, int64_t b, int v, const uint32_t* count, const Penalties& pen) {
+    if (p.bf16) {
+      const float w0 = l[0], w1 = l[1];
+      l = cm_f32x4{__uint_as_float(__float_as_uint(w0) << 16), __uint_as_float(__float_as_uint(w0) & 0xffff0000u),
+                   __uint_as_float(__float_as_uint(w1) << 16), __uint_as_float(__float_as_uint(w1) & 0xffff0000u)};
+    }
+    // one bit for each entry, at 8 i + 7
     if (p.mask_kind == AZ_MASK_BYTES) {
-      uint64_t w;
-      __builtin_memcpy(&w, (const uint8_t*)p.mask + b * p.ld_mask + v, 8);
-      ok = 0;
-#pragma unroll
-      for (int i = 0; i < 8; i++) ok |= ((w >> (8 * i)) & 0xffu) != 0 ? 1u << i : 0u;
+      ok |= (ok & 0x7f7f7f7fu) + 0x7f7f7f7fu;
     } else if (p.mask_kind == AZ_MASK_BITS) {
-      ok = ((const uint8_t*)p.mask)[4 * b * p.ld_mask + (v >> 3)];
+      ok = ok >> (v & 4);
+      ok = (ok & 1u) << 7 | (ok & 2u) << 14 | (ok & 4u) << 21 | (ok & 8u) << 28;
+    } else {
+      ok = 0x80808080u;
     }
+    if (v + 4 > p.vocab) edge(p, b, v);
+    if constexpr (HIST) {
+      const cm_i32x4 c = *reinterpret_cast<const cm_i32x4*>(count);
+      if (c[0] | c[1] | c[2] | c[3]) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      if constexpr (HIST) {
-        const uint32_t c = count[i];
-        if (c) l[i] = (l[i] > 0.0f ? l[i] / rep : l[i] * rep) - (freq * (float)c + pres);
+        for (int i = 0; i < 4; i++) l[i] = c[i] ? pen.of(l[i], (uint32_t)c[i]) : l[i];
       }
-      l[i] = ok & (1u << i) ? l[i] + add[i] : -INFINITY;
     }
-  } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      l[i] = -INFINITY;
-      const int64_t u = v + i;
+    for (int i = 0; i < 4; i++) {
+      const uint32_t keep = (uint32_t)((int32_t)(ok << (24 - 8 * i)) >> 31), sum = __float_as_uint(l[i] + add[i]);
+      l[i] = __uint_as_float((sum & keep) | (0xff800000u & ~keep));  // -inf where the bit is 0
+    }
+  }
+  // The group that the vocabulary ends in, one by one; beyond it nothing is allowed.
+  __device__ __forceinline__ void edge(const PolicyView& p, int64_t b, int v) {
+    ok = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int64_t u = (int64_t)v + i;
+      l[i] = add[i] = 0.0f;
       if (u < p.vocab) {
-        float x = p.bf16 ? f32_of_bf16(((const uint16_t*)p.logits)[b * p.ld + u]) : ((const float*)p.logits)[b * p.ld + u];
-        if constexpr (HIST) {
-          const uint32_t c = count[i];
-          if (c) x = (x > 0.0f ? x / rep : x * rep) - (freq * (float)c + pres);
-        }
-        if (p.bias) x += p.bias[b * p.ld_bias + u];
-        bool ok = true;
-        if (p.mask_kind == AZ_MASK_BYTES) ok = ((const uint8_t*)p.mask)[b * p.ld_mask + u] != 0;
-        else if (p.mask_kind == AZ_MASK_BITS) ok = (((const uint8_t*)p.mask)[4 * b * p.ld_mask + (u >> 3)] >> (u & 7)) & 1;
-        if (ok) l[i] = x;
+        l[i] = p.bf16 ? f32_of_bf16(((const uint16_t*)p.logits)[b * p.ld + u]) : ((const float*)p.logits)[b * p.ld + u];
+        if (p.bias) add[i] = p.bias[b * p.ld_bias + u];
+        bool may = true;
+        if (p.mask_kind == AZ_MASK_BYTES) may = ((const uint8_t*)p.mask)[b * p.ld_mask + u] != 0;
+        else if (p.mask_kind == AZ_MASK_BITS) may = (((const uint8_t*)p.mask)[4 * b * p.ld_mask + (u >> 3)] >> (u & 7)) & 1;
+        if (may) ok |= 0x80u << (8 * i);
       }
     }
   }
-}
-
-__device__ __forceinline__ void store8(const PolicyView& p, int64_t b, int v, const float (&l)[8]) {
-  float* o = p.out + b * p.ld_out + v;
-  if (v + 8 <= p.vocab) {
-    __builtin_memcpy(o, l, 32);
-  } else {
+  __device__ __forceinline__ void store(const PolicyView& p, int64_t b, int v) const {
+    float* o = p.out + b * p.ld_out + v;
+    if (v + 4 <= p.vocab) {
+      __builtin_memcpy(o, &l, 16);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (v + i < p.vocab) o[i] = l[i];
+      for (int i = 0; i < 4; i++)
+        if (v + i < p.vocab) o[i] = l[i];
+    }
+  }
+};
+
+// A thread's groups, `step` entries apart from v on, as they lie in memory (bf16 logits: the first two words).
+__device__ __forceinline__ void load_groups(Entries (&x)[GROUPS], const PolicyView& p, int64_t b, int v, int step) {
+#pragma unroll
+  for (int g = 0; g < GROUPS; g++) {
+    x[g].l = x[g].add = cm_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    x[g].ok = 0;
+  }
+  if (p.vocab < 4) return;
+  int64_t at[GROUPS];
+#pragma unroll
+  for (int g = 0; g < GROUPS; g++) at[g] = min(v + g * step, p.vocab - 4);
+  if (p.bf16) {
+    const uint16_t* row = (const uint16_t*)p.logits + b * p.ld;
+#pragma unroll
+    for (int g = 0; g < GROUPS; g++) __builtin_memcpy(&x[g].l, row + at[g], 8);
+  } else {
+    const float* row = (const float*)p.logits + b * p.ld;
+#pragma unroll
+    for (int g = 0; g < GROUPS; g++) __builtin_memcpy(&x[g].l, row + at[g], 16);
+  }
+  if (p.bias) {
+    const float* row = p.bias + b * p.ld_bias;
+#pragma unroll
+    for (int g = 0; g < GROUPS; g++) __builtin_memcpy(&x[g].add, row + at[g], 16);
+  }
+  if (p.mask_kind == AZ_MASK_BYTES) {
+    const uint8_t* row = (const uint8_t*)p.mask + b * p.ld_mask;
+#pragma unroll
+    for (int g = 0; g < GROUPS; g++) __builtin_memcpy(&x[g].ok, row + at[g], 4);
+  } else if (p.mask_kind == AZ_MASK_BITS) {
+    const uint8_t* row = (const uint8_t*)p.mask + 4 * b * p.ld_mask;
+#pragma unroll
+    for (int g = 0; g < GROUPS; g++) x[g].ok = row[at[g] >> 3];
   }
 }
 
@@ -116,95 +185,106 @@ enum { ADJUST = 0, WHOLE = 1, STATS = 2, WRITE = 3 };
 
 // blockIdx.x: a chunk of 16 entries a thread; blockIdx.y + 65535 blockIdx.z: the row.
 template <int MODE, bool HIST>
-__global__ __launch_bounds__(1024) void az_policy_kernel(PolicyView p, int rows) {
-  extern __shared__ uint32_t count[];  // HIST: one for each entry of the chunk
-  __shared__ float red[2][16];
+__global__ __launch_bounds__(THREADS) void az_policy_kernel(PolicyView p, int rows) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t count[];  // HIST: one for each entry of the chunk
+  __shared__ float red[2][THREADS / 64];
   const int64_t b = (int64_t)blockIdx.z * 65535 + blockIdx.y;
   if (b >= rows) return;
   const int nt = blockDim.x, t = threadIdx.x, v0 = (int)blockIdx.x * nt * PER;
-  float rep = 1.0f, freq = 0.0f, pres = 0.0f;
+  Entries x[GROUPS];
+  load_groups(x, p, b, v0 + t * 4, nt * 4);
+  Penalties pen;
   if constexpr (HIST) {
     const int n = p.lengths ? min(max(p.lengths[b], 0), p.max_history) : p.max_history;
-    rep = p.penalties[3 * b];
-    freq = p.penalties[3 * b + 1];
-    pres = p.penalties[3 * b + 2];
+    const int32_t* past = p.history + b * p.ld_history;
+    pen = Penalties(p.penalties + 3 * b);
+    constexpr int AHEAD = 4;  // past entries of a thread that are on their way while the counters are cleared
+    int32_t e[AHEAD];
 #pragma unroll
-    for (int i = 0; i < PER / 4; i++) reinterpret_cast<cm_i32x4*>(count)[i * nt + t] = cm_i32x4{0, 0, 0, 0};
+    for (int i = 0; i < AHEAD; i++) e[i] = t + i * nt < n ? past[t + i * nt] : -1;
+#pragma unroll
+    for (int i = 0; i < GROUPS; i++) reinterpret_cast<cm_i32x4*>(count)[i * nt + t] = cm_i32x4{0, 0, 0, 0};
     __syncthreads();
-    for (int i = t; i < n; i += nt) {
-      const int v = p.history[b * p.ld_history + i];
-      if (v >= v0 && v < p.vocab && v - v0 < nt * PER) atomicAdd(&count[v - v0], 1u);
-    }
+    const uint32_t here = (uint32_t)min(nt * PER, p.vocab - v0);
+    auto add = [&](int32_t v) {
+      if ((uint32_t)v >= (uint32_t)v0 && (uint32_t)v - (uint32_t)v0 < here) atomicAdd(&count[v - v0], 1u);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) add(e[i]);
+    for (int i = t + AHEAD * nt; i < n; i += nt) add(past[i]);
     __syncthreads();
   }
-  float l[2][8];
 #pragma unroll
-  for (int g = 0; g < 2; g++) load8<HIST>(p, b, v0 + (g * nt + t) * 8, count + (g * nt + t) * 8, rep, freq, pres, l[g]);
+  for (int g = 0; g < GROUPS; g++) x[g].adjust<HIST>(p, b, v0 + (g * nt + t) * 4, count + (g * nt + t) * 4, pen);
 
+  // m: the row's (STATS: the chunk's) maximum, 0 where nothing is above -inf; inv: 1 / sum of exp(l - m), 0
+  // where that is 0 for want of an entry.
   float m = 0.0f, inv = 1.0f;
   if constexpr (MODE == WHOLE || MODE == STATS) {
-    m = -INFINITY;
+    float top = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < 2; g++)
+    for (int g = 0; g < GROUPS; g++)
 #pragma unroll
-      for (int i = 0; i < 8; i++) m = fmaxf(m, l[g][i]);
-    const float base = m == -INFINITY ? 0.0f : m;
+      for (int i = 0; i < 4; i++) top = fmaxf(top, x[g].l[i]);
+    top = wave_top(top);
+    if ((t & 63) == 0) red[0][t >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < nt / 64; w++) top = fmaxf(top, red[0][w]);
+    m = top == -INFINITY ? 0.0f : top;
     float s = 0.0f;
 #pragma unroll
-    for (int g = 0; g < 2; g++)
+    for (int g = 0; g < GROUPS; g++)
 #pragma unroll
-      for (int i = 0; i < 8; i++) s += exp_below(l[g][i], base);
-    for (int o = 32; o > 0; o >>= 1) {
-      const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
-      join(m, s, m2, s2);
-    }
-    if ((t & 63) == 0) {
-      red[0][t >> 6] = m;
-      red[1][t >> 6] = s;
-    }
+      for (int i = 0; i < 4; i++) s += exp_below(x[g].l[i], m);
+    s = wave_total(s);
+    if ((t & 63) == 0) red[1][t >> 6] = s;
     __syncthreads();
-    m = red[0][0];
-    s = red[1][0];
-    for (int w = 1; w < nt / 64; w++) join(m, s, red[0][w], red[1][w]);
+    s = 0.0f;
+    for (int w = 0; w < nt / 64; w++) s += red[1][w];
     if constexpr (MODE == STATS) {
-      if (t == 0) p.stats[b * gridDim.x + blockIdx.x] = make_float2(m, s);
+      if (t == 0) p.stats[b * gridDim.x + blockIdx.x] = make_float2(top, s);
       return;
     }
-    inv = 1.0f / s;
-    if (m == -INFINITY && s == 0.0f) m = inv = 0.0f;
+    inv = top == -INFINITY && s == 0.0f ? 0.0f : 1.0f / s;
   }
   if constexpr (MODE == WRITE) {
     // Every wave joins the row's chunks: lane i those of i, i + 64, ..., then the lanes.
-    float s = 0.0f;
-    m = -INFINITY;
+    const float2* parts = p.stats + b * gridDim.x;
+    float top = -INFINITY, s = 0.0f;
+    for (int i = t & 63; i < (int)gridDim.x; i += 64) top = fmaxf(top, parts[i].x);
+    top = wave_top(top);
+    m = top == -INFINITY ? 0.0f : top;
+    // (a chunk without an entry above -inf has a sum of 0, or NaN where it holds one)
     for (int i = t & 63; i < (int)gridDim.x; i += 64) {
-      const float2 x = p.stats[b * gridDim.x + i];
-      join(m, s, x.x, x.y);
+      const float2 part = parts[i];
+      s += part.x == -INFINITY ? part.y : part.y * exp_below(part.x, m);
     }
-    for (int o = 32; o > 0; o >>= 1) {
-      const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
-      join(m, s, m2, s2);
-    }
-    inv = 1.0f / s;
-    if (m == -INFINITY && s == 0.0f) m = inv = 0.0f;
+    s = wave_total(s);
+    inv = top == -INFINITY && s == 0.0f ? 0.0f : 1.0f / s;
   }
 #pragma unroll
-  for (int g = 0; g < 2; g++) {
+  for (int g = 0; g < GROUPS; g++) {
     if constexpr (MODE != ADJUST) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) l[g][i] = l[g][i] == -INFINITY ? 0.0f : exp_below(l[g][i], m) * inv;
+      for (int i = 0; i < 4; i++) {
+        // (a NaN row's inv must not reach what is not allowed)
+        const float e = exp_below(x[g].l[i], m) * inv;
+        x[g].l[i] = x[g].l[i] == -INFINITY ? 0.0f : e;
+      }
     }
-    store8(p, b, v0 + (g * nt + t) * 8, l[g]);
+    x[g].store(p, b, v0 + (g * nt + t) * 4);
   }
 }
 
 // Threads of a workgroup: enough for the row, up to 1,024.  Rows that need several
-// workgroups get smaller ones where there are few of them, so that the chip is used.
+// workgroups get 512 (512 rows of 131,072: 174 us, 185 with 1,024), or 256 where that takes to fill the chip.
 int policy_threads(int64_t rows, int64_t vocab) {
-  if (vocab <= MOST) return vocab <= 256 * PER ? 256 : vocab <= 512 * PER ? 512 : 1024;
-  for (int nt = 1024; nt > 256; nt /= 2)
-    if (rows * ((vocab + nt * PER - 1) / (nt * PER)) >= 512) return nt;
-  return 256;
+  int nt = 256;
+  if (vocab <= MOST) {
+    while (nt * PER < vocab) nt *= 2;
+    return nt;
+  }
+  return rows * ((vocab + 512 * PER - 1) / (512 * PER)) >= 512 ? 512 : 256;
 }
 
 template <int MODE>
