@@ -446,9 +446,14 @@ int az_codes_dequantize(const az_code_matrix* q, void* x, int32_t dtype, int64_t
  * norm, a hundredth of a bf16 rounding) and accumulates in fp32.  AZ_F32 multiplies on
  * the bf16 instruction: every product is exact, sums are fp32.  Sums have a fixed
  * order: equal calls give equal bits.
+ *   workspace  device, 16-byte aligned, at least az_codes_matmul_workspace bytes
+ *              (which may be 0; then it may be NULL).  It holds sums over parts of
+ *              the columns where there are few outputs, is written before it is
+ *              read, and must not be shared by two calls that may run at once.
  * M = 0 or N = 0 (rows): AZ_OK, nothing is launched.  Errors as above. */
+size_t az_codes_matmul_workspace(const az_code_matrix* a, const az_code_matrix* b, int32_t dtype);
 int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b, const float* bias, void* out,
-                    int32_t dtype, int64_t ld_out, void* stream);
+                    int32_t dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The weight's and bias's gradients of y = x W^T + bias, x as it was saved in 8
  * bits (scale_rows 1):

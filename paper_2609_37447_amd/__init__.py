@@ -16,6 +16,6 @@ from ._binding import (AZ_ABI_VERSION, AZ_BF16, AZ_ERR_DEVICE, AZ_ERR_INVALID_AR
                        az_pipeline_free, az_pipeline_query, az_pipeline_slot, az_pipeline_submit,
                        az_pipeline_wait, az_pipeline_drive, az_debug_fail_allocation, az_debug_live_allocations,
                        AZ_CODE_BLOCK, AZ_MASK_NONE, AZ_MASK_BYTES, AZ_MASK_BITS, az_code_matrix, az_logits,
-                       az_codes_quantize, az_codes_dequantize, az_codes_matmul, az_codes_weight_grad,
+                       az_codes_quantize, az_codes_dequantize, az_codes_matmul, az_codes_matmul_workspace, az_codes_weight_grad,
                        az_codes_weight_grad_workspace, az_logits_policy, az_logits_policy_workspace, CodeMatrix,
                        quantize_tensors, dequantize_tensors, matmul_tensors, weight_grad_tensors, policy_tensors)

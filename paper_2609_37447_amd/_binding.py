@@ -29,8 +29,8 @@ EXPORTS = ("az_weight_count", "az_net_load", "az_eval_batch", "az_eval_batch_wdl
            "az_pipeline_create", "az_pipeline_slot", "az_pipeline_submit", "az_pipeline_query",
            "az_pipeline_wait", "az_pipeline_drive", "az_pipeline_free", "az_debug_fail_allocation",
            "az_debug_live_allocations", "az_eval_batch_compact_noalloc",
-           "az_codes_quantize", "az_codes_dequantize", "az_codes_matmul", "az_codes_weight_grad",
-           "az_codes_weight_grad_workspace", "az_logits_policy", "az_logits_policy_workspace",
+           "az_codes_quantize", "az_codes_dequantize", "az_codes_matmul", "az_codes_matmul_workspace",
+           "az_codes_weight_grad",           "az_codes_weight_grad_workspace", "az_logits_policy", "az_logits_policy_workspace",
            "az_status_string", "az_last_error")
 
 
@@ -123,7 +123,8 @@ def lib():
         M, I64 = ctypes.POINTER(az_code_matrix), ctypes.c_int64
         L.az_codes_quantize.argtypes = [P, I32, I64, M, M, P]
         L.az_codes_dequantize.argtypes = [M, P, I32, I64, P]
-        L.az_codes_matmul.argtypes = [M, M, P, P, I32, I64, P]
+        L.az_codes_matmul.argtypes = [M, M, P, P, I32, I64, P, SZ, P]
+        L.az_codes_matmul_workspace.argtypes, L.az_codes_matmul_workspace.restype = [M, M, I32], SZ
         L.az_codes_weight_grad.argtypes = [P, I64, I32, M, P, I32, I64, P, I32, P, SZ, P]
         L.az_logits_policy.argtypes = [ctypes.POINTER(az_logits), I32, P, I64, P, SZ, P]
         for f in (L.az_codes_quantize, L.az_codes_dequantize, L.az_codes_matmul, L.az_codes_weight_grad,
@@ -330,9 +331,13 @@ def az_codes_dequantize(q: az_code_matrix, x, dtype: int, ldx: int, stream: int 
     return _check(st, "az_codes_dequantize") if raise_on_error else st
 
 
-def az_codes_matmul(a: az_code_matrix, b: az_code_matrix, bias, out, dtype: int, ld_out: int, stream: int = 0,
-                    raise_on_error: bool = True) -> int:
-    st = lib().az_codes_matmul(a, b, bias, out, dtype, ld_out, stream)
+def az_codes_matmul_workspace(a: az_code_matrix, b: az_code_matrix, dtype: int) -> int:
+    return int(lib().az_codes_matmul_workspace(a, b, dtype))
+
+
+def az_codes_matmul(a: az_code_matrix, b: az_code_matrix, bias, out, dtype: int, ld_out: int, workspace=None,
+                    workspace_bytes: int = 0, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_codes_matmul(a, b, bias, out, dtype, ld_out, workspace, workspace_bytes, stream)
     return _check(st, "az_codes_matmul") if raise_on_error else st
 
 
@@ -477,8 +482,10 @@ def dequantize_tensors(q: CodeMatrix, x, stream=None) -> int:
         return az_codes_dequantize(q.c, x.data_ptr(), _float_type(x), ld, s)
 
 
-def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, stream=None) -> int:
-    """az_codes_matmul: out [a.rows][b.rows] (bfloat16 or float32) = a b^T + bias (float32 [b.rows])."""
+def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, workspace=None, stream=None) -> int:
+    """az_codes_matmul: out [a.rows][b.rows] (bfloat16 or float32) = a b^T + bias (float32 [b.rows]).
+    A workspace is made for the call (torch's allocator, on the call's stream) unless a tensor is
+    given."""
     import torch
     m, n, ld = _rows_of("out", out, (torch.float32, torch.bfloat16))
     if (m, n) != (a.rows, b.rows):
@@ -486,7 +493,9 @@ def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, stream=None) ->
     if bias is not None:
         _vector_of("bias", bias, torch.float32, n)
     with _On(stream, out.device, a, b, bias) as s:
-        return az_codes_matmul(a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), _float_type(out), ld, s)
+        dt = _float_type(out)
+        ws, size, keep = _workspace(workspace, az_codes_matmul_workspace(a.c, b.c, dt), out.device, stream)
+        return az_codes_matmul(a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), dt, ld, ws, size, s)
 
 
 def weight_grad_tensors(dy, x: CodeMatrix, dw, db=None, accumulate: bool = False, workspace=None, stream=None) -> int:

@@ -28,93 +28,117 @@ __device__ __forceinline__ cm_bf16x8 fragment_bf16(const cm_i32x8& w, int i, flo
   return __builtin_bit_cast(cm_bf16x8, u);
 }
 
-// A workgroup of NW waves owns 16 FM rows of a times 16 FN rows of b.  Each wave takes
-// every NW-th K step straight from memory to registers; the partial sums meet in LDS in
-// the order of the waves.
-template <int FM, int FN, int NW, bool F32>
+// Few rows of a.  A workgroup of NW waves owns 16 FM rows of a times 16 rows of b.  Each wave takes
+// every NW-th K step of the workgroup's part of them straight from memory to registers, U steps'
+// loads on their way together; the waves' sums meet in LDS in the order of the waves.  Bound by
+// b's bytes, and by their latency where a wave has few steps.
+template <int FM, int NW, int U, bool EXACT>
+struct Direct {
+  struct Step {
+    cm_i32x8 a[FM], b;
+    uint32_t sa[FM], sb;
+  };
+  // (Which columns a lane's 32 codes are does not matter as long as a and b agree: four lanes take
+  // 64 bytes side by side, twice.)
+  static __device__ __forceinline__ cm_i32x8 whole_fragment(const uint8_t* row, int k0) {
+    const cm_i32x4 lo = *reinterpret_cast<const cm_i32x4*>(row + k0), hi = *reinterpret_cast<const cm_i32x4*>(row + k0 + 64);
+    return cm_i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  }
+  static __device__ __forceinline__ void multiply(cm_f32x4 (&acc)[FM], const Step& s) {
+    if constexpr (!EXACT) {
+#pragma unroll
+      for (int i = 0; i < FM; i++)
+        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(s.b, s.a[i], acc[i], 0, 0, 0, (int)s.sb, 0, (int)s.sa[i]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const cm_bf16x8 vb = fragment_bf16(s.b, q, scale_value(s.sb));
+#pragma unroll
+        for (int i = 0; i < FM; i++)
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, fragment_bf16(s.a[i], q, scale_value(s.sa[i])), acc[i], 0, 0, 0);
+      }
+    }
+  }
+};
+
+template <int FM, int NW, int U, bool EXACT, bool F32>
 __global__ __launch_bounds__(NW * 64) void az_matmul_direct(CodeView a, CodeView b, const float* __restrict__ bias,
-                                                            void* __restrict__ out, int64_t ldo) {
-  __shared__ cm_f32x4 part[NW > 1 ? (NW - 1) * FM * FN * 64 : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+                                                            void* __restrict__ out, int64_t ldo, int part_steps, int64_t part_stride) {
+  using D = Direct<FM, NW, U, EXACT>;
+  __shared__ cm_f32x4 part[(NW - 1) * FM * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int m0 = blockIdx.y * 16 * FM, n0 = blockIdx.x * 16 * FN;
-  cm_f32x4 acc[FM][FN];
-  const uint8_t *ar[FM], *br[FN], *as[FM], *bs[FN];
+  const int m0 = blockIdx.y * 16 * FM, n0 = blockIdx.x * 16;
+  const int first = (int)blockIdx.z * part_steps, last = min(first + part_steps, a.nb), whole = min(last, a.cols / CB);
+  const uint8_t *ar[FM], *as[FM];
 #pragma unroll
   for (int i = 0; i < FM; i++) {
     const int row = min(m0 + 16 * i + r, a.rows - 1);
     ar[i] = a.codes + row * a.ld;
     as[i] = a.scales + (int64_t)(row >> a.shift) * a.nb;
   }
+  const int brow = min(n0 + r, b.rows - 1);
+  const uint8_t* br = b.codes + brow * b.ld;
+  const uint8_t* bs = b.scales + (int64_t)(brow >> b.shift) * b.nb;
+  cm_f32x4 acc[FM];
 #pragma unroll
-  for (int j = 0; j < FN; j++) {
-    const int row = min(n0 + 16 * j + r, b.rows - 1);
-    br[j] = b.codes + row * b.ld;
-    bs[j] = b.scales + (int64_t)(row >> b.shift) * b.nb;
-  }
+  for (int i = 0; i < FM; i++) acc[i] = cm_f32x4{0, 0, 0, 0};
+  for (int kb = first + wave; kb < whole; kb += NW * U) {
+    typename D::Step s[U];
 #pragma unroll
-  for (int i = 0; i < FM; i++)
+    for (int u = 0; u < U; u++) {
+      const int k = min(kb + u * NW, whole - 1);
+      s[u].b = D::whole_fragment(br, k * CB + g * 16);
+      s[u].sb = bs[k];
 #pragma unroll
-    for (int j = 0; j < FN; j++) acc[i][j] = cm_f32x4{0, 0, 0, 0};
-  for (int kb = wave; kb < a.nb; kb += NW) {
-    const int k0 = kb * CB + g * 32;
-    cm_i32x8 fa[FM], fb[FN];
-    uint32_t sa[FM], sb[FN];
-#pragma unroll
-    for (int i = 0; i < FM; i++) { fa[i] = row_fragment(ar[i], k0, a.cols); sa[i] = as[i][kb]; }
-#pragma unroll
-    for (int j = 0; j < FN; j++) { fb[j] = row_fragment(br[j], k0, a.cols); sb[j] = bs[j][kb]; }
-    if constexpr (!F32) {
-#pragma unroll
-      for (int i = 0; i < FM; i++)
-#pragma unroll
-        for (int j = 0; j < FN; j++)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, (int)sb[j], 0, (int)sa[i]);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        cm_bf16x8 va[FM], vb[FN];
-#pragma unroll
-        for (int i = 0; i < FM; i++) va[i] = fragment_bf16(fa[i], q, scale_value(sa[i]));
-#pragma unroll
-        for (int j = 0; j < FN; j++) vb[j] = fragment_bf16(fb[j], q, scale_value(sb[j]));
-#pragma unroll
-        for (int i = 0; i < FM; i++)
-#pragma unroll
-          for (int j = 0; j < FN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb[j], va[i], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < FM; i++) {
+        s[u].a[i] = D::whole_fragment(ar[i], k * CB + g * 16);
+        s[u].sa[i] = as[i][k];
       }
     }
-  }
-  if constexpr (NW > 1) {
-    if (wave > 0) {
+    __builtin_amdgcn_sched_barrier(0);  // all of them before the first is waited for
 #pragma unroll
-      for (int i = 0; i < FM; i++)
-#pragma unroll
-        for (int j = 0; j < FN; j++) part[((wave - 1) * FM * FN + i * FN + j) * 64 + lane] = acc[i][j];
+    for (int u = 0; u < U; u++) {
+      // (past the end the last step was read again: its codes count as zeros, which adds nothing but
+      // a NaN that is in the result already)
+      if (u > 0) s[u].b &= -(int)(kb + u * NW < whole);
+      D::multiply(acc, s[u]);
     }
-    __syncthreads();
-    if (wave > 0) return;
-#pragma unroll
-    for (int w = 0; w < NW - 1; w++)
-#pragma unroll
-      for (int i = 0; i < FM; i++)
-#pragma unroll
-        for (int j = 0; j < FN; j++) acc[i][j] += part[(w * FM * FN + i * FN + j) * 64 + lane];
   }
+  if (whole < last && wave == (whole - first) % NW) {  // the columns that do not fill a step
+    typename D::Step s;
+    const int k0 = whole * CB + g * 32;
+    s.b = row_fragment(br, k0, a.cols);
+    s.sb = bs[whole];
+#pragma unroll
+    for (int i = 0; i < FM; i++) {
+      s.a[i] = row_fragment(ar[i], k0, a.cols);
+      s.sa[i] = as[i][whole];
+    }
+    D::multiply(acc, s);
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < FM; i++) part[((wave - 1) * FM + i) * 64 + lane] = acc[i];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < NW - 1; w++)
+#pragma unroll
+    for (int i = 0; i < FM; i++) acc[i] += part[(w * FM + i) * 64 + lane];
+  const int64_t at = (int64_t)blockIdx.z * part_stride;
 #pragma unroll
   for (int i = 0; i < FM; i++) {
     const int m = m0 + 16 * i + r;
     if (m >= a.rows) continue;
 #pragma unroll
-    for (int j = 0; j < FN; j++) {
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const int n = n0 + 16 * j + 4 * g + e;
-        if (n >= b.rows) continue;
-        const float v = acc[i][j][e] + (bias ? bias[n] : 0.0f);
-        if constexpr (F32) ((float*)out)[m * ldo + n] = v;
-        else ((uint16_t*)out)[m * ldo + n] = bf16_of(v);
-      }
+    for (int e = 0; e < 4; e++) {
+      const int n = n0 + 4 * g + e;
+      if (n >= b.rows) continue;
+      const float v = acc[i][e] + (bias ? bias[n] : 0.0f);
+      if constexpr (F32) ((float*)out)[at + m * ldo + n] = v;
+      else ((uint16_t*)out)[at + m * ldo + n] = bf16_of(v);
     }
   }
 }
@@ -134,23 +158,24 @@ __device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, in
 
 typedef __attribute__((address_space(3))) uint8_t lds_bytes;
 
-// Large products.  Four waves own a square tile of 64 W rows of each operand, a wave a
-// quarter of it (W x W blocks of 32 x 32).  K steps of 128 columns go straight from memory
-// into LDS, two steps in turn; a wave reads fragments of half a step (64 columns) while
-// the matrix unit works on the half before.
+// More rows of a.  Four waves own a tile of TM rows of a and TN rows of b, WM x WN parts of FA x FB
+// blocks of 32 x 32.  K steps of 128 columns go straight from memory into LDS, two steps in
+// turn (four were no faster); a wave reads fragments of half a step (64 columns) while the
+// matrix unit works on the half before.
 //
 // LDS rows are 128 bytes, their 16-byte chunks exchanged by the row's place (chunk ^ (row /
 // 2) % 8), which spreads the 16 rows that are read together over all banks.  The copy into
 // LDS puts lanes side by side, so that the exchange is made on the source address.
-template <int W, int NW, bool F32>
+template <int FA_, int FB_, int WM, int WN, bool EXACT>
 struct Tiled {
-  static constexpr int T = 64 * W;           // rows of a and of b of a tile
-  static constexpr int STEP = T * CB;        // LDS bytes of one operand's step
-  static constexpr int SCALES = 2 * STEP;    // where a word of scale bytes for each row of a, then of b, begins
-  static constexpr int STAGE = 2 * STEP + 2 * T * 4;
-  static constexpr int ROWS = 8 * NW;        // rows that one copy instruction of the workgroup fills
-  static constexpr int CHUNKS = T / ROWS;
-  static constexpr int FA = W, FB = 4 * W / NW;  // 32-row blocks of a wave
+  static constexpr int FA = FA_, FB = FB_, TM = 32 * FA * WM, TN = 32 * FB * WN;
+  static constexpr int ASTEP = TM * CB, BSTEP = TN * CB;  // LDS bytes of an operand's step
+  static constexpr int SCALES = ASTEP + BSTEP;  // where a word of scale bytes for each row of a, then of b, begins
+  static constexpr int SA = TM < 64 ? 64 : TM;  // words of a (a wave copies 64)
+  static constexpr int STAGE = SCALES + (SA + TN) * 4;
+  static constexpr int LDS = 2 * STAGE;
+  static constexpr int ROWS = 32;               // rows that one copy instruction of the workgroup fills
+  static_assert(WM * WN == 4 && (SA + TN) % 64 == 0 && TM % ROWS == 0 && TN % ROWS == 0, "four waves' work");
 
   struct Frag {
     cm_i32x8 a[FA], b[FB];
@@ -158,15 +183,19 @@ struct Tiled {
 
   // A thread's chunks of a step, one of each ROWS rows: `off` within the step's first rows, `at`
   // the step's place in the tile.
+  template <int CHUNKS>
   static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, int ld, uint32_t off, int at, lds_bytes* to) {
 #pragma unroll
     for (int j = 0; j < CHUNKS; j++)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * ROWS * CB, 16, off, at + j * ROWS * ld, 0, 0);
   }
+  static __device__ __forceinline__ void scale_words(__amdgpu_buffer_rsrc_t words, lds_bytes* to, uint32_t at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(words, to, 4, at, 0, 0, 0);
+  }
   // Spreads half a step's LDS reads (of the next half's fragments) and loads over its matrix
   // instructions, reads first, so that they are back before the half ends.
   static __device__ __forceinline__ void interleave() {
-    if constexpr (!F32) {
+    if constexpr (!EXACT) {
 #pragma unroll
       for (int i = 0; i < FA * FB; i++) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
@@ -186,7 +215,7 @@ struct Tiled {
     for (int j = 0; j < FB; j++) f.b[j] = fragment(b0 + j * 32 * CB, b1 + j * 32 * CB);
   }
   static __device__ __forceinline__ void multiply(cm_f32x16 (&acc)[FA][FB], const Frag& f, const uint32_t (&sa)[FA], const uint32_t (&sb)[FB]) {
-    if constexpr (!F32) {
+    if constexpr (!EXACT) {
 #pragma unroll
       for (int i = 0; i < FA; i++)
 #pragma unroll
@@ -222,61 +251,70 @@ struct ScaleWords {
   __device__ __forceinline__ uint32_t place(const CodeView& m, int row) const { return skip + (uint32_t)(row >> m.shift) * (uint32_t)m.nb; }
 };
 
-template <int W, int NW, bool F32>
-__global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_tiled(CodeView a, CodeView b, const float* __restrict__ bias,
-                                                                       void* __restrict__ out, int64_t ldo, int mt, int nt) {
-  using K = Tiled<W, NW, F32>;
+template <int FA, int FB, int WM, int WN, bool EXACT, bool F32>
+__global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(CodeView a, CodeView b, const float* __restrict__ bias,
+                                                                              void* __restrict__ out, int64_t ldo, int mt, int nt,
+                                                                              int part_steps, int64_t part_stride) {
+  using K = Tiled<FA, FB, WM, WN, EXACT>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   int tm, tn;
   tile_of(blockIdx.x, mt, nt, tm, tn);
-  // The last tile of a side ends with the matrix (which has at least a tile's rows): what it
-  // shares with the tile before is computed twice, to the same bits.
-  const int m0 = min(tm * K::T, a.rows - K::T), n0 = min(tn * K::T, b.rows - K::T);
+  // The last tile of a side ends with the matrix: what it shares with the tile before is computed
+  // twice, to the same bits.  A matrix of fewer rows than a tile is the one tile's beginning.
+  const int m0 = max(min(tm * K::TM, a.rows - K::TM), 0), n0 = max(min(tn * K::TN, b.rows - K::TN), 0);
+  const int ms = min(a.rows, K::TM), ns = min(b.rows, K::TN);
 
-  // Copying: wave w of instruction j takes rows 32 j + 8 w .. + 7, a lane one chunk of one row.
+  // Copying: wave w of instruction j takes rows 32 j + 8 w .. + 7, a lane one chunk of one row.  Rows
+  // past the matrix are out of the buffer's range and read as zeros.
   const int crow = 8 * wave + (lane >> 3), chunk = (lane & 7) ^ ((crow >> 1) & 7);
   const uint32_t aoff = (uint32_t)crow * (uint32_t)a.ld + chunk * 16, boff = (uint32_t)crow * (uint32_t)b.ld + chunk * 16;
-  const __amdgpu_buffer_rsrc_t abuf = __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, K::T * (int)a.ld, 0x00027000);
-  const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, K::T * (int)b.ld, 0x00027000);
+  const int width = (a.cols + 15) & ~15;
+  const __amdgpu_buffer_rsrc_t abuf = __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, (ms - 1) * (int)a.ld + width, 0x00027000);
+  const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, (ns - 1) * (int)b.ld + width, 0x00027000);
   lds_bytes* const lds0 = (lds_bytes*)smem + 8 * wave * CB;
-  const int whole = a.cols / CB;  // steps that fill their columns
-  // Scales: a thread's row of a and of b, or of a for half of the threads and of b for the others.
+  // The part's steps, of which `whole` is the first that does not fill its columns or is not the part's.
+  const int first = (int)blockIdx.y * part_steps, last = min(first + part_steps, a.nb), whole = min(last, a.cols / CB);
+  // Scales: words of a, then of b, 64 a wave and turn.
   const ScaleWords aw(a), bw(b);
-  constexpr bool BOTH = 64 * NW == K::T;
-  const bool half = !BOTH && wave >= NW / 2;
-  const uint32_t srow = half ? bw.place(b, n0 + (t & (K::T - 1))) : aw.place(a, m0 + (t & (K::T - 1)));
-  const uint32_t srow2 = BOTH ? bw.place(b, n0 + t) : 0u;
+  constexpr int TURNS = ((K::SA + K::TN) / 64 + 3) / 4;
+  uint32_t srow[TURNS];
+#pragma unroll
+  for (int i = 0; i < TURNS; i++) {
+    const int w = i * 256 + t;
+    srow[i] = w < K::SA ? aw.place(a, m0 + min(w, ms - 1)) : bw.place(b, n0 + min(w - K::SA, ns - 1));
+  }
   lds_bytes* const slds = (lds_bytes*)smem + K::SCALES + wave * 64 * 4;
   // (past the last step: that step again, which nothing reads)
   auto fetch = [&](int kb) {
     const int stage = (kb & 1) * K::STAGE;
     kb = min(kb, whole - 1);
-    K::copy(abuf, (int)a.ld, aoff, kb * CB, lds0 + stage);
-    K::copy(bbuf, (int)b.ld, boff, kb * CB, lds0 + stage + K::STEP);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(half ? bw.words : aw.words, slds + stage, 4, (srow + kb) & ~3u, 0, 0, 0);
-    if constexpr (BOTH)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(bw.words, slds + stage + K::T * 4, 4, (srow2 + kb) & ~3u, 0, 0, 0);
+    K::template copy<K::TM / 32>(abuf, (int)a.ld, aoff, kb * CB, lds0 + stage);
+    K::template copy<K::TN / 32>(bbuf, (int)b.ld, boff, kb * CB, lds0 + stage + K::ASTEP);
+#pragma unroll
+    for (int i = 0; i < TURNS; i++)
+      if ((K::SA + K::TN) % 256 == 0 || i * 4 + wave < (K::SA + K::TN) / 64)
+        K::scale_words(i * 4 + wave < K::SA / 64 ? aw.words : bw.words, slds + stage + i * 1024, (srow[i] + kb) & ~3u);
   };
 
   // Reading: a lane holds row l % 32 of a block, columns 32 (l / 32) + 64 s on of half s.
-  const int r = lane & 31, h = lane >> 5, wm = (wave & 1) * 32 * K::FA, wn = (wave >> 1) * 32 * K::FB;
+  const int r = lane & 31, h = lane >> 5, wm = (wave % WM) * 32 * K::FA, wn = (wave / WM) * 32 * K::FB;
   const int sw = (r >> 1) & 7;
   const uint8_t* ap = smem + (wm + r) * CB;
-  const uint8_t* bp = smem + K::STEP + (wn + r) * CB;
+  const uint8_t* bp = smem + K::ASTEP + (wn + r) * CB;
   const int at[2][2] = {{((2 * h) ^ sw) * 16, ((2 * h + 1) ^ sw) * 16}, {((2 * h + 4) ^ sw) * 16, ((2 * h + 5) ^ sw) * 16}};
   uint32_t ac[K::FA], bc[K::FB];  // places of the lane's rows' scales
 #pragma unroll
-  for (int i = 0; i < K::FA; i++) ac[i] = aw.place(a, m0 + wm + 32 * i + r);
+  for (int i = 0; i < K::FA; i++) ac[i] = aw.place(a, m0 + min(wm + 32 * i + r, ms - 1));
 #pragma unroll
-  for (int j = 0; j < K::FB; j++) bc[j] = bw.place(b, n0 + wn + 32 * j + r);
+  for (int j = 0; j < K::FB; j++) bc[j] = bw.place(b, n0 + min(wn + 32 * j + r, ns - 1));
   uint32_t sa[K::FA], sb[K::FB], na[K::FA], nb[K::FB];
   auto scales = [&](uint32_t (&pa)[K::FA], uint32_t (&pb)[K::FB], int kb) {
     const uint8_t* from = smem + (kb & 1) * K::STAGE + K::SCALES + r * 4;
 #pragma unroll
     for (int i = 0; i < K::FA; i++) pa[i] = from[(wm + 32 * i) * 4 + ((ac[i] + kb) & 3u)];
 #pragma unroll
-    for (int j = 0; j < K::FB; j++) pb[j] = from[(K::T + wn + 32 * j) * 4 + ((bc[j] + kb) & 3u)];
+    for (int j = 0; j < K::FB; j++) pb[j] = from[(K::SA + wn + 32 * j) * 4 + ((bc[j] + kb) & 3u)];
   };
 
   cm_f32x16 acc[K::FA][K::FB];
@@ -285,15 +323,16 @@ __global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_
 #pragma unroll
     for (int j = 0; j < K::FB; j++) acc[i][j] = cm_f32x16{};
   typename K::Frag f0, f1;
-  if (whole > 0) {
-    fetch(0);
+  if (whole > first) {
+    const int stage = (first & 1) * K::STAGE;
+    fetch(first);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    fetch(1);
-    scales(sa, sb, 0);
-    K::read(f0, ap + at[0][0], ap + at[0][1], bp + at[0][0], bp + at[0][1]);
+    fetch(first + 1);
+    scales(sa, sb, first);
+    K::read(f0, ap + stage + at[0][0], ap + stage + at[0][1], bp + stage + at[0][0], bp + stage + at[0][1]);
   }
-  for (int kb = 0; kb < whole; kb++) {
+  for (int kb = first; kb < whole; kb++) {
     const int stage = (kb & 1) * K::STAGE, next = K::STAGE - stage;
     K::read(f1, ap + stage + at[1][0], ap + stage + at[1][1], bp + stage + at[1][0], bp + stage + at[1][1]);
     K::multiply(acc, f0, sa, sb);
@@ -315,7 +354,7 @@ __global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_
     for (int j = 0; j < K::FB; j++) sb[j] = nb[j];
   }
   __builtin_amdgcn_s_waitcnt(0);  // no copy into LDS is under way when the workgroup ends
-  if (whole < a.nb) {  // the columns that do not fill a step, straight from memory
+  if (whole < last) {  // the columns that do not fill a step, straight from memory
 #pragma unroll
     for (int i = 0; i < K::FA; i++) sa[i] = a.scales[ac[i] - aw.skip + whole];
 #pragma unroll
@@ -323,17 +362,17 @@ __global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_
 #pragma unroll
     for (int s = 0; s < 2; s++) {
 #pragma unroll
-      for (int i = 0; i < K::FA; i++) f0.a[i] = row_fragment(a.codes + (m0 + wm + 32 * i + r) * a.ld, whole * CB + 64 * s + 32 * h, a.cols);
+      for (int i = 0; i < K::FA; i++) f0.a[i] = row_fragment(a.codes + (m0 + min(wm + 32 * i + r, ms - 1)) * a.ld, whole * CB + 64 * s + 32 * h, a.cols);
 #pragma unroll
-      for (int j = 0; j < K::FB; j++) f0.b[j] = row_fragment(b.codes + (n0 + wn + 32 * j + r) * b.ld, whole * CB + 64 * s + 32 * h, a.cols);
+      for (int j = 0; j < K::FB; j++) f0.b[j] = row_fragment(b.codes + (n0 + min(wn + 32 * j + r, ns - 1)) * b.ld, whole * CB + 64 * s + 32 * h, a.cols);
       K::multiply(acc, f0, sa, sb);
     }
   }
   // Results leave through LDS, so that whole rows of the tile are written: a lane's four neighbours
   // would be 16 bytes of each of 32 rows.  Chunks are exchanged by the row, as above.
-  constexpr int ES = F32 ? 4 : 2, OROW = K::T * ES;
-  constexpr int PASSES = 2 * K::STAGE >= K::T * OROW ? 1 : 2;  // fp32: half of each wave's rows at a time
-  constexpr int PF = K::FA / PASSES, PROWS = K::T / PASSES;
+  constexpr int ES = F32 ? 4 : 2, OROW = K::TN * ES, RC = OROW / 16;  // bytes and chunks of a row
+  constexpr int PASSES = K::LDS >= K::TM * OROW ? 1 : 2;  // fp32 of the largest tile: half of each wave's rows at a time
+  constexpr int PF = K::FA / PASSES, PROWS = K::TM / PASSES;
 #pragma unroll
   for (int p = 0; p < PASSES; p++) {
     __syncthreads();
@@ -342,11 +381,14 @@ __global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_
 #pragma unroll
       for (int q = 0; q < 4; q++) {
         const int n = wn + 32 * j + 8 * q + 4 * h;
-        cm_f32x4 add = {0, 0, 0, 0};
-        if (bias) __builtin_memcpy(&add, bias + n0 + n, 16);
+        float add[4] = {};
+        if (bias) {
+#pragma unroll
+          for (int e = 0; e < 4; e++) add[e] = bias[n0 + min(n + e, ns - 1)];
+        }
 #pragma unroll
         for (int i = 0; i < PF; i++) {
-          const int row = (wave & 1) * 32 * PF + 32 * i + r;
+          const int row = (wave % WM) * 32 * PF + 32 * i + r;
           cm_f32x4 v;
 #pragma unroll
           for (int e = 0; e < 4; e++) v[e] = acc[PF * p + i][j][4 * q + e] + add[e];
@@ -355,53 +397,146 @@ __global__ __launch_bounds__(64 * NW, W == 4 && NW == 4 ? 1 : 2) void az_matmul_
           } else {
             const cm_i32x2 w = {(int)((uint32_t)bf16_of(v[0]) | ((uint32_t)bf16_of(v[1]) << 16)),
                                 (int)((uint32_t)bf16_of(v[2]) | ((uint32_t)bf16_of(v[3]) << 16))};
-            *reinterpret_cast<cm_i32x2*>(smem + row * OROW + (((n >> 3) ^ (r & (OROW / 16 - 1))) * 16) + (n & 4) * 2) = w;
+            *reinterpret_cast<cm_i32x2*>(smem + row * OROW + (((n >> 3) ^ (r & (RC - 1))) * 16) + (n & 4) * 2) = w;
           }
         }
       }
     __syncthreads();
-    constexpr int RC = OROW / 16;  // chunks of a row
+    uint8_t* const to = (uint8_t*)out + (blockIdx.y * part_stride + (int64_t)m0 * ldo + n0) * ES;
 #pragma unroll 8
-    for (int c = t; c < PROWS * RC; c += 64 * NW) {
+    for (int c = t; c < PROWS * RC; c += 256) {
       const int row = c / RC, in = c % RC;
       const cm_i32x4 v = *reinterpret_cast<const cm_i32x4*>(smem + row * OROW + ((in ^ (row & 31 & (RC - 1))) * 16));
-      // rows of the two halves of the waves lie FA blocks apart
-      const int m = m0 + row / (32 * PF) * (32 * K::FA) + p * 32 * PF + row % (32 * PF);
-      __builtin_memcpy((uint8_t*)out + ((int64_t)m * ldo + n0) * ES + in * 16, &v, 16);
+      // rows of the waves lie FA blocks apart
+      const int m = row / (32 * PF) * (32 * K::FA) + p * 32 * PF + row % (32 * PF);
+      const int left = ns * ES - in * 16;  // bytes of the row from here on
+      uint8_t* o = to + (int64_t)m * ldo * ES + in * 16;
+      if (m < ms && left >= 16) {
+        __builtin_memcpy(o, &v, 16);
+      } else if (m < ms && left > 0) {
+#pragma unroll
+        for (int e = 0; e < 16 / ES; e++)
+          if (e * ES < left) {
+            if constexpr (F32) reinterpret_cast<int*>(o)[e] = v[e];
+            else reinterpret_cast<uint16_t*>(o)[e] = (uint16_t)((uint32_t)v[e >> 1] >> (16 * (e & 1)));
+          }
+      }
     }
   }
 }
 
-template <int FM, int FN, int NW, bool F32>
-void launch_direct(const CodeView& a, const CodeView& b, const float* bias, void* out, int64_t ldo, hipStream_t s) {
-  const dim3 g((b.rows + 16 * FN - 1) / (16 * FN), (a.rows + 16 * FM - 1) / (16 * FM));
-  hipLaunchKernelGGL((az_matmul_direct<FM, FN, NW, F32>), g, dim3(NW * 64), 0, s, a, b, bias, out, ldo);
-}
-
-template <int W, int NW, bool F32>
-void launch_tiled(const CodeView& a, const CodeView& b, const float* bias, void* out, int64_t ldo, hipStream_t s) {
-  using K = Tiled<W, NW, F32>;
-  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<W, NW, F32>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, 2 * K::STAGE);
-  (void)once;
-  const int mt = (a.rows + K::T - 1) / K::T, nt = (b.rows + K::T - 1) / K::T;
-  hipLaunchKernelGGL((az_matmul_tiled<W, NW, F32>), dim3((unsigned)mt * (unsigned)nt), dim3(64 * NW), 2 * K::STAGE, s, a, b, bias, out, ldo, mt, nt);
-}
-
+// out from the sums over parts of the columns, in the order of the parts.
 template <bool F32>
-void launch(const CodeView& a, const CodeView& b, const float* bias, void* out, int64_t ldo, hipStream_t s) {
-  const bool fits = a.ld < (1 << 22) && b.ld < (1 << 22);  // a tile's offsets stay below 2^30
-  if (fits && a.rows >= 1024 && b.rows >= 256) { launch_tiled<4, 4, F32>(a, b, bias, out, ldo, s); return; }
-  if (fits && a.rows >= 128 && b.rows >= 128) { launch_tiled<2, 4, F32>(a, b, bias, out, ldo, s); return; }
-  if (a.rows <= 16) launch_direct<1, 1, 8, F32>(a, b, bias, out, ldo, s);
-  else if (a.rows <= 64) launch_direct<4, 1, 8, F32>(a, b, bias, out, ldo, s);
-  else launch_direct<4, 4, 4, F32>(a, b, bias, out, ldo, s);
+__global__ __launch_bounds__(256) void az_join_products(const float* __restrict__ parts, int count, int m, int n,
+                                                        const float* __restrict__ bias, void* __restrict__ out, int64_t ldo) {
+  const int64_t total = (int64_t)m * n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    float v = 0.0f;
+    for (int p = 0; p < count; p++) v += parts[p * total + i];
+    const int64_t r = i / n, c = i - r * n;
+    if (bias) v += bias[c];
+    if constexpr (F32) ((float*)out)[r * ldo + c] = v;
+    else ((uint16_t*)out)[r * ldo + c] = bf16_of(v);
+  }
 }
+
+// How a product runs: the kernel, and `parts` parts of the columns of part_steps K steps each.
+enum { DIRECT = 0, TILE32 = 1, TILE64 = 2, TILE128 = 3, TILE256 = 4 };
+struct Plan {
+  int kind, parts, part_steps;
+};
+
+// The plan with the least estimated time, in microseconds.  A tile kernel's K step takes a
+// workgroup `one` alone on a compute unit (bound by the step's own chain of copies, LDS reads and
+// the barrier) and `all` with `occ` of them there; both were measured, for bf16 results and for
+// the exact products of fp32 ones.  What parts cost is their way through memory and a second
+// launch.  Measured, chosen against the next best: 64 x 1880 x 10240 in 32-row tiles and 8 parts
+// 15.6 (4 parts 18.8, one part 46); 320 x 1880 x 10240 in 64-row tiles and 4 parts 25 (128-row,
+// 8 parts 26, one part 69); 1024 x 4672 x 8192 in 128-row tiles 54 (256-row 91); 4096^3 in 256-row
+// tiles 59 (128-row 67).
+Plan choose_plan(int64_t m, int64_t n, int64_t k, bool exact, bool fits) {
+  struct Tile {
+    int kind, tm, tn, occ;
+    double one, all, one_exact, all_exact;
+  };
+  static const Tile tiles[] = {{TILE32, 32, 128, 3, 0.53, 0.70, 0.55, 0.80},
+                               {TILE64, 64, 128, 3, 0.60, 0.87, 0.63, 1.35},
+                               {TILE128, 128, 128, 2, 0.69, 0.90, 0.80, 1.50},
+                               {TILE256, 256, 256, 1, 1.45, 1.72, 2.75, 3.30}};
+  const int nb = (int)((k + CB - 1) / CB);
+  const double write = 1.0 / 4.5e6;  // microseconds a byte
+  const double out = (double)m * (double)n * (exact ? 4 : 2) * write;
+  auto rounds = [](int64_t groups, int64_t slots) { return (double)((groups + slots - 1) / slots); };
+  Plan best = {DIRECT, 1, nb};
+  // eight waves take every eighth step each; rows of a that coincide are read once
+  double least = 4.0 + rounds((n + 15) / 16 * ((m + 15) / 16), 256) * (nb / 8.0 + 0.5) * (m <= 4 ? 0.6 : 1.0) + out;
+  if (!fits) return best;
+  for (const Tile& t : tiles) {
+    const int64_t count = ((m + t.tm - 1) / t.tm) * ((n + t.tn - 1) / t.tn);
+    const double one = exact ? t.one_exact : t.one, all = exact ? t.all_exact : t.all;
+    for (int parts = 1; parts <= 8 && (parts == 1 || 2 * parts <= nb); parts *= 2) {
+      const int64_t groups = count * parts, per = (groups + 255) / 256;
+      const int steps = (nb + parts - 1) / parts;
+      const int occ = per < t.occ ? (int)per : t.occ;
+      const double step = t.occ == 1 ? (per > 1 ? all : one) : one + (all - one) * (occ - 1) / (t.occ - 1);
+      double cost = 4.0 + rounds(groups, 256 * t.occ) * (steps * step + 2.0) + out;
+      if (parts > 1) cost += 3.5 + (double)parts * (double)m * (double)n * 8 * write;
+      if (cost < least) {
+        least = cost;
+        best = {t.kind, (nb + steps - 1) / steps, steps};
+      }
+    }
+  }
+  return best;
+}
+
+struct Operands {
+  CodeView a, b;
+  const float* bias;
+  void* out;
+  int64_t ldo, part_stride;
+  hipStream_t stream;
+};
+
+template <bool EXACT, bool F32>
+void launch_direct(const Plan& p, const Operands& o) {
+  const dim3 g((o.b.rows + 15) / 16, (o.a.rows + 15) / 16, p.parts);
+  hipLaunchKernelGGL((az_matmul_direct<1, 8, 2, EXACT, F32>), g, dim3(512), 0, o.stream, o.a, o.b, o.bias, o.out, o.ldo, p.part_steps, o.part_stride);
+}
+
+template <int FA, int FB, int WM, int WN, bool EXACT, bool F32>
+void launch_tiled(const Plan& p, const Operands& o) {
+  using K = Tiled<FA, FB, WM, WN, EXACT>;
+  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS);
+  (void)once;
+  const int mt = (o.a.rows + K::TM - 1) / K::TM, nt = (o.b.rows + K::TN - 1) / K::TN;
+  hipLaunchKernelGGL((az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>), dim3((unsigned)mt * (unsigned)nt, p.parts), dim3(256), K::LDS, o.stream,
+                     o.a, o.b, o.bias, o.out, o.ldo, mt, nt, p.part_steps, o.part_stride);
+}
+
+template <bool EXACT, bool F32>
+void launch(const Plan& p, const Operands& o) {
+  if (p.kind == TILE256) launch_tiled<4, 4, 2, 2, EXACT, F32>(p, o);
+  else if (p.kind == TILE128) launch_tiled<2, 2, 2, 2, EXACT, F32>(p, o);
+  else if (p.kind == TILE64) launch_tiled<1, 2, 2, 2, EXACT, F32>(p, o);
+  else if (p.kind == TILE32) launch_tiled<1, 1, 1, 4, EXACT, F32>(p, o);
+  else launch_direct<EXACT, F32>(p, o);
+}
+
+// A tile's offsets stay below 2^30.
+bool tile_fits(int64_t lda, int64_t ldb) { return lda < (1 << 22) && ldb < (1 << 22); }
 
 }  // namespace
 
+extern "C" size_t az_codes_matmul_workspace(const az_code_matrix* a, const az_code_matrix* b, int32_t dtype) {
+  if (!a || !b || a->rows <= 0 || b->rows <= 0 || a->cols <= 0) return 0;
+  const Plan p = choose_plan(a->rows, b->rows, a->cols, dtype == AZ_F32, tile_fits(a->ld, b->ld));
+  return p.parts > 1 ? (size_t)p.parts * (size_t)a->rows * (size_t)b->rows * sizeof(float) : 0;
+}
+
 extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b, const float* bias, void* out,
-                               int32_t dtype, int64_t ld_out, void* stream) {
+                               int32_t dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
   static const char who[] = "az_codes_matmul";
   int st = code_check(a, who);
   if (st == AZ_OK) st = code_check(b, who);
@@ -411,12 +546,34 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
   if (a->rows == 0 || b->rows == 0) return AZ_OK;
   if ((st = dense_check(out, dtype, ld_out, b->rows, who)) != AZ_OK) return st;
   if ((uintptr_t)bias & 3u) return code_fail(AZ_ERR_INVALID_ARG, who, "bias must be 4-byte aligned");
-  // 64 rows of a per workgroup row, and at most 65,535 of those in a grid
-  if (a->rows > (int64_t)65535 * 64) return code_fail(AZ_ERR_UNSUPPORTED, who, "more than 4,194,240 rows of a");
-  const CodeView va = code_view(*a), vb = code_view(*b);
-  const hipStream_t s = static_cast<hipStream_t>(stream);
+  // 16 rows of a to a row of the grid, and at most 65,535 of those; tiles in 31 bits
+  if (a->rows > (int64_t)65535 * 16 || ((a->rows + 31) / 32) * ((b->rows + 127) / 128) > INT32_MAX)
+    return code_fail(AZ_ERR_UNSUPPORTED, who, "a product past the size limits");
+  const size_t need = az_codes_matmul_workspace(a, b, dtype);
+  if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
+  if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
+  const Plan p = choose_plan(a->rows, b->rows, a->cols, dtype == AZ_F32, tile_fits(a->ld, b->ld));
+  Operands o = {code_view(*a), code_view(*b), bias, out, ld_out, 0, static_cast<hipStream_t>(stream)};
   (void)hipGetLastError();
-  if (dtype == AZ_F32) launch<true>(va, vb, bias, out, ld_out, s);
-  else launch<false>(va, vb, bias, out, ld_out, s);
+  if (p.parts > 1) {
+    o.bias = nullptr;
+    o.out = workspace;
+    o.ldo = b->rows;
+    o.part_stride = a->rows * b->rows;
+    if (dtype == AZ_F32) launch<true, true>(p, o);
+    else launch<false, true>(p, o);
+    if ((st = launch_status(who)) != AZ_OK) return st;
+    const int64_t groups = (a->rows * b->rows + 255) / 256;
+    const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
+    const float* parts = static_cast<const float*>(workspace);
+    if (dtype == AZ_F32)
+      hipLaunchKernelGGL((az_join_products<true>), g, dim3(256), 0, o.stream, parts, p.parts, (int)a->rows, (int)b->rows, bias, out, ld_out);
+    else
+      hipLaunchKernelGGL((az_join_products<false>), g, dim3(256), 0, o.stream, parts, p.parts, (int)a->rows, (int)b->rows, bias, out, ld_out);
+  } else if (dtype == AZ_F32) {
+    launch<true, true>(p, o);
+  } else {
+    launch<false, false>(p, o);
+  }
   return launch_status(who);
 }

@@ -326,19 +326,21 @@ class _Layer:
         self.dy = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
         self.dw, self.db = torch.empty((n, k), device="cuda"), torch.empty((n,), device="cuda")
         self.dx = torch.empty((m, k), dtype=torch.bfloat16, device="cuda")
-        self.ws = torch.empty((max(16, az.az_codes_weight_grad_workspace(m, n, k), az.az_logits_policy_workspace(m, n)),),
+        self.ws = torch.empty((max(16, az.az_codes_weight_grad_workspace(m, n, k), az.az_logits_policy_workspace(m, n),
+                                   az.az_codes_matmul_workspace(self.xq.c, self.wq.c, az.AZ_F32),
+                                   az.az_codes_matmul_workspace(self.dq.c, self.wt.c, az.AZ_BF16)),),
                               dtype=torch.uint8, device="cuda")
 
     def step(self):
         az = self.az
         az.quantize_tensors(self.x, self.xq)
         az.quantize_tensors(self.w, self.wq, self.wt)
-        az.matmul_tensors(self.xq, self.wq, self.z, bias=self.b)
+        az.matmul_tensors(self.xq, self.wq, self.z, bias=self.b, workspace=self.ws)
         az.policy_tensors(self.z, self.p, mask=self.legal, workspace=self.ws)
         self.dy.copy_((self.p - self.target) / self.m)
         az.weight_grad_tensors(self.dy, self.xq, self.dw, db=self.db, workspace=self.ws)
         az.quantize_tensors(self.dy, self.dq)
-        az.matmul_tensors(self.dq, self.wt, self.dx)
+        az.matmul_tensors(self.dq, self.wt, self.dx, workspace=self.ws)
 
     def outputs(self):
         return [t.clone() for t in (self.xq.codes, self.wt.codes, self.z, self.p, self.dw, self.db, self.dx)]

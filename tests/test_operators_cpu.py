@@ -28,8 +28,8 @@ def test_bad_matrices_are_refused(m, status):
     good = M()
     assert L.az_codes_quantize(P, az.AZ_F32, 1 << 40, m, None, None) == status
     assert L.az_codes_dequantize(m, P, az.AZ_F32, 1 << 40, None) == status
-    assert L.az_codes_matmul(m, good, None, P, az.AZ_F32, 1 << 40, None) == status
-    assert L.az_codes_matmul(good, m, None, P, az.AZ_F32, 1 << 40, None) == status
+    assert L.az_codes_matmul(m, good, None, P, az.AZ_F32, 1 << 40, P, 1 << 40, None) == status
+    assert L.az_codes_matmul(good, m, None, P, az.AZ_F32, 1 << 40, P, 1 << 40, None) == status
     if m.scale_rows == 1:
         assert L.az_codes_weight_grad(P, 1 << 40, 4, m, P, az.AZ_F32, 1 << 40, None, 0, P, 1 << 40, None) == status
     assert b"az_codes" in L.az_last_error()
@@ -55,14 +55,14 @@ def test_bad_calls_are_refused():
     assert d(m, None, az.AZ_F32, 40, None) == E and d(m, P, 7, 40, None) == E and d(m, P, az.AZ_F32, 39, None) == E
     assert d(None, P, az.AZ_F32, 40, None) == E
     mm = L.az_codes_matmul
-    assert mm(m, M(cols=41), None, P, az.AZ_F32, 4, None) == E
-    assert mm(m, m, None, P, az.AZ_INT8, 4, None) == E
-    assert mm(m, m, None, P, az.AZ_F32, 3, None) == E
-    assert mm(m, m, None, None, az.AZ_F32, 4, None) == E
-    assert mm(m, m, P + 1, P, az.AZ_F32, 4, None) == E
-    assert mm(m, m, None, P + 2, az.AZ_F32, 4, None) == E
-    assert mm(M(rows=0), m, None, None, az.AZ_F32, 4, None) == az.AZ_OK
-    assert mm(m, M(rows=0), None, None, az.AZ_F32, 4, None) == az.AZ_OK
+    assert mm(m, M(cols=41), None, P, az.AZ_F32, 4, P, 1 << 40, None) == E
+    assert mm(m, m, None, P, az.AZ_INT8, 4, P, 1 << 40, None) == E
+    assert mm(m, m, None, P, az.AZ_F32, 3, P, 1 << 40, None) == E
+    assert mm(m, m, None, None, az.AZ_F32, 4, P, 1 << 40, None) == E
+    assert mm(m, m, P + 1, P, az.AZ_F32, 4, P, 1 << 40, None) == E
+    assert mm(m, m, None, P + 2, az.AZ_F32, 4, P, 1 << 40, None) == E
+    assert mm(M(rows=0), m, None, None, az.AZ_F32, 4, P, 1 << 40, None) == az.AZ_OK
+    assert mm(m, M(rows=0), None, None, az.AZ_F32, 4, P, 1 << 40, None) == az.AZ_OK
     g = L.az_codes_weight_grad
     need = az.az_codes_weight_grad_workspace(4, 8, 40)
     ok = (P, 8, 8, m, P, az.AZ_F32, 40, None, 0, P, need, None)
@@ -85,6 +85,13 @@ def test_workspaces_are_demanded():
         x = M(rows=rows, cols=cols, ld=cols)
         assert L.az_codes_weight_grad(P, n, n, x, P, az.AZ_F32, cols, None, 0, P, need - 1, None) == E
         assert L.az_codes_weight_grad(P, n, n, x, P, az.AZ_F32, cols, None, 0, None, need, None) == E
+    a, b = M(rows=64, cols=1 << 14, ld=1 << 14), M(rows=256, cols=1 << 14, ld=1 << 14)
+    need = az.az_codes_matmul_workspace(a, b, az.AZ_BF16)
+    if need:
+        assert L.az_codes_matmul(a, b, None, P, az.AZ_BF16, 256, P, need - 1, None) == E
+        assert L.az_codes_matmul(a, b, None, P, az.AZ_BF16, 256, None, need, None) == E
+    assert L.az_codes_matmul(a, b, None, P, az.AZ_BF16, 256, P + 8, 1 << 40, None) == E
+    assert az.az_codes_matmul_workspace(M(rows=0), b, az.AZ_BF16) == 0
     need = az.az_logits_policy_workspace(1, 1 << 17)
     if need:
         l = logits(rows=1, vocab=1 << 17, ld=1 << 17)
