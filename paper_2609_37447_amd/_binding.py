@@ -417,26 +417,23 @@ class CodeMatrix:
         return cls(codes, scales, cols, scale_rows)
 
 
-class _On:
-    """The device that all operands share made the current one for a call, and the stream (torch's
-    current one by default) as the library takes it."""
+def _on(device, stream, *others):
+    """The call's stream as the library takes it (torch's current one by default), for operands that are all
+    on `device`."""
+    import torch
+    for t in others:
+        if t is not None and t.device != device:
+            raise ValueError("the operands are on different devices")
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
-    def __init__(self, stream, first, *others):
-        import torch
-        for t in others:
-            if t is not None and t.device != first:
-                raise ValueError("the operands are on different devices")
-        self.guard = torch.cuda.device(first) if first.index != torch.cuda.current_device() else None
-        self.s = torch.cuda.current_stream(first) if stream is None else stream
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.s.cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(device, fn, *args) -> int:
+    """fn(*args) with `device` as the current one."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
 
 
 def _workspace(given, need, device, stream):
@@ -468,8 +465,9 @@ def quantize_tensors(x, q: CodeMatrix, transposed: CodeMatrix = None, stream=Non
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
-    with _On(stream, x.device, q, transposed) as s:
-        return az_codes_quantize(x.data_ptr(), _float_type(x), ld, q.c, transposed.c if transposed is not None else None, s)
+    s = _on(x.device, stream, q, transposed)
+    return _call(x.device, az_codes_quantize, x.data_ptr(), _float_type(x), ld, q.c,
+                 transposed.c if transposed is not None else None, s)
 
 
 def dequantize_tensors(q: CodeMatrix, x, stream=None) -> int:
@@ -478,8 +476,8 @@ def dequantize_tensors(q: CodeMatrix, x, stream=None) -> int:
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
-    with _On(stream, x.device, q) as s:
-        return az_codes_dequantize(q.c, x.data_ptr(), _float_type(x), ld, s)
+    s = _on(x.device, stream, q)
+    return _call(x.device, az_codes_dequantize, q.c, x.data_ptr(), _float_type(x), ld, s)
 
 
 def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, workspace=None, stream=None) -> int:
@@ -492,10 +490,10 @@ def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, workspace=None,
         raise ValueError(f"out is {[m, n]}, the product {[a.rows, b.rows]}")
     if bias is not None:
         _vector_of("bias", bias, torch.float32, n)
-    with _On(stream, out.device, a, b, bias) as s:
-        dt = _float_type(out)
-        ws, size, keep = _workspace(workspace, az_codes_matmul_workspace(a.c, b.c, dt), out.device, stream)
-        return az_codes_matmul(a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), dt, ld, ws, size, s)
+    s, dt = _on(out.device, stream, a, b, bias), _float_type(out)
+    ws, size, keep = _workspace(workspace, az_codes_matmul_workspace(a.c, b.c, dt), out.device, stream)
+    return _call(out.device, az_codes_matmul, a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), dt,
+                 ld, ws, size, s)
 
 
 def weight_grad_tensors(dy, x: CodeMatrix, dw, db=None, accumulate: bool = False, workspace=None, stream=None) -> int:
@@ -511,10 +509,10 @@ def weight_grad_tensors(dy, x: CodeMatrix, dw, db=None, accumulate: bool = False
         raise ValueError(f"dw is {[wn, wk]}, the gradient {[n, x.cols]}")
     if db is not None:
         _vector_of("db", db, torch.float32, n)
-    with _On(stream, dw.device, dy, x, db) as s:
-        ws, size, keep = _workspace(workspace, az_codes_weight_grad_workspace(m, n, x.cols), dw.device, stream)
-        return az_codes_weight_grad(dy.data_ptr(), ldy, n, x.c, dw.data_ptr(), _float_type(dw), ldw,
-                                    db.data_ptr() if db is not None else None, accumulate, ws, size, s)
+    s = _on(dw.device, stream, dy, x, db)
+    ws, size, keep = _workspace(workspace, az_codes_weight_grad_workspace(m, n, x.cols), dw.device, stream)
+    return _call(dw.device, az_codes_weight_grad, dy.data_ptr(), ldy, n, x.c, dw.data_ptr(), _float_type(dw), ldw,
+                 db.data_ptr() if db is not None else None, accumulate, ws, size, s)
 
 
 def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None, penalties=None,
@@ -556,12 +554,12 @@ def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None
             _vector_of("lengths", lengths, torch.int32, b)
     elif lengths is not None or penalties is not None:
         raise ValueError("lengths and penalties come with a history")
-    with _On(stream, logits.device, out, mask, bias, history, lengths, penalties) as s:
-        ws, size, keep = _workspace(workspace, az_logits_policy_workspace(b, v), logits.device, stream)
-        p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
-        return az_logits_policy(az_logits(p(logits), _float_type(logits), b, v, ld, p(mask), kind, ldm, p(bias), ldb,
-                                          p(history), ldh, t, p(lengths), p(penalties)), probabilities, out.data_ptr(), ldo,
-                                ws, size, s)
+    s = _on(logits.device, stream, out, mask, bias, history, lengths, penalties)
+    ws, size, keep = _workspace(workspace, az_logits_policy_workspace(b, v), logits.device, stream)
+    p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
+    rows = az_logits(p(logits), _float_type(logits), b, v, ld, p(mask), kind, ldm, p(bias), ldb, p(history), ldh, t,
+                     p(lengths), p(penalties))
+    return _call(logits.device, az_logits_policy, rows, probabilities, out.data_ptr(), ldo, ws, size, s)
 
 
 AZ_PIPE_GRAPHS = 1
