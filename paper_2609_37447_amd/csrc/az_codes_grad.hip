@@ -65,7 +65,7 @@ __device__ __forceinline__ cm_i32x4 short_row(const uint16_t* row, int c, int n)
   return v;
 }
 
-// 64 columns of dy summed by one workgroup: 32 groups of rows, joined in order.
+// 64 columns of dy summed over `m` rows by one workgroup: 32 groups of rows, joined in order.
 __device__ void bias_columns(const uint16_t* __restrict__ dy, int64_t ldy, int n, int m, int n0, float* db, bool add, float* sums) {
   const int c = (threadIdx.x & 7) * 8, q = threadIdx.x >> 3;
   float s[8] = {};
@@ -76,12 +76,14 @@ __device__ void bias_columns(const uint16_t* __restrict__ dy, int64_t ldy, int n
   if (n >= 8) {
     const Chunk8 k(n0 + c, n);
     int i = q;
-    for (; i + 7 * 32 < m; i += 8 * 32) {
-      cm_i32x4 v[8];
+    constexpr int AHEAD = 16;  // loads on their way: a workgroup alone on its compute unit has latency to hide
+    for (; i + (AHEAD - 1) * 32 < m; i += AHEAD * 32) {
+      cm_i32x4 v[AHEAD];
 #pragma unroll
-      for (int u = 0; u < 8; u++) v[u] = k.load(dy + (i + u * 32) * ldy);
+      for (int u = 0; u < AHEAD; u++) v[u] = k.load(dy + (i + u * 32) * ldy);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < 8; u++) more(k.place(v[u]));
+      for (int u = 0; u < AHEAD; u++) more(k.place(v[u]));
     }
     for (; i < m; i += 32) more(k.place(k.load(dy + i * ldy)));
   } else {
@@ -160,17 +162,19 @@ struct Grad {
   }
 };
 
-// Blocks 0..bias-1 sum dy's columns; the others own a tile of dw each, for rows
-// part * rows_of_part on of blockIdx.y = part (sums over several parts go to
-// dw + part * part_stride of a workspace).
+// Blocks 0..bias-1 sum dy's columns; the others own a tile of dw each.  Both take the rows
+// part * part_rows on, part = blockIdx.y; sums over one of several parts go to a workspace, dw's at
+// part * part_stride and db's at part * n.
 template <int W, bool F32, int FEED>
 __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint16_t* __restrict__ dy, int64_t ldy, int n, CodeView x,
                                                                      void* __restrict__ dw, int64_t ldw, float* __restrict__ db,
-                                                                     int bias, int add, int part_rows, int64_t part_stride, int add_bias) {
+                                                                     int bias, int add, int part_rows, int64_t part_stride) {
   using G = Grad<W>;
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   if ((int)blockIdx.x < bias) {
-    if (blockIdx.y == 0) bias_columns(dy, ldy, n, x.rows, (int)blockIdx.x * 64, db, add_bias, reinterpret_cast<float*>(smem));
+    const int from = (int)blockIdx.y * part_rows;
+    bias_columns(dy + from * ldy, ldy, n, min(part_rows, x.rows - from), (int)blockIdx.x * 64, db + (int64_t)blockIdx.y * n, add,
+                 reinterpret_cast<float*>(smem));
     return;
   }
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -322,16 +326,23 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   }
 }
 
-// dw from the sums over parts, in the order of the parts.
+// dw and db from the sums over parts, in the order of the parts (db's lie behind dw's).
 template <bool F32>
 __global__ __launch_bounds__(NT) void az_join_parts(const float* __restrict__ parts, int count, int n, int cols,
-                                                    void* __restrict__ dw, int64_t ldw, int add) {
-  const int64_t total = (int64_t)n * cols;
-  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < total; i += (int64_t)gridDim.x * NT) {
+                                                    void* __restrict__ dw, int64_t ldw, float* __restrict__ db, int add) {
+  const int64_t total = (int64_t)n * cols, all = total + (db ? n : 0);
+  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < all; i += (int64_t)gridDim.x * NT) {
+    const bool weight = i < total;
+    const float* from = weight ? parts + i : parts + count * total + (i - total);
+    const int64_t step = weight ? total : n;
     float v = 0.0f;
-    for (int p = 0; p < count; p++) v += parts[p * total + i];
-    const int64_t r = i / cols;
-    put<F32>(dw, r * ldw + (i - r * cols), v, add);
+    for (int p = 0; p < count; p++) v += from[p * step];
+    if (weight) {
+      const int64_t r = i / cols;
+      put<F32>(dw, r * ldw + (i - r * cols), v, add);
+    } else {
+      put<true>(db, i - total, v, add);
+    }
   }
 }
 
@@ -340,22 +351,24 @@ struct Cut {
   int w, parts, part_rows;
 };
 
-// The cheapest cut by an estimate of its time in units of a quarter of a compute unit's
-// matrix work on a 64-row step of a 256 tile: rounds of workgroups times their steps
-// (and four steps' worth of start and end), plus the parts' way through memory (written,
-// read: about 50 outputs a unit).
+// The cut with the least estimated time, in microseconds.  A 64-row step takes a workgroup 0.72 (W = 2)
+// or 1.48 (W = 4) alone on a compute unit, bound by the step's own chain, 1.0 with two workgroups there
+// (W = 2) and 1.86 with every compute unit busy (W = 4), as measured.  Parts cost their way through
+// memory and a second launch.  Measured, chosen against others: 16384 x 512 x 512 in 16 parts of small
+// tiles 29 (32 parts 33, large tiles 45); 16384 x 4096 x 4096 in one part of large tiles 477; 16384 x
+// 1024 x 1024 in 8 parts of small tiles 58 (16 of large ones 63).
 Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
   const int64_t steps = rows > 0 ? (rows + MS - 1) / MS : 1;
+  const double write = 1.0 / 4.5e6, outputs = (double)n * (double)cols;  // microseconds a byte
   Cut best = {2, 1, (int)(steps * MS)};
   double least = 0;
   for (int w = n < 8 ? 2 : 4; w >= 2; w -= 2) {  // (rows of fewer than eight are read by the small tile alone)
     const int64_t t = 64 * w, tiles = ((n + t - 1) / t) * ((cols + t - 1) / t);
-    const int64_t slots = w == 4 ? 256 : 512;
-    for (int64_t parts = 1; parts <= 64 && (parts == 1 || parts * 4 <= steps); parts *= 2) {
-      const int64_t per = (steps + parts - 1) / parts;
-      const double rounds = (double)((tiles * parts + slots - 1) / slots);
-      const double cost = rounds * (double)(per + 4) * (w == 4 ? 4.0 : 2.2) +
-                          (parts > 1 ? 8.0 + (double)(parts * n * cols) / 50000.0 : 0.0);
+    for (int64_t parts = 1; parts <= 64 && (parts == 1 || 2 * parts <= steps); parts *= 2) {
+      const int64_t per = (steps + parts - 1) / parts, groups = tiles * parts, slots = w == 4 ? 256 : 512;
+      const double step = w == 4 ? (groups <= 128 ? 1.48 : 1.86) : (groups <= 256 ? 0.72 : 1.0);
+      double cost = (double)((groups + slots - 1) / slots) * ((double)per * step + 3.0) + outputs * 4 * write;
+      if (parts > 1) cost += 3.5 + (double)parts * outputs * 8 * write;
       if (least == 0 || cost < least) {
         least = cost;
         best = {w, (int)((steps + per - 1) / per), (int)(per * MS)};
@@ -366,7 +379,7 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
 }
 
 template <int W, bool F32, int FEED>
-void launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add, int add_bias,
+void launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
             const Cut& cut, int64_t part_stride, hipStream_t s) {
   using G = Grad<W>;
   constexpr int LDS = 2 * G::STAGE;
@@ -376,15 +389,15 @@ void launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw,
   const int bias = db ? (n + 63) / 64 : 0;
   const int64_t tiles = (int64_t)((n + G::T - 1) / G::T) * ((x.cols + G::T - 1) / G::T);
   hipLaunchKernelGGL((az_weight_grad<W, F32, FEED>), dim3((unsigned)(bias + tiles), (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
-                     dw, ldw, db, bias, add, cut.part_rows, part_stride, add_bias);
+                     dw, ldw, db, bias, add, cut.part_rows, part_stride);
 }
 
 template <int W, bool F32>
 void launch_feed(int feed, const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
-                 int add_bias, const Cut& cut, int64_t part_stride, hipStream_t s) {
-  if (feed == COPY) launch<W, F32, COPY>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
-  else if (feed == MOVE) launch<W, F32, MOVE>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
-  else if constexpr (W == 2) launch<W, F32, SHORT>(dy, ldy, n, x, dw, ldw, db, add, add_bias, cut, part_stride, s);
+                 const Cut& cut, int64_t part_stride, hipStream_t s) {
+  if (feed == COPY) launch<W, F32, COPY>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
+  else if (feed == MOVE) launch<W, F32, MOVE>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
+  else if constexpr (W == 2) launch<W, F32, SHORT>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
 }
 
 }  // namespace
@@ -392,7 +405,7 @@ void launch_feed(int feed, const uint16_t* dy, int64_t ldy, int n, const CodeVie
 extern "C" size_t az_codes_weight_grad_workspace(int64_t rows, int32_t n, int64_t cols) {
   if (rows <= 0 || n <= 0 || cols <= 0) return 0;
   const Cut cut = choose_cut(rows, n, cols);
-  return cut.parts > 1 ? (size_t)cut.parts * (size_t)n * (size_t)cols * sizeof(float) : 0;
+  return cut.parts > 1 ? (size_t)cut.parts * (size_t)n * ((size_t)cols + 1) * sizeof(float) : 0;
 }
 
 extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, const az_code_matrix* x, void* dw,
@@ -425,21 +438,22 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   void* to = direct ? dw : workspace;
   const int64_t ld = direct ? ld_dw : x->cols, stride = direct ? 0 : (int64_t)n * x->cols;
   const int add_here = direct ? add : 0;
+  float* bias = !db || direct ? db : static_cast<float*>(workspace) + (int64_t)cut.parts * n * x->cols;
   if (dtype == AZ_F32 || !direct) {
-    if (cut.w == 4) launch_feed<4, true>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
-    else launch_feed<2, true>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    if (cut.w == 4) launch_feed<4, true>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
+    else launch_feed<2, true>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
   } else {
-    if (cut.w == 4) launch_feed<4, false>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
-    else launch_feed<2, false>(feed, y, ld_dy, n, v, to, ld, db, add_here, add, cut, stride, s);
+    if (cut.w == 4) launch_feed<4, false>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
+    else launch_feed<2, false>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
   }
   if (!direct) {
     const int64_t groups = ((int64_t)n * x->cols + NT - 1) / NT;
     const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
     if ((st = launch_status(who)) != AZ_OK) return st;
     if (dtype == AZ_F32)
-      hipLaunchKernelGGL((az_join_parts<true>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, add);
+      hipLaunchKernelGGL((az_join_parts<true>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, db, add);
     else
-      hipLaunchKernelGGL((az_join_parts<false>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, add);
+      hipLaunchKernelGGL((az_join_parts<false>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, db, add);
   }
   return launch_status(who);
 }
