@@ -224,14 +224,16 @@ int pass_grid(const CodeView& q) {
 }
 
 template <bool BF16, bool VEC>
-void launch_quantize(const void* x, int64_t ldx, const CodeView& q, const CodeView* qt, hipStream_t s) {
+int launch_quantize(const void* x, int64_t ldx, const CodeView& q, const CodeView* qt, hipStream_t s) {
   if (q.shift == 0) {
     hipLaunchKernelGGL((az_quantize_rows<BF16, VEC>), dim3(pass_grid(q)), dim3(NT), 0, s, x, ldx, q);
-    return;
+    return AZ_OK;
   }
-  const int tiles = (q.rows + CB - 1) / CB * q.nb;
-  if (qt) hipLaunchKernelGGL((az_quantize_tiles<BF16, VEC, true>), dim3(tiles), dim3(NT), 0, s, x, ldx, q, *qt);
-  else hipLaunchKernelGGL((az_quantize_tiles<BF16, VEC, false>), dim3(tiles), dim3(NT), 0, s, x, ldx, q, q);
+  const int64_t tiles = (int64_t)((q.rows + CB - 1) / CB) * q.nb;
+  if (!grid_fits(tiles, NT)) return AZ_ERR_UNSUPPORTED;
+  if (qt) hipLaunchKernelGGL((az_quantize_tiles<BF16, VEC, true>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, *qt);
+  else hipLaunchKernelGGL((az_quantize_tiles<BF16, VEC, false>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, q);
+  return AZ_OK;
 }
 
 }  // namespace
@@ -256,14 +258,10 @@ extern "C" int az_codes_quantize(const void* x, int32_t dtype, int64_t ldx, cons
   const CodeView vt = qt ? code_view(*qt) : v;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (dtype == AZ_BF16) {
-    if (rows_aligned16(x, ldx, 2)) launch_quantize<true, true>(x, ldx, v, qt ? &vt : nullptr, s);
-    else launch_quantize<true, false>(x, ldx, v, qt ? &vt : nullptr, s);
-  } else {
-    if (rows_aligned16(x, ldx, 4)) launch_quantize<false, true>(x, ldx, v, qt ? &vt : nullptr, s);
-    else launch_quantize<false, false>(x, ldx, v, qt ? &vt : nullptr, s);
-  }
-  return launch_status(who);
+  const CodeView* t = qt ? &vt : nullptr;
+  if (dtype == AZ_BF16) st = rows_aligned16(x, ldx, 2) ? launch_quantize<true, true>(x, ldx, v, t, s) : launch_quantize<true, false>(x, ldx, v, t, s);
+  else st = rows_aligned16(x, ldx, 4) ? launch_quantize<false, true>(x, ldx, v, t, s) : launch_quantize<false, false>(x, ldx, v, t, s);
+  return launched(who, st);
 }
 
 extern "C" int az_codes_dequantize(const az_code_matrix* q, void* x, int32_t dtype, int64_t ldx, void* stream) {

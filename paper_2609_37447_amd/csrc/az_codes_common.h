@@ -76,6 +76,16 @@ inline int launch_status(const char* who) {
   return e == hipSuccess ? AZ_OK : code_fail(AZ_ERR_DEVICE, who, hipGetErrorString(e));
 }
 
+// Whether a grid of this many workgroups can be launched (its threads are counted in 32 bits).
+inline bool grid_fits(int64_t groups, int threads) { return groups * threads <= (int64_t)UINT32_MAX; }
+
+// The status of a launch: one that was refused before it, or the runtime's.
+inline int launched(const char* who, int status) {
+  if (status == AZ_ERR_UNSUPPORTED) return code_fail(status, who, "more results than a launch can cover");
+  if (status != AZ_OK) return code_fail(status, who, "the kernel's LDS size was refused");
+  return launch_status(who);
+}
+
 // 2^(s - 127) of a scale byte in 10..246; NaN for 255.
 __device__ __forceinline__ float scale_value(uint32_t s) {
   return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23);

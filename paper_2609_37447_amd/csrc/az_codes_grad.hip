@@ -379,25 +379,29 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
 }
 
 template <int W, bool F32, int FEED>
-void launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
-            const Cut& cut, int64_t part_stride, hipStream_t s) {
+int launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add, const Cut& cut,
+           int64_t part_stride, hipStream_t s) {
   using G = Grad<W>;
   constexpr int LDS = 2 * G::STAGE;
-  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_weight_grad<W, F32, FEED>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-  (void)once;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(az_weight_grad<W, F32, FEED>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (e != hipSuccess) return AZ_ERR_DEVICE;
   const int bias = db ? (n + 63) / 64 : 0;
-  const int64_t tiles = (int64_t)((n + G::T - 1) / G::T) * ((x.cols + G::T - 1) / G::T);
-  hipLaunchKernelGGL((az_weight_grad<W, F32, FEED>), dim3((unsigned)(bias + tiles), (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
+  const int64_t groups = bias + (int64_t)((n + G::T - 1) / G::T) * ((x.cols + G::T - 1) / G::T);
+  if (!grid_fits(groups, NT)) return AZ_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((az_weight_grad<W, F32, FEED>), dim3((unsigned)groups, (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
                      dw, ldw, db, bias, add, cut.part_rows, part_stride);
+  return AZ_OK;
 }
 
 template <int W, bool F32>
-void launch_feed(int feed, const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
-                 const Cut& cut, int64_t part_stride, hipStream_t s) {
-  if (feed == COPY) launch<W, F32, COPY>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
-  else if (feed == MOVE) launch<W, F32, MOVE>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
-  else if constexpr (W == 2) launch<W, F32, SHORT>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
+int launch_feed(int feed, const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, int64_t ldw, float* db, int add,
+                const Cut& cut, int64_t part_stride, hipStream_t s) {
+  if (feed == COPY) return launch<W, F32, COPY>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
+  if constexpr (W == 2) {
+    if (feed == SHORT) return launch<W, F32, SHORT>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
+  }
+  return launch<W, F32, MOVE>(dy, ldy, n, x, dw, ldw, db, add, cut, part_stride, s);
 }
 
 }  // namespace
@@ -425,8 +429,6 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
   if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
   const CodeView v = code_view(*x);
-  if ((((int64_t)n + 127) / 128) * ((x->cols + 127) / 128) > (1 << 30))
-    return code_fail(AZ_ERR_UNSUPPORTED, who, "a gradient past the size limits");
   const Cut cut = choose_cut(x->rows, n, x->cols);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint16_t* y = static_cast<const uint16_t*>(dy);
@@ -439,17 +441,16 @@ extern "C" int az_codes_weight_grad(const void* dy, int64_t ld_dy, int32_t n, co
   const int64_t ld = direct ? ld_dw : x->cols, stride = direct ? 0 : (int64_t)n * x->cols;
   const int add_here = direct ? add : 0;
   float* bias = !db || direct ? db : static_cast<float*>(workspace) + (int64_t)cut.parts * n * x->cols;
-  if (dtype == AZ_F32 || !direct) {
-    if (cut.w == 4) launch_feed<4, true>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
-    else launch_feed<2, true>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
-  } else {
-    if (cut.w == 4) launch_feed<4, false>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
-    else launch_feed<2, false>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
-  }
+  if (dtype == AZ_F32 || !direct)
+    st = cut.w == 4 ? launch_feed<4, true>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s)
+                    : launch_feed<2, true>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
+  else
+    st = cut.w == 4 ? launch_feed<4, false>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s)
+                    : launch_feed<2, false>(feed, y, ld_dy, n, v, to, ld, bias, add_here, cut, stride, s);
+  if ((st = launched(who, st)) != AZ_OK) return st;
   if (!direct) {
     const int64_t groups = ((int64_t)n * x->cols + NT - 1) / NT;
     const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
-    if ((st = launch_status(who)) != AZ_OK) return st;
     if (dtype == AZ_F32)
       hipLaunchKernelGGL((az_join_parts<true>), g, dim3(NT), 0, s, static_cast<const float*>(workspace), cut.parts, n, (int)x->cols, dw, ld_dw, db, add);
     else

@@ -28,118 +28,83 @@ __device__ __forceinline__ cm_bf16x8 fragment_bf16(const cm_i32x8& w, int i, flo
   return __builtin_bit_cast(cm_bf16x8, u);
 }
 
-// Few rows of a.  A workgroup of NW waves owns 16 FM rows of a times 16 rows of b.  Each wave takes
-// every NW-th K step of the workgroup's part of them straight from memory to registers, U steps'
-// loads on their way together; the waves' sums meet in LDS in the order of the waves.  Bound by
-// b's bytes, and by their latency where a wave has few steps.
-template <int FM, int NW, int U, bool EXACT>
-struct Direct {
-  struct Step {
-    cm_i32x8 a[FM], b;
-    uint32_t sa[FM], sb;
-  };
-  // (Which columns a lane's 32 codes are does not matter as long as a and b agree: four lanes take
-  // 64 bytes side by side, twice.)
-  static __device__ __forceinline__ cm_i32x8 whole_fragment(const uint8_t* row, int k0) {
-    const cm_i32x4 lo = *reinterpret_cast<const cm_i32x4*>(row + k0), hi = *reinterpret_cast<const cm_i32x4*>(row + k0 + 64);
-    return cm_i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-  }
-  static __device__ __forceinline__ void multiply(cm_f32x4 (&acc)[FM], const Step& s) {
+// Few rows of a.  A workgroup of eight waves owns 16 rows of a times 16 rows of b.  Each wave takes
+// every eighth K step straight from memory to registers, two steps' loads on their way together; the
+// waves' sums meet in LDS in the order of the waves.  Bound by b's bytes and their latency
+// (1 x 4672 x 8192: 13 us, of which a launch takes 4); four or eight steps at once were no faster, and
+// sixteen waves neither.
+constexpr int DW = 8, DU = 2;
+
+struct DirectStep {
+  cm_i32x8 a, b;
+  uint32_t sa, sb;
+  template <bool EXACT>
+  __device__ __forceinline__ void add_to(cm_f32x4& acc) const {
     if constexpr (!EXACT) {
-#pragma unroll
-      for (int i = 0; i < FM; i++)
-        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(s.b, s.a[i], acc[i], 0, 0, 0, (int)s.sb, 0, (int)s.sa[i]);
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, 0, 0, 0, (int)sb, 0, (int)sa);
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const cm_bf16x8 vb = fragment_bf16(s.b, q, scale_value(s.sb));
-#pragma unroll
-        for (int i = 0; i < FM; i++)
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, fragment_bf16(s.a[i], q, scale_value(s.sa[i])), acc[i], 0, 0, 0);
-      }
+      for (int q = 0; q < 4; q++)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fragment_bf16(b, q, scale_value(sb)), fragment_bf16(a, q, scale_value(sa)), acc, 0, 0, 0);
     }
   }
 };
 
-template <int FM, int NW, int U, bool EXACT, bool F32>
-__global__ __launch_bounds__(NW * 64) void az_matmul_direct(CodeView a, CodeView b, const float* __restrict__ bias,
-                                                            void* __restrict__ out, int64_t ldo, int part_steps, int64_t part_stride) {
-  using D = Direct<FM, NW, U, EXACT>;
-  __shared__ cm_f32x4 part[(NW - 1) * FM * 64];
+// (Which columns a lane's 32 codes are does not matter as long as a and b agree: four lanes take
+// 64 bytes side by side, twice.)
+__device__ __forceinline__ cm_i32x8 direct_fragment(const uint8_t* p) {
+  const cm_i32x4 lo = *reinterpret_cast<const cm_i32x4*>(p), hi = *reinterpret_cast<const cm_i32x4*>(p + 64);
+  return cm_i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+}
+
+// EXACT: products on the bf16 instruction, fp32 out; otherwise on the e4m3 one, bf16 out.
+template <bool EXACT>
+__global__ __launch_bounds__(DW * 64) void az_matmul_direct(CodeView a, CodeView b, const float* __restrict__ bias,
+                                                            void* __restrict__ out, int64_t ldo, int nt) {
+  __shared__ cm_f32x4 part[(DW - 1) * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int m0 = blockIdx.y * 16 * FM, n0 = blockIdx.x * 16;
-  const int first = (int)blockIdx.z * part_steps, last = min(first + part_steps, a.nb), whole = min(last, a.cols / CB);
-  const uint8_t *ar[FM], *as[FM];
+  const int m0 = (int)(blockIdx.x / (uint32_t)nt) * 16, n0 = (int)(blockIdx.x % (uint32_t)nt) * 16;
+  const int whole = a.cols / CB;
+  const int am = min(m0 + r, a.rows - 1), bn = min(n0 + r, b.rows - 1);
+  const uint8_t *ar = a.codes + am * a.ld, *br = b.codes + bn * b.ld;
+  const uint8_t *as = a.scales + (int64_t)(am >> a.shift) * a.nb, *bs = b.scales + (int64_t)(bn >> b.shift) * b.nb;
+  cm_f32x4 acc = {0, 0, 0, 0};
+  for (int kb = wave; kb < whole; kb += DW * DU) {
+    DirectStep s[DU];
 #pragma unroll
-  for (int i = 0; i < FM; i++) {
-    const int row = min(m0 + 16 * i + r, a.rows - 1);
-    ar[i] = a.codes + row * a.ld;
-    as[i] = a.scales + (int64_t)(row >> a.shift) * a.nb;
-  }
-  const int brow = min(n0 + r, b.rows - 1);
-  const uint8_t* br = b.codes + brow * b.ld;
-  const uint8_t* bs = b.scales + (int64_t)(brow >> b.shift) * b.nb;
-  cm_f32x4 acc[FM];
-#pragma unroll
-  for (int i = 0; i < FM; i++) acc[i] = cm_f32x4{0, 0, 0, 0};
-  for (int kb = first + wave; kb < whole; kb += NW * U) {
-    typename D::Step s[U];
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int k = min(kb + u * NW, whole - 1);
-      s[u].b = D::whole_fragment(br, k * CB + g * 16);
-      s[u].sb = bs[k];
-#pragma unroll
-      for (int i = 0; i < FM; i++) {
-        s[u].a[i] = D::whole_fragment(ar[i], k * CB + g * 16);
-        s[u].sa[i] = as[i][k];
-      }
+    for (int u = 0; u < DU; u++) {
+      const int k = min(kb + u * DW, whole - 1);
+      s[u] = {direct_fragment(ar + k * CB + g * 16), direct_fragment(br + k * CB + g * 16), as[k], bs[k]};
     }
     __builtin_amdgcn_sched_barrier(0);  // all of them before the first is waited for
 #pragma unroll
-    for (int u = 0; u < U; u++) {
+    for (int u = 0; u < DU; u++) {
       // (past the end the last step was read again: its codes count as zeros, which adds nothing but
       // a NaN that is in the result already)
-      if (u > 0) s[u].b &= -(int)(kb + u * NW < whole);
-      D::multiply(acc, s[u]);
+      if (u > 0) s[u].b &= -(int)(kb + u * DW < whole);
+      s[u].add_to<EXACT>(acc);
     }
   }
-  if (whole < last && wave == (whole - first) % NW) {  // the columns that do not fill a step
-    typename D::Step s;
+  if (whole < a.nb && wave == whole % DW) {  // the columns that do not fill a step
     const int k0 = whole * CB + g * 32;
-    s.b = row_fragment(br, k0, a.cols);
-    s.sb = bs[whole];
-#pragma unroll
-    for (int i = 0; i < FM; i++) {
-      s.a[i] = row_fragment(ar[i], k0, a.cols);
-      s.sa[i] = as[i][whole];
-    }
-    D::multiply(acc, s);
+    const DirectStep s = {row_fragment(ar, k0, a.cols), row_fragment(br, k0, a.cols), as[whole], bs[whole]};
+    s.add_to<EXACT>(acc);
   }
-  if (wave > 0) {
-#pragma unroll
-    for (int i = 0; i < FM; i++) part[((wave - 1) * FM + i) * 64 + lane] = acc[i];
-  }
+  if (wave > 0) part[(wave - 1) * 64 + lane] = acc;
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
-  for (int w = 0; w < NW - 1; w++)
+  for (int w = 0; w < DW - 1; w++) acc += part[w * 64 + lane];
+  const int m = m0 + r;
+  if (m >= a.rows) return;
 #pragma unroll
-    for (int i = 0; i < FM; i++) acc[i] += part[(w * FM + i) * 64 + lane];
-  const int64_t at = (int64_t)blockIdx.z * part_stride;
-#pragma unroll
-  for (int i = 0; i < FM; i++) {
-    const int m = m0 + 16 * i + r;
-    if (m >= a.rows) continue;
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-      const int n = n0 + 4 * g + e;
-      if (n >= b.rows) continue;
-      const float v = acc[i][e] + (bias ? bias[n] : 0.0f);
-      if constexpr (F32) ((float*)out)[at + m * ldo + n] = v;
-      else ((uint16_t*)out)[at + m * ldo + n] = bf16_of(v);
-    }
+  for (int e = 0; e < 4; e++) {
+    const int n = n0 + 4 * g + e;
+    if (n >= b.rows) continue;
+    const float v = acc[e] + (bias ? bias[n] : 0.0f);
+    if constexpr (EXACT) ((float*)out)[m * ldo + n] = v;
+    else ((uint16_t*)out)[m * ldo + n] = bf16_of(v);
   }
 }
 
@@ -498,30 +463,37 @@ struct Operands {
   hipStream_t stream;
 };
 
-template <bool EXACT, bool F32>
-void launch_direct(const Plan& p, const Operands& o) {
-  const dim3 g((o.b.rows + 15) / 16, (o.a.rows + 15) / 16, p.parts);
-  hipLaunchKernelGGL((az_matmul_direct<1, 8, 2, EXACT, F32>), g, dim3(512), 0, o.stream, o.a, o.b, o.bias, o.out, o.ldo, p.part_steps, o.part_stride);
+template <bool EXACT>
+int launch_direct(const Operands& o) {
+  const int nt = (o.b.rows + 15) / 16;
+  const int64_t groups = (int64_t)nt * ((o.a.rows + 15) / 16);
+  if (!grid_fits(groups, DW * 64)) return AZ_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((az_matmul_direct<EXACT>), dim3((unsigned)groups), dim3(DW * 64), 0, o.stream, o.a, o.b, o.bias, o.out, o.ldo, nt);
+  return AZ_OK;
 }
 
 template <int FA, int FB, int WM, int WN, bool EXACT, bool F32>
-void launch_tiled(const Plan& p, const Operands& o) {
+int launch_tiled(const Plan& p, const Operands& o) {
   using K = Tiled<FA, FB, WM, WN, EXACT>;
-  static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS);
-  (void)once;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS);
+  if (e != hipSuccess) return AZ_ERR_DEVICE;
   const int mt = (o.a.rows + K::TM - 1) / K::TM, nt = (o.b.rows + K::TN - 1) / K::TN;
-  hipLaunchKernelGGL((az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>), dim3((unsigned)mt * (unsigned)nt, p.parts), dim3(256), K::LDS, o.stream,
+  if (!grid_fits((int64_t)mt * nt, 256)) return AZ_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>), dim3((unsigned)(mt * nt), p.parts), dim3(256), K::LDS, o.stream,
                      o.a, o.b, o.bias, o.out, o.ldo, mt, nt, p.part_steps, o.part_stride);
+  return AZ_OK;
 }
 
 template <bool EXACT, bool F32>
-void launch(const Plan& p, const Operands& o) {
-  if (p.kind == TILE256) launch_tiled<4, 4, 2, 2, EXACT, F32>(p, o);
-  else if (p.kind == TILE128) launch_tiled<2, 2, 2, 2, EXACT, F32>(p, o);
-  else if (p.kind == TILE64) launch_tiled<1, 2, 2, 2, EXACT, F32>(p, o);
-  else if (p.kind == TILE32) launch_tiled<1, 1, 1, 4, EXACT, F32>(p, o);
-  else launch_direct<EXACT, F32>(p, o);
+int launch(const Plan& p, const Operands& o) {
+  int st = AZ_OK;
+  if (p.kind == TILE256) st = launch_tiled<4, 4, 2, 2, EXACT, F32>(p, o);
+  else if (p.kind == TILE128) st = launch_tiled<2, 2, 2, 2, EXACT, F32>(p, o);
+  else if (p.kind == TILE64) st = launch_tiled<1, 2, 2, 2, EXACT, F32>(p, o);
+  else if (p.kind == TILE32) st = launch_tiled<1, 1, 1, 4, EXACT, F32>(p, o);
+  else if constexpr (EXACT == F32) st = launch_direct<EXACT>(o);  // (in one part: never sums of e4m3 products in fp32)
+  return launched("az_codes_matmul", st);
 }
 
 // A tile's offsets stay below 2^30.
@@ -546,9 +518,6 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
   if (a->rows == 0 || b->rows == 0) return AZ_OK;
   if ((st = dense_check(out, dtype, ld_out, b->rows, who)) != AZ_OK) return st;
   if ((uintptr_t)bias & 3u) return code_fail(AZ_ERR_INVALID_ARG, who, "bias must be 4-byte aligned");
-  // 16 rows of a to a row of the grid, and at most 65,535 of those; tiles in 31 bits
-  if (a->rows > (int64_t)65535 * 16 || ((a->rows + 31) / 32) * ((b->rows + 127) / 128) > INT32_MAX)
-    return code_fail(AZ_ERR_UNSUPPORTED, who, "a product past the size limits");
   const size_t need = az_codes_matmul_workspace(a, b, dtype);
   if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
   if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
@@ -560,9 +529,7 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
     o.out = workspace;
     o.ldo = b->rows;
     o.part_stride = a->rows * b->rows;
-    if (dtype == AZ_F32) launch<true, true>(p, o);
-    else launch<false, true>(p, o);
-    if ((st = launch_status(who)) != AZ_OK) return st;
+    if ((st = dtype == AZ_F32 ? launch<true, true>(p, o) : launch<false, true>(p, o)) != AZ_OK) return st;
     const int64_t groups = (a->rows * b->rows + 255) / 256;
     const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
     const float* parts = static_cast<const float*>(workspace);
@@ -570,10 +537,7 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
       hipLaunchKernelGGL((az_join_products<true>), g, dim3(256), 0, o.stream, parts, p.parts, (int)a->rows, (int)b->rows, bias, out, ld_out);
     else
       hipLaunchKernelGGL((az_join_products<false>), g, dim3(256), 0, o.stream, parts, p.parts, (int)a->rows, (int)b->rows, bias, out, ld_out);
-  } else if (dtype == AZ_F32) {
-    launch<true, true>(p, o);
-  } else {
-    launch<false, false>(p, o);
+    return launch_status(who);
   }
-  return launch_status(who);
+  return dtype == AZ_F32 ? launch<true, true>(p, o) : launch<false, false>(p, o);
 }
