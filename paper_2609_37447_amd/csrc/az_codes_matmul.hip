@@ -268,18 +268,27 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(Co
   const uint8_t* ap = smem + (wm + r) * CB;
   const uint8_t* bp = smem + K::ASTEP + (wn + r) * CB;
   const int at[2][2] = {{((2 * h) ^ sw) * 16, ((2 * h + 1) ^ sw) * 16}, {((2 * h + 4) ^ sw) * 16, ((2 * h + 5) ^ sw) * 16}};
-  uint32_t ac[K::FA], bc[K::FB];  // places of the lane's rows' scales
+  // Scales: the byte that counts is moved down to the lowest, which is the one that the instruction
+  // takes; a shift goes by its amount's low five bits, so that (place + kb) % 4 costs nothing.
+  uint32_t ac[K::FA], bc[K::FB];  // eight times the places of the lane's rows' scales
 #pragma unroll
-  for (int i = 0; i < K::FA; i++) ac[i] = aw.place(a, m0 + min(wm + 32 * i + r, ms - 1));
+  for (int i = 0; i < K::FA; i++) ac[i] = 8 * aw.place(a, m0 + min(wm + 32 * i + r, ms - 1));
 #pragma unroll
-  for (int j = 0; j < K::FB; j++) bc[j] = bw.place(b, n0 + min(wn + 32 * j + r, ns - 1));
+  for (int j = 0; j < K::FB; j++) bc[j] = 8 * bw.place(b, n0 + min(wn + 32 * j + r, ns - 1));
   uint32_t sa[K::FA], sb[K::FB], na[K::FA], nb[K::FB];
-  auto scales = [&](uint32_t (&pa)[K::FA], uint32_t (&pb)[K::FB], int kb) {
-    const uint8_t* from = smem + (kb & 1) * K::STAGE + K::SCALES + r * 4;
+  auto scale_words = [&](int kb) {
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(smem + (kb & 1) * K::STAGE + K::SCALES) + r;
 #pragma unroll
-    for (int i = 0; i < K::FA; i++) pa[i] = from[(wm + 32 * i) * 4 + ((ac[i] + kb) & 3u)];
+    for (int i = 0; i < K::FA; i++) na[i] = from[wm + 32 * i];
 #pragma unroll
-    for (int j = 0; j < K::FB; j++) pb[j] = from[(K::SA + wn + 32 * j) * 4 + ((bc[j] + kb) & 3u)];
+    for (int j = 0; j < K::FB; j++) nb[j] = from[K::SA + wn + 32 * j];
+  };
+  auto scales = [&](int kb) {
+    constexpr uint32_t ONE = EXACT ? 0xffu : ~0u;
+#pragma unroll
+    for (int i = 0; i < K::FA; i++) sa[i] = (na[i] >> ((ac[i] + 8 * kb) & 31)) & ONE;
+#pragma unroll
+    for (int j = 0; j < K::FB; j++) sb[j] = (nb[j] >> ((bc[j] + 8 * kb) & 31)) & ONE;
   };
 
   cm_f32x16 acc[K::FA][K::FB];
@@ -294,7 +303,8 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(Co
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     fetch(first + 1);
-    scales(sa, sb, first);
+    scale_words(first);
+    scales(first);
     K::read(f0, ap + stage + at[0][0], ap + stage + at[0][1], bp + stage + at[0][0], bp + stage + at[0][1]);
   }
   for (int kb = first; kb < whole; kb++) {
@@ -309,21 +319,18 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(Co
     __syncthreads();
     // (after the last step these are the bytes of the step before: read, not used)
     K::read(f0, ap + next + at[0][0], ap + next + at[0][1], bp + next + at[0][0], bp + next + at[0][1]);
-    scales(na, nb, kb + 1);
+    scale_words(kb + 1);
     fetch(kb + 2);
     K::multiply(acc, f1, sa, sb);
     K::interleave();
-#pragma unroll
-    for (int i = 0; i < K::FA; i++) sa[i] = na[i];
-#pragma unroll
-    for (int j = 0; j < K::FB; j++) sb[j] = nb[j];
+    scales(kb + 1);
   }
   __builtin_amdgcn_s_waitcnt(0);  // no copy into LDS is under way when the workgroup ends
   if (whole < last) {  // the columns that do not fill a step, straight from memory
 #pragma unroll
-    for (int i = 0; i < K::FA; i++) sa[i] = a.scales[ac[i] - aw.skip + whole];
+    for (int i = 0; i < K::FA; i++) sa[i] = a.scales[(int64_t)((m0 + min(wm + 32 * i + r, ms - 1)) >> a.shift) * a.nb + whole];
 #pragma unroll
-    for (int j = 0; j < K::FB; j++) sb[j] = b.scales[bc[j] - bw.skip + whole];
+    for (int j = 0; j < K::FB; j++) sb[j] = b.scales[(int64_t)((n0 + min(wn + 32 * j + r, ns - 1)) >> b.shift) * b.nb + whole];
 #pragma unroll
     for (int s = 0; s < 2; s++) {
 #pragma unroll
