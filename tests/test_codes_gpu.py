@@ -450,3 +450,67 @@ def test_tensor_checks():
                                torch.empty((30, 50), device="cuda"))
     with pytest.raises(ValueError):
         az.CodeMatrix(torch.zeros((4, 32), dtype=torch.uint8, device="cuda"), torch.zeros((4, 2), dtype=torch.uint8, device="cuda"))
+
+
+# --------------------------------------------------------------------------- #
+# Offsets past 32 bits
+# --------------------------------------------------------------------------- #
+def _decoded(codes, scales):
+    """Values of a coded matrix with a scale for each row's blocks, float64, on its device."""
+    import torch
+    table = torch.tensor(O.TABLE, device=codes.device)
+    s = torch.tensor([2.0 ** (b - 127) for b in range(256)], dtype=torch.float64, device=codes.device)
+    return table[codes.long()] * s[scales.long()].repeat_interleave(128, dim=1)[:, :codes.shape[1]]
+
+
+def test_offsets_past_32_bits():
+    az, torch = _az()
+    rows, cols = 36000, 131072  # 4.7 GB of codes
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn((rows, cols), generator=g, device="cuda", dtype=torch.bfloat16)
+    q = az.CodeMatrix.empty(rows, cols)
+    az.quantize_tensors(x, q)
+    tail = az.CodeMatrix.empty(100, cols)
+    az.quantize_tensors(x[-100:].clone(), tail)
+    assert torch.equal(q.codes[-100:], tail.codes) and torch.equal(q.scales[-100:], tail.scales)
+    # restored into the 9.4 GB it came from
+    az.dequantize_tensors(q, x)
+    assert torch.equal(x[-100:].double(), _decoded(tail.codes, tail.scales))
+    del x
+    # as the weights of a product, by the kernels of few and of more rows
+    tv = _decoded(tail.codes, tail.scales)
+    for m in (2, 40, 200):
+        a = az.CodeMatrix.empty(m, cols)
+        az.quantize_tensors(torch.randn((m, cols), generator=g, device="cuda"), a)
+        out = torch.empty((m, rows), device="cuda")
+        az.matmul_tensors(a, q, out)
+        av = _decoded(a.codes, a.scales)
+        want = torch.mm(av, tv.t().contiguous())
+        assert bool(((out[:, -100:].double() - want).abs() <= cols * 2.0 ** -23 * torch.mm(av.abs(), tv.abs().t().contiguous())).all())
+        other = torch.empty((rows, m), device="cuda")  # and as the activations
+        az.matmul_tensors(q, a, other)
+        assert bool(((other[-100:].t().double() - want).abs() <= cols * 2.0 ** -23 * torch.mm(av.abs(), tv.abs().t().contiguous())).all())
+    # as a saved activation: only the last rows have a gradient
+    dy = torch.zeros((rows, 24), device="cuda", dtype=torch.bfloat16)
+    dy[-100:] = torch.randn((100, 24), generator=g, device="cuda").to(torch.bfloat16)
+    dw, small = torch.empty((24, cols), device="cuda"), torch.empty((24, cols), device="cuda")
+    az.weight_grad_tensors(dy, q, dw)
+    az.weight_grad_tensors(dy[-100:].clone(), tail, small)
+    y = dy[-100:].double()
+    size = torch.mm(y.t().abs().contiguous(), tv.abs())
+    want = torch.mm(y.t().contiguous(), tv)
+    assert bool(((dw.double() - want).abs() <= 200 * 2.0 ** -23 * size).all())
+    assert bool(((small.double() - want).abs() <= 200 * 2.0 ** -23 * size).all())
+
+
+def test_outputs_past_32_bits():
+    az, torch = _az()
+    m, n = 40000, 30000  # 4.8 GB of fp32 results
+    a, av = _coded(_rng(31), m, 20)
+    b, bv = _coded(_rng(32), n, 20)
+    out = torch.full((m, n), float("nan"), device="cuda")
+    az.matmul_tensors(a, b, out)
+    got = _host(out[-70:, -300:])
+    _check(got, av[-70:] @ bv[-300:].T, np.abs(av[-70:]) @ np.abs(bv[-300:]).T, 21, False)
+    assert bool(torch.isfinite(out.sum(dim=1)).all())

@@ -278,3 +278,33 @@ def test_tensor_checks():
     with pytest.raises(ValueError):
         az.policy_tensors(x.half(), out)
     az.policy_tensors(torch.zeros((0, 100), device="cuda"), torch.zeros((0, 100), device="cuda"))
+
+
+def test_offsets_past_32_bits():
+    import torch
+
+    import paper_2609_37447_amd as az
+    rows, vocab = 17000, 131072  # 4.5 GB of logits, 8.9 GB of results
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn((rows, vocab), generator=g, device="cuda", dtype=torch.bfloat16)
+    mask = torch.randint(0, 2, (rows, vocab), generator=g, device="cuda", dtype=torch.uint8)
+    out = torch.full((rows, vocab), float("nan"), device="cuda")
+    az.policy_tensors(x, out, mask=mask)
+    last = torch.empty((3, vocab), device="cuda")
+    az.policy_tensors(x[-3:].clone(), last, mask=mask[-3:].clone())
+    assert bool(((out[-3:] - last).abs() <= last * U * (22 * 12 + 8 + vocab / 64 + 64)).all())
+    want = torch.softmax(x[-3:].double().masked_fill(mask[-3:] == 0, float("-inf")), dim=1)
+    assert bool(((out[-3:].double() - want).abs() <= want * U * (22 * 6 + 8 + vocab / 64 + 64)).all())
+    assert bool((out.sum(dim=1) - 1).abs().max() < 1e-4)
+
+
+def test_more_rows_than_a_grid_has():
+    import torch
+
+    import paper_2609_37447_amd as az
+    x = torch.randn((70001, 9), device="cuda")
+    out = torch.full_like(x, float("nan"))
+    az.policy_tensors(x, out)
+    want = torch.softmax(x.double(), dim=1)
+    assert bool(((out.double() - want).abs() <= want * U * (22 * float(x.abs().max()) + 80)).all())
