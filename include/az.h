@@ -437,7 +437,8 @@ int az_codes_quantize(const void* x, int32_t dtype, int64_t ldx, const az_code_m
 int az_codes_dequantize(const az_code_matrix* q, void* x, int32_t dtype, int64_t ldx, void* stream);
 
 /* out[m][n] = bias[n] + sum_k a[m][k] b[n][k]: a is [M][K] (activations), b [N][K]
- * (a layer's weights, one row per output); either may have scale_rows 1 or 128.
+ * (a layer's weights, one row per output); either may have scale_rows 1 or 128, and
+ * both an ld below 2^27.
  *   bias  device, [N] fp32, or NULL.
  *   out   device, [M][N], dtype AZ_BF16 or AZ_F32, ld_out elements from row to row,
  *         aligned to its element.

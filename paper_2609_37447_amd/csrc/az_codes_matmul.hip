@@ -14,6 +14,8 @@
 
 namespace {
 
+typedef __attribute__((address_space(3))) uint8_t lds_bytes;
+
 // 32 consecutive codes of a row for K step kb, the operand of a lane (row l % 16,
 // columns 32 (l / 16) on).
 __device__ __forceinline__ cm_i32x8 row_fragment(const uint8_t* row, int k0, int cols) {
@@ -29,10 +31,10 @@ __device__ __forceinline__ cm_bf16x8 fragment_bf16(const cm_i32x8& w, int i, flo
 }
 
 // Few rows of a.  A workgroup of eight waves owns 16 rows of a times 16 rows of b.  Each wave takes
-// every eighth K step straight from memory to registers, two steps' loads on their way together; the
-// waves' sums meet in LDS in the order of the waves.  Bound by b's bytes and their latency
-// (1 x 4672 x 8192: 13 us, of which a launch takes 4); four or eight steps at once were no faster, and
-// sixteen waves neither.
+// every eighth K step, two steps on their way together, through LDS of its own: the copies read whole
+// 128-byte lines (loads straight into the operands' places would take 64 bytes of each of 16 rows:
+// 1 x 4672 x 8192 13.2 us instead of 11.2).  The waves' sums meet in LDS in the order of the waves.
+// Bound by b's bytes and their latency; four steps at once, or sixteen waves, were no faster.
 constexpr int DW = 8, DU = 2;
 
 struct DirectStep {
@@ -50,47 +52,67 @@ struct DirectStep {
   }
 };
 
-// (Which columns a lane's 32 codes are does not matter as long as a and b agree: four lanes take
-// 64 bytes side by side, twice.)
-__device__ __forceinline__ cm_i32x8 direct_fragment(const uint8_t* p) {
-  const cm_i32x4 lo = *reinterpret_cast<const cm_i32x4*>(p), hi = *reinterpret_cast<const cm_i32x4*>(p + 64);
-  return cm_i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+// 16 rows of a step, straight into 2 KB of LDS: a lane one chunk of row lane / 8 (`row` bytes in) and
+// of the row eight below, whose chunks are exchanged by 4 more.
+__device__ __forceinline__ void direct_copy(__amdgpu_buffer_rsrc_t rows, int ld, uint32_t row, int chunk, int at, lds_bytes* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to, 16, row + chunk * 16, at, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to + 1024, 16, row + (chunk ^ 4) * 16, at + 8 * ld, 0, 0);
 }
 
 // EXACT: products on the bf16 instruction, fp32 out; otherwise on the e4m3 one, bf16 out.
 template <bool EXACT>
 __global__ __launch_bounds__(DW * 64) void az_matmul_direct(CodeView a, CodeView b, const float* __restrict__ bias,
                                                             void* __restrict__ out, int64_t ldo, int nt) {
-  __shared__ cm_f32x4 part[(DW - 1) * 64];
+  __shared__ __attribute__((aligned(16))) uint8_t tiles[DW][DU][2][16 * CB];  // and the waves' sums, afterwards
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int m0 = (int)(blockIdx.x / (uint32_t)nt) * 16, n0 = (int)(blockIdx.x % (uint32_t)nt) * 16;
-  const int whole = a.cols / CB;
+  const int whole = a.cols / CB, width = (a.cols + 15) & ~15;
   const int am = min(m0 + r, a.rows - 1), bn = min(n0 + r, b.rows - 1);
-  const uint8_t *ar = a.codes + am * a.ld, *br = b.codes + bn * b.ld;
   const uint8_t *as = a.scales + (int64_t)(am >> a.shift) * a.nb, *bs = b.scales + (int64_t)(bn >> b.shift) * b.nb;
+  // Chunks are exchanged by the row, as in the tiles below; rows past the matrix read as zeros.
+  const int crow = lane >> 3, chunk = (lane & 7) ^ ((crow >> 1) & 7);
+  const uint32_t arow = (uint32_t)crow * (uint32_t)a.ld, brow = (uint32_t)crow * (uint32_t)b.ld;
+  const __amdgpu_buffer_rsrc_t abuf =
+      __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, (min(a.rows - m0, 16) - 1) * (int)a.ld + width, 0x00027000);
+  const __amdgpu_buffer_rsrc_t bbuf =
+      __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, (min(b.rows - n0, 16) - 1) * (int)b.ld + width, 0x00027000);
+  const int sw = (r >> 1) & 7, c0 = (g ^ sw) * 16, c1 = ((g + 4) ^ sw) * 16;  // (any columns do, if a and b agree)
   cm_f32x4 acc = {0, 0, 0, 0};
   for (int kb = wave; kb < whole; kb += DW * DU) {
     DirectStep s[DU];
 #pragma unroll
     for (int u = 0; u < DU; u++) {
       const int k = min(kb + u * DW, whole - 1);
-      s[u] = {direct_fragment(ar + k * CB + g * 16), direct_fragment(br + k * CB + g * 16), as[k], bs[k]};
+      direct_copy(abuf, (int)a.ld, arow, chunk, k * CB, (lds_bytes*)&tiles[wave][u][0][0]);
+      direct_copy(bbuf, (int)b.ld, brow, chunk, k * CB, (lds_bytes*)&tiles[wave][u][1][0]);
+      s[u].sa = as[k];
+      s[u].sb = bs[k];
     }
-    __builtin_amdgcn_sched_barrier(0);  // all of them before the first is waited for
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < DU; u++) {
+      const uint8_t *ta = &tiles[wave][u][0][r * CB], *tb = &tiles[wave][u][1][r * CB];
+      const cm_i32x4 a0 = *reinterpret_cast<const cm_i32x4*>(ta + c0), a1 = *reinterpret_cast<const cm_i32x4*>(ta + c1);
+      const cm_i32x4 b0 = *reinterpret_cast<const cm_i32x4*>(tb + c0), b1 = *reinterpret_cast<const cm_i32x4*>(tb + c1);
+      s[u].a = cm_i32x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+      s[u].b = cm_i32x8{b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
       // (past the end the last step was read again: its codes count as zeros, which adds nothing but
       // a NaN that is in the result already)
       if (u > 0) s[u].b &= -(int)(kb + u * DW < whole);
       s[u].add_to<EXACT>(acc);
     }
+    __builtin_amdgcn_s_waitcnt(0);  // the reads are back before the next copies overwrite what they read
+    __builtin_amdgcn_sched_barrier(0);
   }
   if (whole < a.nb && wave == whole % DW) {  // the columns that do not fill a step
     const int k0 = whole * CB + g * 32;
-    const DirectStep s = {row_fragment(ar, k0, a.cols), row_fragment(br, k0, a.cols), as[whole], bs[whole]};
+    const DirectStep s = {row_fragment(a.codes + am * a.ld, k0, a.cols), row_fragment(b.codes + bn * b.ld, k0, a.cols), as[whole], bs[whole]};
     s.add_to<EXACT>(acc);
   }
+  __syncthreads();  // every wave is done with its tiles
+  cm_f32x4* const part = reinterpret_cast<cm_f32x4*>(&tiles[0][0][0][0]);
   if (wave > 0) part[(wave - 1) * 64 + lane] = acc;
   __syncthreads();
   if (wave > 0) return;
@@ -120,8 +142,6 @@ __device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, in
   tm = (int)(8u * g + in % high);
   tn = (int)(in / high);
 }
-
-typedef __attribute__((address_space(3))) uint8_t lds_bytes;
 
 // More rows of a.  Four waves own a tile of TM rows of a and TN rows of b, WM x WN parts of FA x FB
 // blocks of 32 x 32.  K steps of 128 columns go straight from memory into LDS, two steps in
@@ -422,10 +442,10 @@ struct Plan {
 // workgroup `one` alone on a compute unit (bound by the step's own chain of copies, LDS reads and
 // the barrier) and `all` with `occ` of them there; both were measured, for bf16 results and for
 // the exact products of fp32 ones.  What parts cost is their way through memory and a second
-// launch.  Measured, chosen against the next best: 64 x 1880 x 10240 in 32-row tiles and 8 parts
-// 15.6 (4 parts 18.8, one part 46); 320 x 1880 x 10240 in 64-row tiles and 4 parts 25 (128-row,
-// 8 parts 26, one part 69); 1024 x 4672 x 8192 in 128-row tiles 54 (256-row 91); 4096^3 in 256-row
-// tiles 59 (128-row 67).
+// launch.  Measured, chosen against others: 16 x 1880 x 10240 by the kernel of few rows 8.4 (32-row
+// tiles in 8 parts 13.7); 64 x 4672 x 8192 in 32-row tiles and 8 parts 16.9 (128-row, 8 parts 18.4,
+// one part 48); 320 x 1880 x 10240 in 64-row tiles and 8 parts 26 (128-row, one part 69); 1024 x
+// 4672 x 8192 in 128-row tiles 54 (256-row 91); 4096^3 in 256-row tiles 59 (128-row 67).
 Plan choose_plan(int64_t m, int64_t n, int64_t k, bool exact, bool fits) {
   struct Tile {
     int kind, tm, tn, occ;
@@ -440,8 +460,8 @@ Plan choose_plan(int64_t m, int64_t n, int64_t k, bool exact, bool fits) {
   const double out = (double)m * (double)n * (exact ? 4 : 2) * write;
   auto rounds = [](int64_t groups, int64_t slots) { return (double)((groups + slots - 1) / slots); };
   Plan best = {DIRECT, 1, nb};
-  // eight waves take every eighth step each; rows of a that coincide are read once
-  double least = 4.0 + rounds((n + 15) / 16 * ((m + 15) / 16), 256) * (nb / 8.0 + 0.5) * (m <= 4 ? 0.6 : 1.0) + out;
+  // eight waves take every eighth step each
+  double least = 3.0 + rounds((n + 15) / 16 * ((m + 15) / 16), 256) * (nb / 8.0 * 0.55 + 0.6) + out;
   if (!fits) return best;
   for (const Tile& t : tiles) {
     const int64_t count = ((m + t.tm - 1) / t.tm) * ((n + t.tn - 1) / t.tn);
@@ -525,6 +545,8 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
   if (a->rows == 0 || b->rows == 0) return AZ_OK;
   if ((st = dense_check(out, dtype, ld_out, b->rows, who)) != AZ_OK) return st;
   if ((uintptr_t)bias & 3u) return code_fail(AZ_ERR_INVALID_ARG, who, "bias must be 4-byte aligned");
+  // 16 rows in the 32 bits of a buffer's range
+  if (a->ld >= (1 << 27) || b->ld >= (1 << 27)) return code_fail(AZ_ERR_UNSUPPORTED, who, "rows of 2^27 bytes or more");
   const size_t need = az_codes_matmul_workspace(a, b, dtype);
   if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
   if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
