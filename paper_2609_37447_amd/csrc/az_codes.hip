@@ -38,37 +38,38 @@ __device__ __forceinline__ uint32_t finite_size(float x) {
   return a >= INF_BITS ? 0u : a;
 }
 
-// 16 elements of a row from column c on, as fp32; zero at and past cols.
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void load16(const void* x, int64_t at, int c, int cols, float (&v)[16]) {
-  if (VEC && c + 16 <= cols) {
+// 16 elements of a row of `cols` from column c on, as fp32; zero at and past cols.  Memory is read 16
+// bytes at a time at any alignment of the elements; where the row ends before the 16 do, its last
+// 16 are read and moved down, so that no load waits for another.
+template <bool BF16>
+__device__ __forceinline__ void load16(const void* x, int64_t row, int c, int cols, float (&v)[16]) {
+  if (cols >= 16) {
+    const int at = min(c, cols - 16), down = min(c - at, 16);
     if constexpr (BF16) {
-      const cm_i32x4* p = reinterpret_cast<const cm_i32x4*>((const uint16_t*)x + at + c);
+      cm_i32x4 w[2];
+      __builtin_memcpy(w, (const uint16_t*)x + row + at, 32);
 #pragma unroll
-      for (int h = 0; h < 2; h++) {
-        const cm_i32x4 w = p[h];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          v[8 * h + 2 * i] = __uint_as_float((uint32_t)w[i] << 16);
-          v[8 * h + 2 * i + 1] = __uint_as_float((uint32_t)w[i] & 0xffff0000u);
-        }
+      for (int i = 0; i < 8; i++) {
+        v[2 * i] = __uint_as_float((uint32_t)w[i >> 2][i & 3] << 16);
+        v[2 * i + 1] = __uint_as_float((uint32_t)w[i >> 2][i & 3] & 0xffff0000u);
       }
     } else {
-      const cm_f32x4* p = reinterpret_cast<const cm_f32x4*>((const float*)x + at + c);
+      __builtin_memcpy(v, (const float*)x + row + at, 64);
+    }
+    if (down) {
 #pragma unroll
-      for (int h = 0; h < 4; h++) {
-        const cm_f32x4 w = p[h];
+      for (int s = 16; s > 0; s >>= 1)
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[4 * h + i] = w[i];
-      }
+        for (int i = 0; i < 16; i++)
+          if (down & s) v[i] = i + s < 16 ? v[(i + s) & 15] : 0.0f;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 16; i++) {
       v[i] = 0.0f;
       if (c + i < cols) {
-        if constexpr (BF16) v[i] = f32_of_bf16(((const uint16_t*)x)[at + c + i]);
-        else v[i] = ((const float*)x)[at + c + i];
+        if constexpr (BF16) v[i] = f32_of_bf16(((const uint16_t*)x)[row + c + i]);
+        else v[i] = ((const float*)x)[row + c + i];
       }
     }
   }
@@ -76,15 +77,33 @@ __device__ __forceinline__ void load16(const void* x, int64_t at, int c, int col
 
 // Writes the codes of 16 columns from c on, none past cols.
 __device__ __forceinline__ void store16(uint8_t* row, int c, int cols, const cm_i32x4& w) {
-  if (c + 16 <= cols) {
-    *reinterpret_cast<cm_i32x4*>(row + c) = w;
-  } else {
-    for (int i = 0; i < cols - c; i++) row[c + i] = (uint8_t)((uint32_t)w[i >> 2] >> (8 * (i & 3)));
+  uint8_t* to = row + c;
+  const int left = cols - c;
+  if (left >= 16) {
+    *reinterpret_cast<cm_i32x4*>(to) = w;
+  } else if (left > 0) {
+    uint64_t u = (uint32_t)w[0] | (uint64_t)(uint32_t)w[1] << 32;
+    if (left & 8) {
+      *reinterpret_cast<uint64_t*>(to) = u;
+      u = (uint32_t)w[2] | (uint64_t)(uint32_t)w[3] << 32;
+      to += 8;
+    }
+    if (left & 4) {
+      *reinterpret_cast<uint32_t*>(to) = (uint32_t)u;
+      u >>= 32;
+      to += 4;
+    }
+    if (left & 2) {
+      *reinterpret_cast<uint16_t*>(to) = (uint16_t)u;
+      u >>= 16;
+      to += 2;
+    }
+    if (left & 1) *to = (uint8_t)u;
   }
 }
 
 // Rows with a scale of their own: eight lanes take a block of 128, 16 columns each.
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ __launch_bounds__(NT) void az_quantize_rows(const void* __restrict__ x, int64_t ldx, CodeView q) {
   const uint32_t total = (uint32_t)q.rows * (uint32_t)q.nb;
   const uint32_t lane8 = threadIdx.x & 7;
@@ -92,7 +111,7 @@ __global__ __launch_bounds__(NT) void az_quantize_rows(const void* __restrict__ 
     const uint32_t r = id / (uint32_t)q.nb, kb = id - r * (uint32_t)q.nb;
     const int c = (int)(kb * CB + lane8 * 16);
     float v[16];
-    load16<BF16, VEC>(x, (int64_t)r * ldx, c, q.cols, v);
+    load16<BF16>(x, (int64_t)r * ldx, c, q.cols, v);
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 16; i++) a = max(a, finite_size(v[i]));
@@ -108,7 +127,7 @@ __global__ __launch_bounds__(NT) void az_quantize_rows(const void* __restrict__ 
 }
 
 // Tiles of 128 x 128 with one scale, and their transposed copy through LDS.
-template <bool BF16, bool VEC, bool TRANSPOSED>
+template <bool BF16, bool TRANSPOSED>
 __global__ __launch_bounds__(NT) void az_quantize_tiles(const void* __restrict__ x, int64_t ldx, CodeView q, CodeView qt) {
   __shared__ uint32_t most[NT / 64];
   __shared__ uint8_t tile[TRANSPOSED ? CB * (CB + 4) : 4];
@@ -120,10 +139,15 @@ __global__ __launch_bounds__(NT) void az_quantize_tiles(const void* __restrict__
 #pragma unroll
   for (int p = 0; p < 4; p++) {
     const int64_t r = r0 + 32 * p;
-    load16<BF16, VEC>(x, r * ldx, c, r < q.rows ? q.cols : 0, v[p]);
-#pragma unroll
-    for (int i = 0; i < 16; i++) a = max(a, finite_size(v[p][i]));
+    load16<BF16>(x, min(r, (int64_t)q.rows - 1) * ldx, c, q.cols, v[p]);
   }
+#pragma unroll
+  for (int p = 0; p < 4; p++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      if (r0 + 32 * p >= q.rows) v[p][i] = 0.0f;
+      a = max(a, finite_size(v[p][i]));
+    }
   for (int o = 32; o > 0; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o));
   if ((t & 63) == 0) most[t >> 6] = a;
   __syncthreads();
@@ -168,7 +192,7 @@ __global__ __launch_bounds__(NT) void az_quantize_tiles(const void* __restrict__
   }
 }
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ __launch_bounds__(NT) void az_dequantize(CodeView q, void* __restrict__ x, int64_t ldx) {
   const uint32_t total = (uint32_t)q.rows * (uint32_t)q.nb;
   const uint32_t lane8 = threadIdx.x & 7;
@@ -189,15 +213,12 @@ __global__ __launch_bounds__(NT) void az_dequantize(CodeView q, void* __restrict
     const int64_t at = (int64_t)r * ldx + c;
     if constexpr (BF16) {
       uint16_t* o = (uint16_t*)x + at;
-      if (VEC && c + 16 <= q.cols) {
+      if (c + 16 <= q.cols) {
+        cm_i32x4 u[2];
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-          cm_i32x4 u;
-#pragma unroll
-          for (int i = 0; i < 4; i++)
-            u[i] = (int)((uint32_t)bf16_of(v[8 * h + 2 * i]) | ((uint32_t)bf16_of(v[8 * h + 2 * i + 1]) << 16));
-          reinterpret_cast<cm_i32x4*>(o)[h] = u;
-        }
+        for (int i = 0; i < 8; i++)
+          u[i >> 2][i & 3] = (int)((uint32_t)bf16_of(v[2 * i]) | ((uint32_t)bf16_of(v[2 * i + 1]) << 16));
+        __builtin_memcpy(o, u, 32);
       } else {
 #pragma unroll
         for (int i = 0; i < 16; i++)
@@ -205,9 +226,8 @@ __global__ __launch_bounds__(NT) void az_dequantize(CodeView q, void* __restrict
       }
     } else {
       float* o = (float*)x + at;
-      if (VEC && c + 16 <= q.cols) {
-#pragma unroll
-        for (int h = 0; h < 4; h++) reinterpret_cast<cm_f32x4*>(o)[h] = cm_f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      if (c + 16 <= q.cols) {
+        __builtin_memcpy(o, v, 64);
       } else {
 #pragma unroll
         for (int i = 0; i < 16; i++)
@@ -223,16 +243,16 @@ int pass_grid(const CodeView& q) {
   return (int)(groups < 65536 ? groups : 65536);
 }
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 int launch_quantize(const void* x, int64_t ldx, const CodeView& q, const CodeView* qt, hipStream_t s) {
   if (q.shift == 0) {
-    hipLaunchKernelGGL((az_quantize_rows<BF16, VEC>), dim3(pass_grid(q)), dim3(NT), 0, s, x, ldx, q);
+    hipLaunchKernelGGL((az_quantize_rows<BF16>), dim3(pass_grid(q)), dim3(NT), 0, s, x, ldx, q);
     return AZ_OK;
   }
   const int64_t tiles = (int64_t)((q.rows + CB - 1) / CB) * q.nb;
   if (!grid_fits(tiles, NT)) return AZ_ERR_UNSUPPORTED;
-  if (qt) hipLaunchKernelGGL((az_quantize_tiles<BF16, VEC, true>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, *qt);
-  else hipLaunchKernelGGL((az_quantize_tiles<BF16, VEC, false>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, q);
+  if (qt) hipLaunchKernelGGL((az_quantize_tiles<BF16, true>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, *qt);
+  else hipLaunchKernelGGL((az_quantize_tiles<BF16, false>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, q);
   return AZ_OK;
 }
 
@@ -259,8 +279,7 @@ extern "C" int az_codes_quantize(const void* x, int32_t dtype, int64_t ldx, cons
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   const CodeView* t = qt ? &vt : nullptr;
-  if (dtype == AZ_BF16) st = rows_aligned16(x, ldx, 2) ? launch_quantize<true, true>(x, ldx, v, t, s) : launch_quantize<true, false>(x, ldx, v, t, s);
-  else st = rows_aligned16(x, ldx, 4) ? launch_quantize<false, true>(x, ldx, v, t, s) : launch_quantize<false, false>(x, ldx, v, t, s);
+  st = dtype == AZ_BF16 ? launch_quantize<true>(x, ldx, v, t, s) : launch_quantize<false>(x, ldx, v, t, s);
   return launched(who, st);
 }
 
@@ -274,12 +293,7 @@ extern "C" int az_codes_dequantize(const az_code_matrix* q, void* x, int32_t dty
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 g(pass_grid(v)), b(NT);
   (void)hipGetLastError();
-  if (dtype == AZ_BF16) {
-    if (rows_aligned16(x, ldx, 2)) hipLaunchKernelGGL((az_dequantize<true, true>), g, b, 0, s, v, x, ldx);
-    else hipLaunchKernelGGL((az_dequantize<true, false>), g, b, 0, s, v, x, ldx);
-  } else {
-    if (rows_aligned16(x, ldx, 4)) hipLaunchKernelGGL((az_dequantize<false, true>), g, b, 0, s, v, x, ldx);
-    else hipLaunchKernelGGL((az_dequantize<false, false>), g, b, 0, s, v, x, ldx);
-  }
+  if (dtype == AZ_BF16) hipLaunchKernelGGL((az_dequantize<true>), g, b, 0, s, v, x, ldx);
+  else hipLaunchKernelGGL((az_dequantize<false>), g, b, 0, s, v, x, ldx);
   return launch_status(who);
 }
