@@ -396,9 +396,9 @@ class CodeMatrix:
         if scale_rows not in (1, AZ_CODE_BLOCK):
             raise ValueError("scale_rows is 1 or 128")
         if rows <= 1:
-            ld = -(-ld // 16) * 16  # one row: only its whole 16-byte chunks have to be there
-            if rows == 1 and codes.untyped_storage().nbytes() - codes.storage_offset() < -(-cols // 16) * 16:
-                raise ValueError("codes needs whole chunks of 16 bytes")
+            ld = -(-ld // 16) * 16
+        if rows and codes.untyped_storage().nbytes() - codes.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
+            raise ValueError("codes must hold whole chunks of 16 bytes in every row")
         want = (-(-rows // scale_rows), -(-cols // AZ_CODE_BLOCK))
         if not scales.is_cuda or scales.dtype != torch.uint8 or tuple(scales.shape) != want or not scales.is_contiguous():
             raise ValueError(f"scales must be a contiguous uint8 device tensor {list(want)}")

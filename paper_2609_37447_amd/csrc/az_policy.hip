@@ -288,10 +288,18 @@ int policy_threads(int64_t rows, int64_t vocab) {
 }
 
 template <int MODE>
-void launch(const PolicyView& p, int rows, int nt, hipStream_t s) {
+int launch(const PolicyView& p, int rows, int nt, hipStream_t s) {
   const dim3 g((unsigned)((p.vocab + nt * PER - 1) / (nt * PER)), (unsigned)(rows < 65535 ? rows : 65535), (unsigned)((rows + 65534) / 65535));
-  if (p.history) hipLaunchKernelGGL((az_policy_kernel<MODE, true>), g, dim3(nt), nt * PER * sizeof(uint32_t), s, p, rows);
-  else hipLaunchKernelGGL((az_policy_kernel<MODE, false>), g, dim3(nt), 0, s, p, rows);
+  if (p.history) {
+    const int lds = nt * PER * (int)sizeof(uint32_t);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(az_policy_kernel<MODE, true>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return launched("az_logits_policy", AZ_ERR_DEVICE);
+    hipLaunchKernelGGL((az_policy_kernel<MODE, true>), g, dim3(nt), lds, s, p, rows);
+  } else {
+    hipLaunchKernelGGL((az_policy_kernel<MODE, false>), g, dim3(nt), 0, s, p, rows);
+  }
+  return launched("az_logits_policy", AZ_OK);
 }
 
 }  // namespace
@@ -338,14 +346,8 @@ extern "C" int az_logits_policy(const az_logits* in, int32_t probabilities, floa
                         in->vocab, in->max_history, in->dtype == AZ_BF16, in->mask_kind};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (!probabilities) {
-    launch<ADJUST>(p, in->rows, nt, s);
-  } else if (in->vocab <= MOST) {
-    launch<WHOLE>(p, in->rows, nt, s);
-  } else {
-    launch<STATS>(p, in->rows, nt, s);
-    if ((st = launch_status(who)) != AZ_OK) return st;
-    launch<WRITE>(p, in->rows, nt, s);
-  }
-  return launch_status(who);
+  if (!probabilities) return launch<ADJUST>(p, in->rows, nt, s);
+  if (in->vocab <= MOST) return launch<WHOLE>(p, in->rows, nt, s);
+  if ((st = launch<STATS>(p, in->rows, nt, s)) != AZ_OK) return st;
+  return launch<WRITE>(p, in->rows, nt, s);
 }

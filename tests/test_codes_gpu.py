@@ -450,6 +450,17 @@ def test_tensor_checks():
                                torch.empty((30, 50), device="cuda"))
     with pytest.raises(ValueError):
         az.CodeMatrix(torch.zeros((4, 32), dtype=torch.uint8, device="cuda"), torch.zeros((4, 2), dtype=torch.uint8, device="cuda"))
+    # the last row's chunks have to be there as well
+    scales = torch.zeros((4, 1), dtype=torch.uint8, device="cuda")
+    short = torch.zeros((3 * 32 + 20,), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        az.CodeMatrix(short.as_strided((4, 20), (32, 1)), scales)
+    with pytest.raises(ValueError):
+        az.CodeMatrix(short[:20].clone().view(1, 20), scales[:1])
+    az.CodeMatrix(torch.zeros((4, 32), dtype=torch.uint8, device="cuda")[:, :20], scales)
+    with pytest.raises(az.AzError):  # rows that are not 16-byte chunks apart
+        az.dequantize_tensors(az.CodeMatrix(torch.zeros((4, 20), dtype=torch.uint8, device="cuda").as_strided((3, 4), (20, 1)), scales[:3]),
+                              torch.zeros((3, 4), device="cuda"))
 
 
 # --------------------------------------------------------------------------- #
