@@ -424,6 +424,8 @@ def _on(device, stream, *others):
     for t in others:
         if t is not None and t.device != device:
             raise ValueError("the operands are on different devices")
+    if stream is not None and stream.device != device:
+        raise ValueError("the stream is another device's")
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 

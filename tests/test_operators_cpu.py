@@ -130,6 +130,18 @@ def test_bad_logits_are_refused():
     assert b"az_logits_policy" in L.az_last_error()
 
 
+def test_streams_and_operands_of_other_devices_are_refused():
+    import torch
+    from types import SimpleNamespace as N
+    from paper_2609_37447_amd import _binding as B
+    d0, d1 = torch.device("cuda", 0), torch.device("cuda", 1)
+    assert B._on(d0, N(device=d0, cuda_stream=7), None, N(device=d0)) == 7
+    with pytest.raises(ValueError, match="stream"):
+        B._on(d0, N(device=d1, cuda_stream=7))
+    with pytest.raises(ValueError, match="operands"):
+        B._on(d0, N(device=d0, cuda_stream=7), N(device=d1))
+
+
 def test_struct_layouts():
     assert ctypes.sizeof(az.az_code_matrix) == 48
     assert ctypes.sizeof(az.az_logits) == 112
