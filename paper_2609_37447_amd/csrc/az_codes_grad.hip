@@ -191,7 +191,8 @@ struct Grad {
 
 // Blocks 0..bias-1 sum dy's columns; the others own a tile of dw each.  Both take the rows
 // part * part_rows on, part = blockIdx.y; sums over one of several parts go to a workspace, dw's at
-// part * part_stride and db's at part * n.
+// part * part_stride and db's at part * n.  16384 x 4096 x 4096: 463-490 us (1,120-1,190 TFLOP/s, power);
+// 1024 x 1880 x 10240: 59 us, of which 77 MB of results take 17 at a copy's rate.
 template <int W, bool F32, int FEED>
 __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint16_t* __restrict__ dy, int64_t ldy, int n, CodeView x,
                                                                      void* __restrict__ dw, int64_t ldw, float* __restrict__ db,

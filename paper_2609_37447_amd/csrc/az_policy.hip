@@ -8,6 +8,10 @@
 // and sum in the workspace, a second one joins them and reads the logits again, which the
 // caches still hold, to write the result.  What has been chosen before is counted in LDS, a
 // counter for each entry of the chunk, so that penalties cost no search.
+//
+// 4,096 rows of 4,672 fp32 logits and bits: 31 us, 5.1 TB/s.  512 rows of 131,072 bf16 logits and bits:
+// 108 us, 136 with 2,048 past entries a row (81 at a copy's rate if the logits were read once).  One workgroup of 1,024 threads that keeps such a row in its registers reads it once,
+// but leaves a compute unit nothing else to do between its barriers: 135 us, 146 with past entries.
 #include <math.h>
 
 #include "az_codes_common.h"
@@ -277,7 +281,7 @@ __global__ __launch_bounds__(THREADS) void az_policy_kernel(PolicyView p, int ro
 }
 
 // Threads of a workgroup: enough for the row, up to 1,024.  Rows that need several
-// workgroups get 512 (512 rows of 131,072: 174 us, 185 with 1,024), or 256 where that takes to fill the chip.
+// workgroups get 512 (512 rows of 131,072: 136 us, 149 with 1,024), or 256 where that takes to fill the chip.
 int policy_threads(int64_t rows, int64_t vocab) {
   int nt = 256;
   if (vocab <= MOST) {
