@@ -215,9 +215,11 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   const uint32_t yoff = (uint32_t)yr * (uint32_t)ldy * 2u + (uint32_t)yc * 16u;
   lds_bytes* const ylds = (lds_bytes*)smem + G::YROWS * wave * G::ROW;
   auto copy_y = [&](int m, int stage) {
-    // (past the last row: nothing is in range, and zeros are read)
+    // (past the last row: nothing is in range, and zeros are read.  The range is checked by whole words, of
+    // which the row's last holds one element where n is odd: the range ends behind that word, which lies in
+    // the row's last aligned 16 bytes.)
     const int rows = min(me - m, MS), first = min(m, me - 1);
-    const uint32_t bytes = (((uint32_t)max(rows, 1) - 1u) * (uint32_t)ldy + (uint32_t)(n - n0)) * 2u;
+    const uint32_t bytes = (((uint32_t)max(rows, 1) - 1u) * (uint32_t)ldy + (((uint32_t)(n - n0) + 1u) & ~1u)) * 2u;
     const __amdgpu_buffer_rsrc_t buf =
         __builtin_amdgcn_make_buffer_rsrc((void*)(dy + first * ldy + n0), 0, (int)(bytes & (uint32_t)-(int)(rows > 0)), 0x00027000);
     G::copy(buf, ylds + stage, yoff, 4 * G::YROWS * (int)ldy * 2);
