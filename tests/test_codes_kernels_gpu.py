@@ -135,3 +135,134 @@ def test_weight_grad_is_exact_on_whole_numbers(shape, cut, out, feed, add, pad, 
         f32 = str(out == "f32" or cut[1] > 1).lower()
         assert [(r[0], r[1][1]) for r in ran[:1]] == [(f"az_weight_grad<{cut[0]},{f32},{kind}>", cut[1])]
         assert [r[0] for r in ran[1:]] == ([f"az_join_parts<{str(out == 'f32').lower()}>"] if cut[1] > 1 else [])
+
+
+# --------------------------------------------------------------------------- #
+# The product
+# --------------------------------------------------------------------------- #
+TILES = {32: "1,1,1,4", 64: "1,2,2,2", 128: "2,2,2,2", 256: "4,4,2,2"}
+# rows of a, of b, columns, and what runs them for bf16 and fp32 results: (rows of a tile, parts of the
+# columns); 16 is the kernel of few rows
+PRODUCTS = [((17, 300, 650), (16, 1), (16, 1)), ((1001, 1003, 1111), (32, 1), (32, 1)), ((65, 4101, 3001), (32, 4), (32, 4)),
+            ((33, 4101, 5003), (32, 8), (32, 8)), ((2051, 2051, 333), (64, 1), (64, 1)), ((33, 3301, 8205), (64, 8), (64, 8)),
+            ((320, 1879, 10230), (64, 8), (32, 4)), ((1501, 2051, 333), (128, 1), (128, 1)), ((1027, 257, 5003), (128, 8), (128, 8)),
+            ((4101, 257, 5003), (128, 4), (128, 2)), ((65, 3301, 4101), (128, 7), (32, 7)), ((2051, 4101, 1111), (256, 1), (256, 1)),
+            ((1739, 1675, 27553), (256, 4), (256, 4))]
+
+
+@pytest.mark.parametrize("shape,bf16,f32", PRODUCTS)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("sa,sb,pad,bias", [(1, 128, 0, True), (1, 1, 3, False), (128, 1, 1, True)])
+def test_matmul_is_exact_on_whole_numbers(shape, bf16, f32, out, sa, sb, pad, bias):
+    az, torch = _az()
+    m, n, k = shape
+    g = _generator(m, n, k, pad)
+    x, w = _whole(g, m, k), _whole(g, n, k)
+    a, b = _coded(x, sa, 16 * pad, pad), _coded(w, sb, 16 * (pad % 2), (pad + 1) % 4)
+    bs = _whole(g, 1, n)[0].contiguous() if bias else None
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    o, whole = _rows(m, n, dt, n + pad, pad)
+    o.fill_(float("nan"))
+    ws = torch.full((max(az.az_codes_matmul_workspace(a.c, b.c, az.AZ_F32 if out == "f32" else az.AZ_BF16), 16),), 0xFF,
+                    dtype=torch.uint8, device="cuda")
+    ran = _launched(lambda: az.matmul_tensors(a, b, o, bias=bs, workspace=ws))
+    want = _dot(x, w)
+    if bias:
+        want += bs.double()
+    assert torch.equal(o, want.float().to(dt))
+    o.fill_(7.0)
+    assert bool((whole == 7.0).all())
+    tile, parts = f32 if out == "f32" else bf16
+    exact = str(out == "f32").lower()
+    if tile == 16:
+        assert [r[0] for r in ran] == [f"az_matmul_direct<{exact}>"]
+    else:
+        sums = "true" if parts > 1 else exact
+        assert [(r[0], r[1][1]) for r in ran[:1]] == [(f"az_matmul_tiled<{TILES[tile]},{exact},{sums}>", parts)]
+        assert [r[0] for r in ran[1:]] == ([f"az_join_products<{exact}>"] if parts > 1 else [])
+
+
+@pytest.mark.parametrize("shape,bf16,f32", PRODUCTS)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_matmul_of_any_numbers(shape, bf16, f32, out):
+    """Normal numbers with a scale each row and block, by the 2-norm: fp32 sums of K terms in a random walk are
+    off by at most sqrt(K) 2^-24 <= 1e-5 of it; a bf16 rounding by at most 2^-8.  And a second call gives the same bits."""
+    az, torch = _az()
+    m, n, k = shape
+    g = _generator(m, n, k, 9)
+    both = []
+    for rows in (m, n):
+        x = torch.randn((rows, k), generator=g, device="cuda")
+        x *= torch.exp2(torch.randint(-6, 7, (rows, 1), generator=g, device="cuda").float())
+        q = _coded(x)
+        az.dequantize_tensors(q, x)  # (exact: every code and scale is tested)
+        both.append((q, x))
+    (a, x), (b, w) = both
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    o, again = torch.empty((m, n), dtype=dt, device="cuda"), torch.empty((m, n), dtype=dt, device="cuda")
+    az.matmul_tensors(a, b, o)
+    az.matmul_tensors(a, b, again)
+    assert torch.equal(o.view(torch.uint8), again.view(torch.uint8))
+    want = _dot(x, w)
+    off = o.double() - want
+    for d in (0, 1):  # a row or column that is wrong shows by itself
+        rel = off.norm(dim=d) / want.norm(dim=d)
+        assert float(rel.max()) <= (2.0 ** -8 if out == "bf16" else 1e-5), (d, float(rel.max()))
+
+
+@pytest.mark.parametrize("shape,bf16,f32", PRODUCTS)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_matmul_nan_stays_in_its_row_and_column_of_every_kernel(shape, bf16, f32, out):
+    az, torch = _az()
+    m, n, k = shape
+    g = _generator(m, n, k, 10)
+    a, b = _coded(_whole(g, m, k)), _coded(_whole(g, n, k))
+    a.codes[m - 2, k - 1] = 0x7F   # in the last step
+    a.codes[3, 0] = 0xFF           # and in the first
+    b.scales[n - 3, -1] = 255
+    b.scales[11, 0] = 255
+    o = torch.zeros((m, n), dtype=torch.float32 if out == "f32" else torch.bfloat16, device="cuda")
+    az.matmul_tensors(a, b, o)
+    want = torch.zeros((m, n), dtype=torch.bool, device="cuda")
+    want[[3, m - 2]] = True
+    want[:, [11, n - 3]] = True
+    assert torch.equal(torch.isnan(o), want)
+
+
+@pytest.mark.parametrize("m,n,k", [(64, 1880, 10240), (1024, 4672, 520), (2050, 1030, 4101)])
+def test_the_inputs_gradient_by_the_transposed_weights(m, n, k):
+    """dx = dy W, the transposed codes of W as the second operand."""
+    az, torch = _az()
+    g = _generator(m, n, k, 11)
+    dy, w = _whole(g, m, n), _whole(g, n, k)
+    wq, wt = az.CodeMatrix.empty(n, k, 128), az.CodeMatrix.empty(k, n, 128)
+    az.quantize_tensors(w, wq, wt)
+    dx = torch.empty((m, k), device="cuda")
+    az.matmul_tensors(_coded(dy), wt, dx)
+    assert torch.equal(dx, _dot(dy, w.t().contiguous()).float())
+
+
+# --------------------------------------------------------------------------- #
+# Offsets past 32 bits
+# --------------------------------------------------------------------------- #
+def test_products_past_32_bits_are_exact():
+    """4.7 GB of codes whose last rows are whole numbers, as the weights and as the activations."""
+    az, torch = _az()
+    rows, cols = 36000, 131072
+    g = _generator(12)
+    q = az.CodeMatrix(torch.zeros((rows, cols), dtype=torch.uint8, device="cuda"),
+                      torch.full((rows, cols // 128), 127, dtype=torch.uint8, device="cuda"))
+    x = torch.randint(-1, 2, (300, cols), generator=g, device="cuda").float()
+    tail = az.CodeMatrix(q.codes[-300:], q.scales[-300:])
+    az.quantize_tensors(x, tail)
+    for m in (2, 40, 200, 700):  # sums of 131,072 products of at most 9
+        y = torch.randint(-3, 4, (m, cols), generator=g, device="cuda").float()
+        a = _coded(y)
+        want = _dot(y, x)
+        for dt in (torch.float32, torch.bfloat16):
+            out = torch.full((m, rows), float("nan"), dtype=dt, device="cuda")
+            az.matmul_tensors(a, q, out)
+            assert torch.equal(out[:, -300:], want.float().to(dt)) and bool((out[:, :-300] == 0).all()), (m, dt)
+            out = torch.full((rows, m), float("nan"), dtype=dt, device="cuda")
+            az.matmul_tensors(q, a, out)
+            assert torch.equal(out[-300:], want.t().float().to(dt)) and bool((out[:-300] == 0).all()), (m, dt)

@@ -1,0 +1,22 @@
+"""Long rows whose chunks are 512 threads wide, with past entries (tests/test_policy_gpu.py has those of 256)."""
+
+import pytest
+
+from .test_policy_gpu import Case
+
+pytestmark = pytest.mark.gpu
+
+
+# rows * chunks of 8,192 entries >= 512
+@pytest.mark.parametrize("rows,vocab", [(171, 20000), (40, 131072), (260, 16385)])
+@pytest.mark.parametrize("mask,hist,bias,dtype", [("bits", 2048, "shared", "bf16"), ("bytes", 1, "none", "f32"), ("none", 600, "rows", "bf16"),
+                                                  ("bytes", 0, "rows", "f32")])
+@pytest.mark.parametrize("probs", [True, False])
+def test_policy_of_wide_chunks(rows, vocab, mask, hist, bias, dtype, probs):
+    Case(rows, vocab, dtype, mask, hist, bias, seed=11).check(probs)
+
+
+@pytest.mark.parametrize("pad,offset", [(1, 0), (5, 3)])
+def test_policy_of_wide_chunks_at_any_alignment(pad, offset):
+    Case(172, 20001, "bf16", "bits", 300, "rows", seed=12).check(pad=pad, offset=offset)
+    Case(172, 20001, "f32", "bytes", 300, "shared", seed=13).check(inplace=True)
