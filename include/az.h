@@ -427,8 +427,9 @@ typedef struct {
  *   qt  NULL, or (scale_rows 128 in both) a second matrix [q->cols][q->rows] that
  *       receives the transposed codes and scales: the operand of the input's
  *       gradient, dx = dy W = az_codes_matmul(dy, Wt).
- * Returns AZ_OK, AZ_ERR_INVALID_ARG, AZ_ERR_UNSUPPORTED (sizes past the limits) or
- * AZ_ERR_DEVICE.  No rows: AZ_OK, nothing is launched. */
+ * Returns AZ_OK, AZ_ERR_INVALID_ARG, AZ_ERR_UNSUPPORTED (sizes past the limits, or more
+ * tiles than the 2^32 - 1 threads of one launch cover) or AZ_ERR_DEVICE.  No rows: AZ_OK,
+ * nothing is launched. */
 int az_codes_quantize(const void* x, int32_t dtype, int64_t ldx, const az_code_matrix* q,
                       const az_code_matrix* qt, void* stream);
 

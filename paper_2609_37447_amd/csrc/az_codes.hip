@@ -252,7 +252,7 @@ int launch_quantize(const void* x, int64_t ldx, const CodeView& q, const CodeVie
     hipLaunchKernelGGL((az_quantize_rows<BF16>), dim3(pass_grid(q)), dim3(NT), 0, s, x, ldx, q);
     return AZ_OK;
   }
-  const int64_t tiles = (int64_t)((q.rows + CB - 1) / CB) * q.nb;
+  const int64_t tiles = ((int64_t)q.rows + CB - 1) / CB * q.nb;
   if (!grid_fits(tiles, NT)) return AZ_ERR_UNSUPPORTED;
   if (qt) hipLaunchKernelGGL((az_quantize_tiles<BF16, true>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, *qt);
   else hipLaunchKernelGGL((az_quantize_tiles<BF16, false>), dim3((unsigned)tiles), dim3(NT), 0, s, x, ldx, q, q);

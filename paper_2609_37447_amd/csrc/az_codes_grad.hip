@@ -208,7 +208,11 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t kt = (uint32_t)(x.cols + G::T - 1) / G::T, id = blockIdx.x - bias;
   const int n0 = (int)(id / kt) * G::T, k0 = (int)(id % kt) * G::T;
-  const int mb = (int)blockIdx.y * part_rows, me = min(mb + part_rows, x.rows);
+  // From here on rows are counted within the part (at most 2^30 of them, so that steps past its end are counted in 32 bits as well).
+  const int from = (int)blockIdx.y * part_rows, me = min(part_rows, x.rows - from);
+  dy += from * ldy;
+  x.codes += from * x.ld;
+  x.scales += (int64_t)from * x.nb;
 
   // dy, copied: a wave fills YROWS rows at a time, a lane one chunk.
   const int yr = G::YROWS * wave + lane / (G::T / 8), yp = lane % (G::T / 8), yc = yp ^ ((yr & 3) << 2);
@@ -297,29 +301,29 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
     for (int j = 0; j < W; j++) acc[i][j] = cm_f32x16{};
 
   typename G::Frag f0, f1;
-  load_x(mb);
+  load_x(0);
   if constexpr (FEED == COPY) {
-    copy_y(mb, 0);
+    copy_y(0, 0);
   } else {
-    load_y(mb);
-    store_y(mb, 0);
-    load_y(mb + MS);
+    load_y(0);
+    store_y(0, 0);
+    load_y(MS);
   }
   store_x(0);
-  load_x(mb + MS);
+  load_x(MS);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if constexpr (FEED == COPY) {
-    copy_y(mb + MS, G::STAGE);
+    copy_y(MS, G::STAGE);
   } else {
-    store_y(mb + MS, G::STAGE);
-    load_y(mb + 2 * MS);
+    store_y(MS, G::STAGE);
+    load_y(2 * MS);
   }
   store_x(G::STAGE);
-  load_x(mb + 2 * MS);
+  load_x(2 * MS);
   G::read(f0, smem, yo, xo, 0);
   uint32_t stage = 0;
-  for (int m = mb; m < me; m += MS, stage ^= G::STAGE) {
+  for (int m = 0; m < me; m += MS, stage ^= G::STAGE) {
     G::read(f1, smem, yo, xo, stage + 32 * G::ROW);
     G::multiply(acc, f0);
     G::template interleave<2>();
@@ -413,6 +417,7 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
     const int64_t t = 64 * w, tiles = ((n + t - 1) / t) * ((cols + t - 1) / t);
     for (int64_t parts = 1; parts <= 64 && (parts == 1 || 2 * parts <= steps); parts *= 2) {
       const int64_t per = (steps + parts - 1) / parts, groups = tiles * parts, slots = w == 4 ? 256 : 512;
+      if (per * MS > 1 << 30) continue;  // (a part's rows are counted in 32 bits)
       const double step = w == 4 ? (groups <= 128 ? 1.48 : 1.86) : (groups <= 256 ? 0.72 : 1.0);
       double cost = (double)((groups + slots - 1) / slots) * ((double)per * step + 3.0) + outputs * 4 * write;
       if (parts > 1) cost += 3.5 + (double)parts * outputs * 8 * write;
@@ -430,12 +435,12 @@ int launch(const uint16_t* dy, int64_t ldy, int n, const CodeView& x, void* dw, 
            int64_t part_stride, hipStream_t s) {
   using G = Grad<W>;
   constexpr int LDS = 2 * G::STAGE;
+  const int bias = db ? (int)(((int64_t)n + 63) / 64) : 0;
+  const int64_t groups = bias + ((int64_t)n + G::T - 1) / G::T * ((x.cols + G::T - 1) / G::T);
+  if (!grid_fits(groups, NT)) return AZ_ERR_UNSUPPORTED;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(az_weight_grad<W, F32, FEED>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (e != hipSuccess) return AZ_ERR_DEVICE;
-  const int bias = db ? (n + 63) / 64 : 0;
-  const int64_t groups = bias + (int64_t)((n + G::T - 1) / G::T) * ((x.cols + G::T - 1) / G::T);
-  if (!grid_fits(groups, NT)) return AZ_ERR_UNSUPPORTED;
   hipLaunchKernelGGL((az_weight_grad<W, F32, FEED>), dim3((unsigned)groups, (unsigned)cut.parts), dim3(NT), LDS, s, dy, ldy, n, x,
                      dw, ldw, db, bias, add, cut.part_rows, part_stride);
   return AZ_OK;

@@ -494,23 +494,22 @@ struct Operands {
 
 template <bool EXACT>
 int launch_direct(const Operands& o) {
-  const int nt = (o.b.rows + 15) / 16;
-  const int64_t groups = (int64_t)nt * ((o.a.rows + 15) / 16);
+  const int64_t nt = ((int64_t)o.b.rows + 15) / 16, groups = nt * (((int64_t)o.a.rows + 15) / 16);
   if (!grid_fits(groups, DW * 64)) return AZ_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((az_matmul_direct<EXACT>), dim3((unsigned)groups), dim3(DW * 64), 0, o.stream, o.a, o.b, o.bias, o.out, o.ldo, nt);
+  hipLaunchKernelGGL((az_matmul_direct<EXACT>), dim3((unsigned)groups), dim3(DW * 64), 0, o.stream, o.a, o.b, o.bias, o.out, o.ldo, (int)nt);
   return AZ_OK;
 }
 
 template <int FA, int FB, int WM, int WN, bool EXACT, bool F32>
 int launch_tiled(const Plan& p, const Operands& o) {
   using K = Tiled<FA, FB, WM, WN, EXACT>;
+  const int64_t mt = ((int64_t)o.a.rows + K::TM - 1) / K::TM, nt = ((int64_t)o.b.rows + K::TN - 1) / K::TN;
+  if (!grid_fits(mt * nt, 256)) return AZ_ERR_UNSUPPORTED;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS);
   if (e != hipSuccess) return AZ_ERR_DEVICE;
-  const int mt = (o.a.rows + K::TM - 1) / K::TM, nt = (o.b.rows + K::TN - 1) / K::TN;
-  if (!grid_fits((int64_t)mt * nt, 256)) return AZ_ERR_UNSUPPORTED;
   hipLaunchKernelGGL((az_matmul_tiled<FA, FB, WM, WN, EXACT, F32>), dim3((unsigned)(mt * nt), p.parts), dim3(256), K::LDS, o.stream,
-                     o.a, o.b, o.bias, o.out, o.ldo, mt, nt, p.part_steps, o.part_stride);
+                     o.a, o.b, o.bias, o.out, o.ldo, (int)mt, (int)nt, p.part_steps, o.part_stride);
   return AZ_OK;
 }
 

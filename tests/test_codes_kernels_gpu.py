@@ -266,3 +266,39 @@ def test_products_past_32_bits_are_exact():
             out = torch.full((rows, m), float("nan"), dtype=dt, device="cuda")
             az.matmul_tensors(q, a, out)
             assert torch.equal(out[-300:], want.t().float().to(dt)) and bool((out[:-300] == 0).all()), (m, dt)
+
+
+# the largest number of rows, and 64 parts whose ends pass 2^31; 34 GB of codes
+@pytest.mark.parametrize("rows", [2 ** 31 - 1, 2 ** 31 - 3001])
+@pytest.mark.parametrize("n", [8, 3])
+def test_weight_grad_of_the_most_rows(rows, n):
+    az, torch = _az()
+    cols, some = 16, 70001
+    g = _generator(rows & 0xffff, n)
+    q = az.CodeMatrix(torch.zeros((rows, cols), dtype=torch.uint8, device="cuda"), torch.full((rows, 1), 127, dtype=torch.uint8, device="cuda"))
+    dy = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda")
+    want, wb = torch.zeros((n, cols), dtype=torch.float64, device="cuda"), torch.zeros((n,), dtype=torch.float64, device="cuda")
+    # whole numbers at the beginning, over the middle and at the end of the rows, zeros elsewhere
+    for at in (0, rows // 2 - some, rows - some):
+        x, y = torch.randint(-3, 4, (some, cols), generator=g, device="cuda").float(), torch.randint(-3, 4, (some, n), generator=g, device="cuda")
+        az.quantize_tensors(x, az.CodeMatrix(q.codes[at:at + some], q.scales[at:at + some]))
+        dy[at:at + some] = y
+        want += torch.mm(y.double().t().contiguous(), x.double())
+        wb += y.double().sum(dim=0)
+    dw, db = torch.full((n, cols), float("nan"), device="cuda"), torch.full((n,), float("nan"), device="cuda")
+    az.weight_grad_tensors(dy, q, dw, db=db)
+    assert torch.equal(dw, want.float()) and torch.equal(db, wb.float())
+
+
+def test_quantize_and_restore_of_the_most_rows():
+    az, torch = _az()
+    rows, some = 2 ** 31 - 1, 5000
+    g = _generator(13)
+    x = torch.zeros((rows, 1), device="cuda")
+    last = torch.randint(-3, 4, (some, 1), generator=g, device="cuda").float()
+    x[-some:] = last
+    q = az.CodeMatrix.empty(rows, 1)
+    az.quantize_tensors(x, q)
+    x.fill_(float("nan"))
+    az.dequantize_tensors(q, x)
+    assert torch.equal(x[-some:], last) and float(x.abs().sum(dtype=torch.float64)) == float(last.abs().sum())

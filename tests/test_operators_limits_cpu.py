@@ -3,7 +3,7 @@ they touch a device."""
 
 import paper_2609_37447_amd as az
 
-from .test_operators_cpu import E, M, P
+from .test_operators_cpu import E, U, M, P
 
 
 def test_a_workspace_a_byte_too_small_is_refused():
@@ -25,3 +25,14 @@ def test_a_workspace_a_byte_too_small_is_refused():
     l = az.az_logits(P, az.AZ_F32, 1, 1 << 17, 1 << 17)
     assert L.az_logits_policy(l, 1, P, 1 << 17, P, need - 1, None) == E
     assert L.az_logits_policy(l, 1, P, 1 << 17, None, need, None) == E
+
+
+def test_more_tiles_than_a_launch_has_are_refused():
+    # the largest sizes that matrices may have: 2^24 tiles of 256 threads, one launch's limit and one more
+    L, top = az.lib(), 2 ** 31 - 1
+    assert L.az_codes_quantize(P, az.AZ_F32, 1, M(rows=top, cols=1, ld=16, scale_rows=128), None, None) == U
+    for dtype in (az.AZ_F32, az.AZ_BF16):
+        assert L.az_codes_matmul(M(rows=1, cols=16, ld=16), M(rows=top, cols=16, ld=16), None, P, dtype, top, P, 1 << 40, None) == U
+    assert az.az_codes_weight_grad_workspace(1, top, 16) == 0
+    assert L.az_codes_weight_grad(P, 1 << 31, top, M(rows=1, cols=16, ld=16), P, az.AZ_F32, 16, P, 0, None, 0, None) == U
+    assert b"launch" in L.az_last_error()
