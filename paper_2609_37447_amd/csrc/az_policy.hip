@@ -215,7 +215,7 @@ __global__ __launch_bounds__(THREADS) void az_policy_kernel(PolicyView p, int ro
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; i++) add(e[i]);
-    for (int i = t + AHEAD * nt; i < n; i += nt) add(past[i]);
+    for (uint32_t i = t + AHEAD * nt; i < (uint32_t)n; i += nt) add(past[i]);  // (n may be 2^31 - 1)
     __syncthreads();
   }
 #pragma unroll

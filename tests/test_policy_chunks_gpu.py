@@ -20,3 +20,20 @@ def test_policy_of_wide_chunks(rows, vocab, mask, hist, bias, dtype, probs):
 def test_policy_of_wide_chunks_at_any_alignment(pad, offset):
     Case(172, 20001, "bf16", "bits", 300, "rows", seed=12).check(pad=pad, offset=offset)
     Case(172, 20001, "f32", "bytes", 300, "shared", seed=13).check(inplace=True)
+
+
+def test_the_longest_history():
+    """2^31 - 1 past entries, of which the first and the last few are in the vocabulary."""
+    import torch
+
+    import paper_2609_37447_amd as az
+    v, n = 16384, 2 ** 31 - 1
+    h = torch.full((1, n), -1, dtype=torch.int32, device="cuda")
+    h[0, :3] = 5
+    h[0, -2000:] = 7
+    h[0, -1] = v - 1
+    x, out = torch.zeros((1, v), device="cuda"), torch.empty((1, v), device="cuda")
+    az.policy_tensors(x, out, history=h, penalties=torch.tensor([[1.0, 0.5, 0.25]], device="cuda"), probabilities=False)
+    want = torch.zeros((1, v), device="cuda")
+    want[0, 5], want[0, 7], want[0, v - 1] = -1.75, -999.75, -0.75
+    assert torch.equal(out, want)
