@@ -265,17 +265,15 @@ extern "C" int az_codes_quantize(const void* x, int32_t dtype, int64_t ldx, cons
                                  const az_code_matrix* qt, void* stream) {
   static const char who[] = "az_codes_quantize";
   int st = code_check(q, who);
-  if (st == AZ_OK && qt) {
-    if (q->scale_rows != CB || qt->scale_rows != CB)
-      return code_fail(AZ_ERR_INVALID_ARG, who, "the transposed matrix needs scale_rows 128 in both");
-    if (qt->rows != q->cols || qt->cols != q->rows) {
-      if (q->rows != 0) return code_fail(AZ_ERR_INVALID_ARG, who, "the transposed matrix has other sizes");
-    } else {
-      st = code_check(qt, who);
-    }
-  }
   if (st != AZ_OK) return st;
-  if (q->rows == 0) return AZ_OK;
+  if (qt && (q->scale_rows != CB || qt->scale_rows != CB))
+    return code_fail(AZ_ERR_INVALID_ARG, who, "the transposed matrix needs scale_rows 128 in both");
+  if (q->rows == 0) return AZ_OK;  // (its transposed form, of no columns, is no matrix to check)
+  if (qt) {
+    if (qt->rows != q->cols || qt->cols != q->rows)
+      return code_fail(AZ_ERR_INVALID_ARG, who, "the transposed matrix has other sizes");
+    if ((st = code_check(qt, who)) != AZ_OK) return st;
+  }
   if ((st = dense_check(x, dtype, ldx, q->cols, who)) != AZ_OK) return st;
   const CodeView v = code_view(*q);
   const CodeView vt = qt ? code_view(*qt) : v;

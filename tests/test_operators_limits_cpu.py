@@ -36,3 +36,11 @@ def test_more_tiles_than_a_launch_has_are_refused():
     assert az.az_codes_weight_grad_workspace(1, top, 16) == 0
     assert L.az_codes_weight_grad(P, 1 << 31, top, M(rows=1, cols=16, ld=16), P, az.AZ_F32, 16, P, 0, None, 0, None) == U
     assert b"launch" in L.az_last_error()
+
+
+def test_no_rows_have_a_transposed_form():
+    L, none = az.lib(), M(rows=0, scale_rows=128, codes=None, scales=None)
+    q = L.az_codes_quantize
+    assert q(None, az.AZ_F32, 40, none, M(rows=40, cols=0, ld=0, scale_rows=128, codes=None, scales=None), None) == az.AZ_OK
+    assert q(None, az.AZ_F32, 40, none, M(rows=40, cols=5, ld=16, scale_rows=128), None) == az.AZ_OK  # (it has no shape to hold it against)
+    assert q(None, az.AZ_F32, 40, none, M(rows=40, cols=0, ld=0, scale_rows=1), None) == E
