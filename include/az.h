@@ -514,7 +514,8 @@ typedef struct {
  *              input otherwise.
  *   workspace  device, 16-byte aligned, at least az_logits_policy_workspace
  *              bytes (which may be 0; then it may be NULL), written before it is
- *              read; not shared by two calls that may run at once.
+ *              read; not shared by two calls that may run at once.  Adjusted
+ *              logits use none: it may be NULL.
  * All arithmetic is fp32, sums in a fixed order.  Buffers are aligned to their
  * elements.  rows = 0: AZ_OK, nothing is launched.  Errors as above. */
 size_t az_logits_policy_workspace(int32_t rows, int32_t vocab);

@@ -557,7 +557,8 @@ def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None
     elif lengths is not None or penalties is not None:
         raise ValueError("lengths and penalties come with a history")
     s = _on(logits.device, stream, out, mask, bias, history, lengths, penalties)
-    ws, size, keep = _workspace(workspace, az_logits_policy_workspace(b, v), logits.device, stream)
+    need = az_logits_policy_workspace(b, v) if probabilities else 0
+    ws, size, keep = _workspace(workspace, need, logits.device, stream)
     p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
     rows = az_logits(p(logits), _float_type(logits), b, v, ld, p(mask), kind, ldm, p(bias), ldb, p(history), ldh, t,
                      p(lengths), p(penalties))

@@ -341,7 +341,7 @@ extern "C" int az_logits_policy(const az_logits* in, int32_t probabilities, floa
   }
   if (((uintptr_t)in->bias | (uintptr_t)in->history | (uintptr_t)in->lengths | (uintptr_t)in->penalties) & 3u)
     return code_fail(AZ_ERR_INVALID_ARG, who, "a buffer that is not aligned to its element");
-  const size_t need = az_logits_policy_workspace(in->rows, in->vocab);
+  const size_t need = probabilities ? az_logits_policy_workspace(in->rows, in->vocab) : 0;  // (adjusted logits have no sums)
   if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
   if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
   const int nt = policy_threads(in->rows, in->vocab);

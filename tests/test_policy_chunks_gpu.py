@@ -37,3 +37,24 @@ def test_the_longest_history():
     want = torch.zeros((1, v), device="cuda")
     want[0, 5], want[0, 7], want[0, v - 1] = -1.75, -999.75, -0.75
     assert torch.equal(out, want)
+
+
+def test_adjusted_logits_of_long_rows_need_no_workspace():
+    import torch
+
+    import paper_2609_37447_amd as az
+    v = 40000
+    x = torch.randn((3, v), device="cuda")
+    mask = torch.randint(0, 2, (3, v), device="cuda", dtype=torch.uint8)
+    out = torch.empty_like(x)
+    l = az.az_logits(x.data_ptr(), az.AZ_F32, 3, v, v, mask.data_ptr(), az.AZ_MASK_BYTES, v)
+    assert az.az_logits_policy_workspace(3, v) > 0
+    assert az.az_logits_policy(l, False, out.data_ptr(), v, None, 0, torch.cuda.current_stream().cuda_stream) == az.AZ_OK
+    assert torch.equal(out, x.masked_fill(mask == 0, float("-inf")))
+    with pytest.raises(az.AzError):  # (the policy needs one)
+        az.az_logits_policy(l, True, out.data_ptr(), v, None, 0, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    az.policy_tensors(x, out, mask=mask, probabilities=False)
+    assert torch.cuda.max_memory_allocated() == held
