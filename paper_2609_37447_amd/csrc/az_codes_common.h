@@ -44,6 +44,11 @@ inline int code_fail(int status, const char* who, const char* what) {
   return az_fail(status, text);
 }
 
+// Whether sizes of at least one row and column are within the limits.
+inline bool code_sizes(int64_t rows, int64_t cols) {
+  return rows <= INT32_MAX && cols <= (1 << 30) && rows * ((cols + CB - 1) / CB) <= INT32_MAX;
+}
+
 // Checks of a matrix that every operator makes.  Pointers are checked where the
 // matrix has entries.
 inline int code_check(const az_code_matrix* m, const char* who) {
@@ -51,8 +56,7 @@ inline int code_check(const az_code_matrix* m, const char* who) {
   if (m->rows < 0 || m->cols < 1) return code_fail(AZ_ERR_INVALID_ARG, who, "rows < 0 or cols < 1");
   if (m->scale_rows != 1 && m->scale_rows != CB) return code_fail(AZ_ERR_INVALID_ARG, who, "scale_rows is neither 1 nor 128");
   if (m->ld < m->cols || m->ld % 16) return code_fail(AZ_ERR_INVALID_ARG, who, "ld is below cols or not a multiple of 16");
-  if (m->rows > INT32_MAX || m->cols > (1 << 30) || m->rows * ((m->cols + CB - 1) / CB) > INT32_MAX)
-    return code_fail(AZ_ERR_UNSUPPORTED, who, "a matrix past the size limits");
+  if (!code_sizes(m->rows, m->cols)) return code_fail(AZ_ERR_UNSUPPORTED, who, "a matrix past the size limits");
   if (m->rows == 0) return AZ_OK;
   if (!m->codes || !m->scales) return code_fail(AZ_ERR_INVALID_ARG, who, "NULL codes or scales");
   if ((uintptr_t)m->codes & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "codes must be 16-byte aligned");

@@ -459,7 +459,7 @@ int launch_feed(int feed, const uint16_t* dy, int64_t ldy, int n, const CodeView
 }  // namespace
 
 extern "C" size_t az_codes_weight_grad_workspace(int64_t rows, int32_t n, int64_t cols) {
-  if (rows <= 0 || n <= 0 || cols <= 0) return 0;
+  if (rows <= 0 || n <= 0 || cols <= 0 || !code_sizes(rows, cols)) return 0;
   const Cut cut = choose_cut(rows, n, cols);
   return cut.parts > 1 ? (size_t)cut.parts * (size_t)n * ((size_t)cols + 1) * sizeof(float) : 0;
 }

@@ -530,7 +530,8 @@ bool tile_fits(int64_t lda, int64_t ldb) { return lda < (1 << 22) && ldb < (1 <<
 }  // namespace
 
 extern "C" size_t az_codes_matmul_workspace(const az_code_matrix* a, const az_code_matrix* b, int32_t dtype) {
-  if (!a || !b || a->rows <= 0 || b->rows <= 0 || a->cols <= 0) return 0;
+  if (!a || !b || a->rows <= 0 || b->rows <= 0 || a->cols <= 0 || b->cols <= 0) return 0;
+  if (!code_sizes(a->rows, a->cols) || !code_sizes(b->rows, b->cols)) return 0;
   const Plan p = choose_plan(a->rows, b->rows, a->cols, dtype == AZ_F32, tile_fits(a->ld, b->ld));
   return p.parts > 1 ? (size_t)p.parts * (size_t)a->rows * (size_t)b->rows * sizeof(float) : 0;
 }

@@ -22,6 +22,7 @@ constexpr int GROUPS = 4;               // a thread's groups of four entries
 constexpr int PER = 4 * GROUPS;         // entries of a thread
 constexpr int THREADS = 1024;           // of the largest workgroup
 constexpr int MOST = THREADS * PER;     // entries of a workgroup
+constexpr int MAX_ROWS = 1 << 20, MAX_VOCAB = 1 << 24;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 struct PolicyView {
@@ -309,7 +310,7 @@ int launch(const PolicyView& p, int rows, int nt, hipStream_t s) {
 }  // namespace
 
 extern "C" size_t az_logits_policy_workspace(int32_t rows, int32_t vocab) {
-  if (rows <= 0 || vocab <= MOST) return 0;
+  if (rows <= 0 || rows > MAX_ROWS || vocab <= MOST || vocab > MAX_VOCAB) return 0;
   const int chunk = policy_threads(rows, vocab) * PER;
   return (size_t)rows * (size_t)((vocab + chunk - 1) / chunk) * sizeof(float2);
 }
@@ -319,7 +320,7 @@ extern "C" int az_logits_policy(const az_logits* in, int32_t probabilities, floa
   static const char who[] = "az_logits_policy";
   if (!in) return code_fail(AZ_ERR_INVALID_ARG, who, "NULL logits");
   if (in->rows < 0 || in->vocab < 1) return code_fail(AZ_ERR_INVALID_ARG, who, "rows < 0 or vocab < 1");
-  if (in->rows > (1 << 20) || in->vocab > (1 << 24)) return code_fail(AZ_ERR_UNSUPPORTED, who, "rows > 2^20 or vocab > 2^24");
+  if (in->rows > MAX_ROWS || in->vocab > MAX_VOCAB) return code_fail(AZ_ERR_UNSUPPORTED, who, "rows > 2^20 or vocab > 2^24");
   if (in->dtype != AZ_F32 && in->dtype != AZ_BF16) return code_fail(AZ_ERR_INVALID_ARG, who, "dtype is neither AZ_F32 nor AZ_BF16");
   if (in->mask_kind < AZ_MASK_NONE || in->mask_kind > AZ_MASK_BITS) return code_fail(AZ_ERR_INVALID_ARG, who, "unknown mask kind");
   if (in->max_history < 0) return code_fail(AZ_ERR_INVALID_ARG, who, "max_history < 0");

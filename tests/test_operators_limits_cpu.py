@@ -44,3 +44,15 @@ def test_no_rows_have_a_transposed_form():
     assert q(None, az.AZ_F32, 40, none, M(rows=40, cols=0, ld=0, scale_rows=128, codes=None, scales=None), None) == az.AZ_OK
     assert q(None, az.AZ_F32, 40, none, M(rows=40, cols=5, ld=16, scale_rows=128), None) == az.AZ_OK  # (it has no shape to hold it against)
     assert q(None, az.AZ_F32, 40, none, M(rows=40, cols=0, ld=0, scale_rows=1), None) == E
+
+
+def test_sizes_that_are_refused_have_no_workspace():
+    L, top = az.lib(), 2 ** 63 - 1
+    assert az.az_logits_policy_workspace(1, 2 ** 31 - 1) == 0 and az.az_logits_policy_workspace(2 ** 31 - 1, 1 << 24) == 0
+    assert az.az_logits_policy_workspace(1 << 20, 1 << 24) > 0
+    assert az.az_codes_weight_grad_workspace(top, 64, 128) == 0 and az.az_codes_weight_grad_workspace(1 << 16, 64, top) == 0
+    assert az.az_codes_weight_grad_workspace(2 ** 31 - 1, 64, 128) > 0
+    good = M(rows=333, cols=10240, ld=10240)
+    for bad in (M(rows=top, cols=10240, ld=10240), M(rows=333, cols=top, ld=10240), M(rows=2 ** 31, cols=1 << 20, ld=1 << 20)):
+        assert az.az_codes_matmul_workspace(bad, good, az.AZ_BF16) == 0 and az.az_codes_matmul_workspace(good, bad, az.AZ_BF16) == 0
+    assert L.az_logits_policy(az.az_logits(P, az.AZ_F32, 1, 2 ** 31 - 1, 2 ** 31), 1, P, 2 ** 31, None, 0, None) == U
