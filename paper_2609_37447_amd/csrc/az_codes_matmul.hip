@@ -514,13 +514,11 @@ int launch_tiled(const Plan& p, const Operands& o) {
 }
 
 template <bool EXACT, bool F32>
-int launch(const Plan& p, const Operands& o) {
-  int st = AZ_OK;
-  if (p.kind == TILE256) st = launch_tiled<4, 4, 2, 2, EXACT, F32>(p, o);
-  else if (p.kind == TILE128) st = launch_tiled<2, 2, 2, 2, EXACT, F32>(p, o);
-  else if (p.kind == TILE64) st = launch_tiled<1, 2, 2, 2, EXACT, F32>(p, o);
-  else if (p.kind == TILE32) st = launch_tiled<1, 1, 1, 4, EXACT, F32>(p, o);
-  else if constexpr (EXACT == F32) st = launch_direct<EXACT>(o);  // (in one part: never sums of e4m3 products in fp32)
+int launch_tiles(const Plan& p, const Operands& o) {
+  const int st = p.kind == TILE256   ? launch_tiled<4, 4, 2, 2, EXACT, F32>(p, o)
+                 : p.kind == TILE128 ? launch_tiled<2, 2, 2, 2, EXACT, F32>(p, o)
+                 : p.kind == TILE64  ? launch_tiled<1, 2, 2, 2, EXACT, F32>(p, o)
+                                     : launch_tiled<1, 1, 1, 4, EXACT, F32>(p, o);
   return launched("az_codes_matmul", st);
 }
 
@@ -555,12 +553,13 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
   const Plan p = choose_plan(a->rows, b->rows, a->cols, dtype == AZ_F32, tile_fits(a->ld, b->ld));
   Operands o = {code_view(*a), code_view(*b), bias, out, ld_out, 0, static_cast<hipStream_t>(stream)};
   (void)hipGetLastError();
+  if (p.kind == DIRECT) return launched(who, dtype == AZ_F32 ? launch_direct<true>(o) : launch_direct<false>(o));
   if (p.parts > 1) {
     o.bias = nullptr;
     o.out = workspace;
     o.ldo = b->rows;
     o.part_stride = a->rows * b->rows;
-    if ((st = dtype == AZ_F32 ? launch<true, true>(p, o) : launch<false, true>(p, o)) != AZ_OK) return st;
+    if ((st = dtype == AZ_F32 ? launch_tiles<true, true>(p, o) : launch_tiles<false, true>(p, o)) != AZ_OK) return st;
     const int64_t groups = (a->rows * b->rows + 255) / 256;
     const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
     const float* parts = static_cast<const float*>(workspace);
@@ -570,5 +569,5 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
       hipLaunchKernelGGL((az_join_products<false>), g, dim3(256), 0, o.stream, parts, p.parts, (int)a->rows, (int)b->rows, bias, out, ld_out);
     return launch_status(who);
   }
-  return dtype == AZ_F32 ? launch<true, true>(p, o) : launch<false, false>(p, o);
+  return dtype == AZ_F32 ? launch_tiles<true, true>(p, o) : launch_tiles<false, false>(p, o);
 }
