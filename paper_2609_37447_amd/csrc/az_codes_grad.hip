@@ -208,21 +208,20 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t kt = (uint32_t)(x.cols + G::T - 1) / G::T, id = blockIdx.x - bias;
   const int n0 = (int)(id / kt) * G::T, k0 = (int)(id % kt) * G::T;
-  // From here on rows are counted within the part (at most 2^30 of them, so that steps past its end are counted in 32 bits as well).
-  const int from = (int)blockIdx.y * part_rows, me = min(part_rows, x.rows - from);
-  dy += from * ldy;
-  x.codes += from * x.ld;
-  x.scales += (int64_t)from * x.nb;
+  // Rows are unsigned: a part's last steps begin past 2^31 where there are nearly as many.  (Counted from the part's
+  // first row instead, with the pointers moved there, unaligned rows took 4% more.)
+  const uint32_t mb = blockIdx.y * (uint32_t)part_rows, me = mb + (uint32_t)min(part_rows, x.rows - (int)mb);
 
   // dy, copied: a wave fills YROWS rows at a time, a lane one chunk.
   const int yr = G::YROWS * wave + lane / (G::T / 8), yp = lane % (G::T / 8), yc = yp ^ ((yr & 3) << 2);
   const uint32_t yoff = (uint32_t)yr * (uint32_t)ldy * 2u + (uint32_t)yc * 16u;
   lds_bytes* const ylds = (lds_bytes*)smem + G::YROWS * wave * G::ROW;
-  auto copy_y = [&](int m, int stage) {
+  auto copy_y = [&](uint32_t m, int stage) {
     // (past the last row: nothing is in range, and zeros are read.  The range is checked by whole words, of
     // which the row's last holds one element where n is odd: the range ends behind that word, which lies in
     // the row's last aligned 16 bytes.)
-    const int rows = min(me - m, MS), first = min(m, me - 1);
+    const int rows = min((int)(me - m), MS);
+    const uint32_t first = min(m, me - 1);
     const uint32_t bytes = (((uint32_t)max(rows, 1) - 1u) * (uint32_t)ldy + (((uint32_t)(n - n0) + 1u) & ~1u)) * 2u;
     const __amdgpu_buffer_rsrc_t buf =
         __builtin_amdgcn_make_buffer_rsrc((void*)(dy + first * ldy + n0), 0, (int)(bytes & (uint32_t)-(int)(rows > 0)), 0x00027000);
@@ -230,14 +229,14 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   };
   const Chunk8 yk(n0 + 8 * yc, n);
   cm_i32x4 yv[FEED == COPY ? 1 : G::YCOPIES];
-  auto load_y = [&](int m) {
+  auto load_y = [&](uint32_t m) {
 #pragma unroll
     for (int j = 0; j < G::YCOPIES; j++) {
-      const uint16_t* row = dy + min(m + yr + j * 4 * G::YROWS, me - 1) * ldy;
+      const uint16_t* row = dy + min(m + (uint32_t)(yr + j * 4 * G::YROWS), me - 1) * ldy;
       yv[FEED == COPY ? 0 : j] = FEED == SHORT ? short_row(row, n0 + 8 * yc, n) : yk.load(row);
     }
   };
-  auto store_y = [&](int m, int stage) {
+  auto store_y = [&](uint32_t m, int stage) {
 #pragma unroll
     for (int j = 0; j < G::YCOPIES; j++) {
       cm_i32x4 v = yv[FEED == COPY ? 0 : j];
@@ -255,8 +254,9 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
   uint8_t* const xlds = smem + G::TILE + xr * G::ROW + (((t % (G::T / 16)) * 2) ^ ((xr & 3) << 2)) * 16;
   cm_i32x4 xv[G::XCHUNKS];
   uint32_t xs[G::XCHUNKS];
-  auto load_x = [&](int m) {
-    const int rows = min(me - m, MS), first = min(m, me - 1), some = -(int)(rows > 0);
+  auto load_x = [&](uint32_t m) {
+    const int rows = min((int)(me - m), MS), some = -(int)(rows > 0);
+    const uint32_t first = min(m, me - 1);
     const uint32_t bytes = ((uint32_t)max(rows, 1) - 1u) * (uint32_t)x.ld + (((uint32_t)x.cols + 15u) & ~15u);
     const __amdgpu_buffer_rsrc_t codes =
         __builtin_amdgcn_make_buffer_rsrc(x.codes + first * x.ld, 0, (int)(bytes & (uint32_t)some), 0x00027000);
@@ -301,29 +301,29 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
     for (int j = 0; j < W; j++) acc[i][j] = cm_f32x16{};
 
   typename G::Frag f0, f1;
-  load_x(0);
+  load_x(mb);
   if constexpr (FEED == COPY) {
-    copy_y(0, 0);
+    copy_y(mb, 0);
   } else {
-    load_y(0);
-    store_y(0, 0);
-    load_y(MS);
+    load_y(mb);
+    store_y(mb, 0);
+    load_y(mb + MS);
   }
   store_x(0);
-  load_x(MS);
+  load_x(mb + MS);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if constexpr (FEED == COPY) {
-    copy_y(MS, G::STAGE);
+    copy_y(mb + MS, G::STAGE);
   } else {
-    store_y(MS, G::STAGE);
-    load_y(2 * MS);
+    store_y(mb + MS, G::STAGE);
+    load_y(mb + 2 * MS);
   }
   store_x(G::STAGE);
-  load_x(2 * MS);
+  load_x(mb + 2 * MS);
   G::read(f0, smem, yo, xo, 0);
   uint32_t stage = 0;
-  for (int m = 0; m < me; m += MS, stage ^= G::STAGE) {
+  for (uint32_t m = mb; m < me; m += MS, stage ^= G::STAGE) {
     G::read(f1, smem, yo, xo, stage + 32 * G::ROW);
     G::multiply(acc, f0);
     G::template interleave<2>();
@@ -417,7 +417,7 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
     const int64_t t = 64 * w, tiles = ((n + t - 1) / t) * ((cols + t - 1) / t);
     for (int64_t parts = 1; parts <= 64 && (parts == 1 || 2 * parts <= steps); parts *= 2) {
       const int64_t per = (steps + parts - 1) / parts, groups = tiles * parts, slots = w == 4 ? 256 : 512;
-      if (per * MS > 1 << 30) continue;  // (a part's rows are counted in 32 bits)
+      if (per * MS > 1 << 30) continue;  // (a part's own rows are counted in an int, with some to spare)
       const double step = w == 4 ? (groups <= 128 ? 1.48 : 1.86) : (groups <= 256 ? 0.72 : 1.0);
       double cost = (double)((groups + slots - 1) / slots) * ((double)per * step + 3.0) + outputs * 4 * write;
       if (parts > 1) cost += 3.5 + (double)parts * outputs * 8 * write;
