@@ -132,7 +132,7 @@ __global__ __launch_bounds__(NT) void az_quantize_rows(const void* __restrict__ 
 template <bool BF16, bool TRANSPOSED>
 __global__ __launch_bounds__(NT) void az_quantize_tiles(const void* __restrict__ x, int64_t ldx, CodeView q, CodeView qt) {
   __shared__ uint32_t most[NT / 64];
-  __shared__ uint8_t tile[TRANSPOSED ? CB * (CB + 4) : 4];
+  __shared__ __attribute__((aligned(16))) uint8_t tile[TRANSPOSED ? CB * (CB + 4) : 4];  // (written by words)
   const uint32_t rb = blockIdx.x / (uint32_t)q.nb, kb = blockIdx.x - rb * (uint32_t)q.nb;
   const int t = threadIdx.x, c = (int)kb * CB + (t & 7) * 16;
   const int64_t r0 = (int64_t)rb * CB + (t >> 3);
