@@ -445,7 +445,8 @@ int az_codes_dequantize(const az_code_matrix* q, void* x, int32_t dtype, int64_t
  *         aligned to its element.
  * AZ_BF16 multiplies on the scaled e4m3 matrix instruction, which cuts products
  * that are far below the largest one next to them (about 1.5e-5 of the result's
- * norm, a hundredth of a bf16 rounding) and accumulates in fp32.  AZ_F32 multiplies on
+ * norm, a hundredth of a bf16 rounding; at most 2^-10 of the sum of the products'
+ * sizes, where they cancel) and accumulates in fp32.  AZ_F32 multiplies on
  * the bf16 instruction: every product is exact, sums are fp32.  Sums have a fixed
  * order: equal calls give equal bits.
  *   workspace  device, 16-byte aligned, at least az_codes_matmul_workspace bytes
@@ -463,7 +464,7 @@ int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b, const floa
  * (accumulate != 0: added to what dw and db hold).
  *   x   ld below 2^25.
  *   dy  device, bf16 [x->rows][N], ld_dy elements from row to row; 16-byte aligned rows
- *       (dy and ld_dy) take a faster path.
+ *       (dy and ld_dy) take a faster path.  What lies past N in a row never matters.
  *   dw  device, [N][x->cols], dtype AZ_F32 or AZ_BF16, ld_dw elements from row to
  *       row.  db  device, [N] fp32, or NULL.
  * Products are exact, sums fp32 in a fixed order.  x->rows = 0 clears dw and db (or,
@@ -516,8 +517,9 @@ typedef struct {
  *              bytes (which may be 0; then it may be NULL), written before it is
  *              read; not shared by two calls that may run at once.  Adjusted
  *              logits use none: it may be NULL.
- * All arithmetic is fp32, sums in a fixed order.  Buffers are aligned to their
- * elements.  rows = 0: AZ_OK, nothing is launched.  Errors as above. */
+ * All arithmetic is fp32, sums in a fixed order; a probability's relative error grows
+ * with its logit's distance from the largest, to about |l - max l| 2^-23.  Buffers are
+ * aligned to their elements.  rows = 0: AZ_OK, nothing is launched.  Errors as above. */
 size_t az_logits_policy_workspace(int32_t rows, int32_t vocab);
 int az_logits_policy(const az_logits* in, int32_t probabilities, float* out, int64_t ld_out, void* workspace,
                      size_t workspace_bytes, void* stream);

@@ -191,7 +191,7 @@ struct Grad {
 
 // Blocks 0..bias-1 sum dy's columns; the others own a tile of dw each.  Both take the rows
 // part * part_rows on, part = blockIdx.y; sums over one of several parts go to a workspace, dw's at
-// part * part_stride and db's at part * n.  16384 x 4096 x 4096: 463-490 us (1,120-1,190 TFLOP/s, power);
+// part * part_stride and db's at part * n.  16384 x 4096 x 4096: 465-490 us warm (1,120-1,180 TFLOP/s, power);
 // 1024 x 1880 x 10240: 59 us, of which 77 MB of results take 17 at a copy's rate.
 template <int W, bool F32, int FEED>
 __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint16_t* __restrict__ dy, int64_t ldy, int n, CodeView x,
@@ -345,8 +345,8 @@ __global__ __launch_bounds__(NT, W == 4 ? 1 : 2) void az_weight_grad(const uint1
 
   // D's rows are k and its columns n: a lane holds four neighbouring k of one n.  They leave through LDS
   // (half of each wave's rows at a time where all do not fit), so that whole rows of the tile are written;
-  // chunks are exchanged by the row against bank conflicts.  100 x 4096 x 4096: 25.1 us by single values
-  // straight from the registers, 19.7 so; rows of 8393 gradients, not 16 bytes apart: 184 and 142 us.
+  // chunks are exchanged by the row against bank conflicts.  100 x 4096 x 4096: 25.3 us by single values
+  // straight from the registers, 19.0 so; rows of 8393 gradients, not 16 bytes apart: 183 and 142 us.
   constexpr int PASSES = 2 * G::STAGE >= G::T * G::T * 4 ? 1 : 2, PF = W / PASSES, PROWS = G::T / PASSES;
   constexpr int OROW = G::T * 4, RC = G::T / 4;  // bytes and chunks of a row
   static_assert(PROWS * OROW <= 2 * G::STAGE && W % PASSES == 0, "a pass fits the stages");
@@ -406,8 +406,8 @@ struct Cut {
 // or 1.48 (W = 4) alone on a compute unit, bound by the step's own chain, 1.0 with two workgroups there
 // (W = 2) and 1.86 with every compute unit busy (W = 4), as measured.  Parts cost their way through
 // memory and a second launch.  Measured, chosen against others: 16384 x 512 x 512 in 16 parts of small
-// tiles 29 (32 parts 33, large tiles 45); 16384 x 4096 x 4096 in one part of large tiles 477; 16384 x
-// 1024 x 1024 in 8 parts of small tiles 58 (16 of large ones 63).
+// tiles 27 (32 parts 32, large tiles 44); 16384 x 4096 x 4096 in one part of large tiles 475; 16384 x
+// 1024 x 1024 in 8 parts of small tiles 56 (16 of large ones 57).
 Cut choose_cut(int64_t rows, int64_t n, int64_t cols) {
   const int64_t steps = rows > 0 ? (rows + MS - 1) / MS : 1;
   const double write = 1.0 / 4.5e6, outputs = (double)n * (double)cols;  // microseconds a byte

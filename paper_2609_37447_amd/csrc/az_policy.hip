@@ -9,8 +9,9 @@
 // caches still hold, to write the result.  What has been chosen before is counted in LDS, a
 // counter for each entry of the chunk, so that penalties cost no search.
 //
-// 4,096 rows of 4,672 fp32 logits and bits: 31 us, 5.1 TB/s.  512 rows of 131,072 bf16 logits and bits:
-// 108 us, 136 with 2,048 past entries a row (81 at a copy's rate if the logits were read once).  One workgroup of 1,024 threads that keeps such a row in its registers reads it once,
+// 4,096 rows of 4,672 fp32 logits and bits: 30.5 us, 5.1 TB/s.  512 rows of 131,072 bf16 logits, bits and a
+// bias: 112 us, 137 with 2,048 past entries a row (81 at a copy's rate if the logits were read once).  One workgroup
+// of 1,024 threads that keeps such a row in its registers reads it once,
 // but leaves a compute unit nothing else to do between its barriers: 135 us, 146 with past entries.
 #include <math.h>
 
@@ -38,7 +39,8 @@ struct PolicyView {
   int vocab, max_history, bf16, mask_kind;
 };
 
-// exp(l - m); 0 for l = -inf where m is finite.
+// exp(l - m); 0 for l = -inf where m is finite.  The difference and its product with log2 e are one fp32 number
+// each, as in the network kernels: the relative error grows to about |l - m| 2^-23.
 __device__ __forceinline__ float exp_below(float l, float m) { return __builtin_amdgcn_exp2f((l - m) * LOG2E); }
 
 // Maximum (of what is not NaN) and sum over a wave, in every lane, by lane exchanges of the
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void az_policy_kernel(PolicyView p, int ro
 }
 
 // Threads of a workgroup: enough for the row, up to 1,024.  Rows that need several
-// workgroups get 512 (512 rows of 131,072: 136 us, 149 with 1,024), or 256 where that takes to fill the chip.
+// workgroups get 512 (512 rows of 131,072: 137 us, 152 with 1,024), or 256 where that takes to fill the chip.
 int policy_threads(int64_t rows, int64_t vocab) {
   int nt = 256;
   if (vocab <= MOST) {
