@@ -524,6 +524,136 @@ size_t az_logits_policy_workspace(int32_t rows, int32_t vocab);
 int az_logits_policy(const az_logits* in, int32_t probabilities, float* out, int64_t ld_out, void* workspace,
                      size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Around a dense layer: the norm in front of it, its weights in 4 bits, and the entry
+ * drawn from its logits.  Called as the operators above: no handle, asynchronous on
+ * `stream`, nothing is allocated, values are not checked.
+ *
+ * Root-mean-square norm of rows, with the addition of a residual:
+ *   h = round(x + residual)  (added in fp32, rounded to dtype; h = x without a residual)
+ *   y = h * r * weight,  r = 1 / sqrt(mean(h^2) + eps)
+ * Sums of squares are fp64 (no finite row overflows), the rest fp32 until y is rounded
+ * once.  An infinity or NaN in a row's h makes the row's y NaN or zero, as the formula has it. */
+typedef struct {
+  int64_t rows, cols;       /* rows 0..2^31-1, cols 1..2^24 */
+  const void* x;            /* device, [rows][cols], aligned to its element */
+  int32_t dtype;            /* AZ_F32 or AZ_BF16: of x, residual, sum and y */
+  float eps;                /* a positive normal number */
+  int64_t ld_x;             /* elements from row to row */
+  const void* residual;     /* device, [rows][cols], or NULL */
+  int64_t ld_residual;
+  const float* weight;      /* device, [cols], or NULL: 1 */
+  void* sum;                /* receives h, or NULL; it may be x's or the residual's own buffer (same ld) */
+  int64_t ld_sum;
+  void* y;                  /* receives y in dtype, or NULL; it may be x's own buffer (same ld) where sum is not */
+  int64_t ld_y;
+  const az_code_matrix* q;  /* receives the codes of y (scale_rows 1; az_codes_quantize of the fp32 y), or NULL */
+} az_norm;
+
+/* At least one of sum, y and q is given.  Outputs overlap neither each other nor any input but as said.  Returns AZ_OK,
+ * AZ_ERR_INVALID_ARG, AZ_ERR_UNSUPPORTED (sizes past the limits) or AZ_ERR_DEVICE.  No rows: AZ_OK, nothing is
+ * launched. */
+int az_rms_norm(const az_norm* norm, void* stream);
+
+/* Its gradients, from h as the norm gave it (or x, without a residual):
+ *   u = h * r;  g = dy * weight;  dx = r * (g - u * mean(g * u)) + dsum;  dweight = sum over rows of dy * u
+ * dx is the gradient of x and of the residual alike.  Codes are taken as their values: dy is the gradient of y. */
+typedef struct {
+  int64_t rows, cols;
+  const void* dy;           /* device, [rows][cols] */
+  int32_t dtype;            /* AZ_F32 or AZ_BF16: of dy, h, dsum and dx */
+  float eps;
+  int64_t ld_dy;
+  const void* h;            /* device, [rows][cols] */
+  int64_t ld_h;
+  const float* weight;      /* device, [cols], or NULL: 1 */
+  const void* dsum;         /* device, [rows][cols]: what else reaches h, or NULL */
+  int64_t ld_dsum;
+  void* dx;                 /* device, [rows][cols], or NULL; it may be dy's or dsum's own buffer (same ld) */
+  int64_t ld_dx;
+  float* dweight;           /* device, [cols], or NULL */
+  int32_t accumulate;       /* nonzero: added to what dweight holds */
+} az_norm_grad;
+
+/* At least one of dx and dweight is given.  No rows clears dweight (or, accumulating, leaves it).
+ *   workspace  device, 16-byte aligned, at least az_rms_norm_grad_workspace bytes where dweight is given (else it may
+ *              be NULL): sums over parts of the rows, written before they are read, joined in a fixed order;
+ *              not shared by two calls that may run at once.
+ * Errors as above. */
+size_t az_rms_norm_grad_workspace(int64_t rows, int64_t cols);
+int az_rms_norm_grad(const az_norm_grad* grad, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A matrix in 4 bits holds OCP e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign bit; no infinity, no NaN) with one
+ * scale 2^(s - 127), s a byte, for each block of 32 consecutive columns of a row: the microscaled fp4 format, which the
+ * matrix instruction multiplies at twice the rate of e4m3.
+ * az_nibbles_quantize writes s in 2..252, for which every value is zero or a normal finite float that fp32 and bf16
+ * hold exactly; the operators take these bytes, and 255, which makes its block NaN.
+ *   codes      device, [rows][ld] bytes, 16-byte aligned; column j in the low (j even) or high four bits of byte j / 2.
+ *   scales     device, [rows][ld_scales] bytes, 4-byte aligned.
+ *   rows, cols rows 0..2^31-1, cols 1..2^30; at most 2^31-1 rows times 128-column parts of a row.
+ *   ld         bytes from row to row, a multiple of 16, >= cols / 2.  What lies past a row's last column never
+ *              matters; quantising writes zero into the other half of an odd row's last byte and nothing past it.
+ *   ld_scales  bytes from row to row, a multiple of 4, >= ceil(cols / 32); the bytes past those are not
+ *              written and never matter. */
+#define AZ_FP4_BLOCK 32
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t rows, cols, ld, ld_scales;
+} az_fp4_matrix;
+
+/* Codes of x [q->rows][q->cols] (AZ_F32 or AZ_BF16): for each block with a = max |x|, e = ceil(log2(a / 6)) clamped to
+ * -125..125 (0 if a = 0), s = e + 127, code = sat(rne(x * 2^-e)), |code| <= 6.  A block with an infinity or NaN gets
+ * s = 255 and zero codes.
+ *   qt  NULL, or a second matrix [q->cols][q->rows] that receives the transposed x, with blocks of its own along
+ *       its rows: the weights of the backward pass.
+ * Errors as for az_codes_quantize. */
+int az_nibbles_quantize(const void* x, int32_t dtype, int64_t ldx, const az_fp4_matrix* q, const az_fp4_matrix* qt,
+                        void* stream);
+
+/* x[i][j] = the value of entry (i, j) of q, in AZ_F32 or AZ_BF16 (exact in both). */
+int az_nibbles_dequantize(const az_fp4_matrix* q, void* x, int32_t dtype, int64_t ldx, void* stream);
+
+/* out[m][n] = bias[n] + sum_k a[m][k] b[n][k], b [N][K] in 4 bits and a [M][K] in 4 bits, or (az_codes_nibbles_matmul)
+ * a coded matrix.  Arguments, workspace and errors as az_codes_matmul's; both ld below 2^27 and ld_scales
+ * below 2^26.  Products of two 4-bit matrices are exact in either result type, sums fp32.  With a coded a, AZ_BF16
+ * multiplies on the scaled instruction, which cuts small products as az_codes_matmul's does, and AZ_F32
+ * on the bf16 one, with exact products. */
+size_t az_nibbles_matmul_workspace(const az_fp4_matrix* a, const az_fp4_matrix* b, int32_t dtype);
+int az_nibbles_matmul(const az_fp4_matrix* a, const az_fp4_matrix* b, const float* bias, void* out, int32_t dtype,
+                      int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
+size_t az_codes_nibbles_matmul_workspace(const az_code_matrix* a, const az_fp4_matrix* b, int32_t dtype);
+int az_codes_nibbles_matmul(const az_code_matrix* a, const az_fp4_matrix* b, const float* bias, void* out, int32_t dtype,
+                            int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One entry of each row of logits (as az_logits_policy adjusts them: -inf = not allowed), drawn with a given random
+ * number. */
+typedef struct {
+  const void* logits;        /* device, [rows][vocab], AZ_F32 or AZ_BF16 */
+  int32_t dtype;
+  int32_t rows, vocab;       /* rows 0..2^20, vocab 1..2^24 */
+  int64_t ld;                /* elements from row to row, >= vocab */
+  const float* u;            /* device, [rows], in [0, 1) (clamped to it; NaN counts as 0) */
+  const float* temperature;  /* device, [rows], or NULL: 1.  0 (and what is not > 0) takes the largest logit */
+  const int32_t* top_k;      /* device, [rows], or NULL; 0 and less: no limit */
+  const float* top_p;        /* device, [rows], or NULL; 1 and more (and NaN): no limit */
+  const float* min_p;        /* device, [rows], or NULL; 0 and less (and NaN): no limit, above 1 counts as 1 */
+} az_sampling;
+
+/* Per row, with w[v] = exp((logits[v] - largest) / temperature), entries in the order of falling logits, equal ones by
+ * rising index:
+ *   top_k  the first k entries stay;
+ *   top_p  of these, an entry stays while the sum of the weights before it is below top_p times the sum
+ *          of all of them (the first always stays);
+ *   min_p  of these, entries with w >= min_p stay.
+ *   out[row]   the first of the entries that stay, by rising index, at which the running sum of weights
+ *              exceeds u times their whole sum; -1 where nothing is allowed or a logit is NaN or +inf.
+ *   prob[row]  its weight over that sum, 0 with -1; or prob = NULL.
+ * Weights are whole multiples of 2^-S, S = 62 - ceil(log2(vocab)) and at most 51, computed in fp64, and sums of them exact:
+ * equal calls give equal results, and an entry of less than 2^-(S + 1) of the largest is never drawn.
+ * Buffers are aligned to their elements.  rows = 0: AZ_OK, nothing is launched.  Errors as above. */
+int az_logits_sample(const az_sampling* in, int32_t* out, float* prob, void* stream);
+
 /* Failure-handling test support.  az_debug_fail_allocation(n), n >= 1: the
  * n-th device or pinned-host allocation the library attempts from now on
  * (weights in az_net_load, buffers in az_pipeline_create) fails as if the

@@ -18,4 +18,8 @@ from ._binding import (AZ_ABI_VERSION, AZ_BF16, AZ_ERR_DEVICE, AZ_ERR_INVALID_AR
                        AZ_CODE_BLOCK, AZ_MASK_NONE, AZ_MASK_BYTES, AZ_MASK_BITS, az_code_matrix, az_logits,
                        az_codes_quantize, az_codes_dequantize, az_codes_matmul, az_codes_matmul_workspace, az_codes_weight_grad,
                        az_codes_weight_grad_workspace, az_logits_policy, az_logits_policy_workspace, CodeMatrix,
-                       quantize_tensors, dequantize_tensors, matmul_tensors, weight_grad_tensors, policy_tensors)
+                       quantize_tensors, dequantize_tensors, matmul_tensors, weight_grad_tensors, policy_tensors,
+                       AZ_FP4_BLOCK, az_fp4_matrix, az_norm, az_norm_grad, az_sampling, az_rms_norm, az_rms_norm_grad,
+                       az_rms_norm_grad_workspace, az_nibbles_quantize, az_nibbles_dequantize, az_nibbles_matmul,
+                       az_nibbles_matmul_workspace, az_codes_nibbles_matmul, az_codes_nibbles_matmul_workspace, az_logits_sample,
+                       Fp4Matrix, norm_tensors, norm_grad_tensors, sample_tensors)

@@ -31,6 +31,9 @@ EXPORTS = ("az_weight_count", "az_net_load", "az_eval_batch", "az_eval_batch_wdl
            "az_debug_live_allocations", "az_eval_batch_compact_noalloc",
            "az_codes_quantize", "az_codes_dequantize", "az_codes_matmul", "az_codes_matmul_workspace",
            "az_codes_weight_grad",           "az_codes_weight_grad_workspace", "az_logits_policy", "az_logits_policy_workspace",
+           "az_rms_norm", "az_rms_norm_grad", "az_rms_norm_grad_workspace", "az_nibbles_quantize", "az_nibbles_dequantize",
+           "az_nibbles_matmul", "az_nibbles_matmul_workspace", "az_codes_nibbles_matmul", "az_codes_nibbles_matmul_workspace",
+           "az_logits_sample",
            "az_status_string", "az_last_error")
 
 
@@ -66,6 +69,37 @@ class az_logits(ctypes.Structure):
                 ("mask_kind", ctypes.c_int32), ("ld_mask", ctypes.c_int64), ("bias", ctypes.c_void_p),
                 ("ld_bias", ctypes.c_int64), ("history", ctypes.c_void_p), ("ld_history", ctypes.c_int64),
                 ("max_history", ctypes.c_int32), ("lengths", ctypes.c_void_p), ("penalties", ctypes.c_void_p)]
+
+
+AZ_FP4_BLOCK = 32
+
+
+class az_fp4_matrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_scales", ctypes.c_int64)]
+
+
+class az_norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("x", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("ld_x", ctypes.c_int64), ("residual", ctypes.c_void_p),
+                ("ld_residual", ctypes.c_int64), ("weight", ctypes.c_void_p), ("sum", ctypes.c_void_p),
+                ("ld_sum", ctypes.c_int64), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64),
+                ("q", ctypes.POINTER(az_code_matrix))]
+
+
+class az_norm_grad(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dy", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("ld_dy", ctypes.c_int64), ("h", ctypes.c_void_p), ("ld_h", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("dsum", ctypes.c_void_p), ("ld_dsum", ctypes.c_int64),
+                ("dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64), ("dweight", ctypes.c_void_p),
+                ("accumulate", ctypes.c_int32)]
+
+
+class az_sampling(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("ld", ctypes.c_int64), ("u", ctypes.c_void_p),
+                ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
 
 
 class AzError(RuntimeError):
@@ -132,6 +166,20 @@ def lib():
             f.restype = ctypes.c_int
         L.az_codes_weight_grad_workspace.argtypes, L.az_codes_weight_grad_workspace.restype = [I64, I32, I64], SZ
         L.az_logits_policy_workspace.argtypes, L.az_logits_policy_workspace.restype = [I32, I32], SZ
+        N4 = ctypes.POINTER(az_fp4_matrix)
+        L.az_rms_norm.argtypes = [ctypes.POINTER(az_norm), P]
+        L.az_rms_norm_grad.argtypes = [ctypes.POINTER(az_norm_grad), P, SZ, P]
+        L.az_nibbles_quantize.argtypes = [P, I32, I64, N4, N4, P]
+        L.az_nibbles_dequantize.argtypes = [N4, P, I32, I64, P]
+        L.az_nibbles_matmul.argtypes = [N4, N4, P, P, I32, I64, P, SZ, P]
+        L.az_codes_nibbles_matmul.argtypes = [M, N4, P, P, I32, I64, P, SZ, P]
+        L.az_logits_sample.argtypes = [ctypes.POINTER(az_sampling), P, P, P]
+        for f in (L.az_rms_norm, L.az_rms_norm_grad, L.az_nibbles_quantize, L.az_nibbles_dequantize, L.az_nibbles_matmul,
+                  L.az_codes_nibbles_matmul, L.az_logits_sample):
+            f.restype = ctypes.c_int
+        L.az_rms_norm_grad_workspace.argtypes, L.az_rms_norm_grad_workspace.restype = [I64, I64], SZ
+        L.az_nibbles_matmul_workspace.argtypes, L.az_nibbles_matmul_workspace.restype = [N4, N4, I32], SZ
+        L.az_codes_nibbles_matmul_workspace.argtypes, L.az_codes_nibbles_matmul_workspace.restype = [M, N4, I32], SZ
         L.az_debug_fail_allocation.argtypes, L.az_debug_fail_allocation.restype = [I32], None
         L.az_debug_live_allocations.argtypes, L.az_debug_live_allocations.restype = [], ctypes.c_int64
         L.az_status_string.argtypes, L.az_status_string.restype = [ctypes.c_int], ctypes.c_char_p
@@ -363,6 +411,57 @@ def az_logits_policy(logits: az_logits, probabilities: bool, out, ld_out: int, w
     return _check(st, "az_logits_policy") if raise_on_error else st
 
 
+def az_rms_norm(norm: az_norm, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_rms_norm(norm, stream)
+    return _check(st, "az_rms_norm") if raise_on_error else st
+
+
+def az_rms_norm_grad_workspace(rows: int, cols: int) -> int:
+    return int(lib().az_rms_norm_grad_workspace(rows, cols))
+
+
+def az_rms_norm_grad(grad: az_norm_grad, workspace=None, workspace_bytes: int = 0, stream: int = 0,
+                     raise_on_error: bool = True) -> int:
+    st = lib().az_rms_norm_grad(grad, workspace, workspace_bytes, stream)
+    return _check(st, "az_rms_norm_grad") if raise_on_error else st
+
+
+def az_nibbles_quantize(x, dtype: int, ldx: int, q: az_fp4_matrix, qt=None, stream: int = 0,
+                        raise_on_error: bool = True) -> int:
+    st = lib().az_nibbles_quantize(x, dtype, ldx, q, qt, stream)
+    return _check(st, "az_nibbles_quantize") if raise_on_error else st
+
+
+def az_nibbles_dequantize(q: az_fp4_matrix, x, dtype: int, ldx: int, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_nibbles_dequantize(q, x, dtype, ldx, stream)
+    return _check(st, "az_nibbles_dequantize") if raise_on_error else st
+
+
+def az_nibbles_matmul_workspace(a: az_fp4_matrix, b: az_fp4_matrix, dtype: int) -> int:
+    return int(lib().az_nibbles_matmul_workspace(a, b, dtype))
+
+
+def az_nibbles_matmul(a: az_fp4_matrix, b: az_fp4_matrix, bias, out, dtype: int, ld_out: int, workspace=None,
+                      workspace_bytes: int = 0, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_nibbles_matmul(a, b, bias, out, dtype, ld_out, workspace, workspace_bytes, stream)
+    return _check(st, "az_nibbles_matmul") if raise_on_error else st
+
+
+def az_codes_nibbles_matmul_workspace(a: az_code_matrix, b: az_fp4_matrix, dtype: int) -> int:
+    return int(lib().az_codes_nibbles_matmul_workspace(a, b, dtype))
+
+
+def az_codes_nibbles_matmul(a: az_code_matrix, b: az_fp4_matrix, bias, out, dtype: int, ld_out: int, workspace=None,
+                            workspace_bytes: int = 0, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_codes_nibbles_matmul(a, b, bias, out, dtype, ld_out, workspace, workspace_bytes, stream)
+    return _check(st, "az_codes_nibbles_matmul") if raise_on_error else st
+
+
+def az_logits_sample(sampling: az_sampling, out, prob=None, stream: int = 0, raise_on_error: bool = True) -> int:
+    st = lib().az_logits_sample(sampling, out, prob, stream)
+    return _check(st, "az_logits_sample") if raise_on_error else st
+
+
 def _rows_of(name, t, dtypes):
     """(rows, columns, elements from row to row) of a two-dimensional device tensor."""
     if not t.is_cuda or t.dtype not in dtypes or t.dim() != 2:
@@ -417,6 +516,44 @@ class CodeMatrix:
         return cls(codes, scales, cols, scale_rows)
 
 
+class Fp4Matrix:
+    """A matrix of 4-bit e2m1 codes, two to a byte, with a power-of-two scale for each block of 32 columns of a row, on
+    torch device tensors: codes uint8 [rows][bytes], rows a multiple of 16 bytes apart and cols / 2 or
+    more of them, and scales uint8 [rows][ceil(cols / 32) or more], rows a multiple of 4 bytes apart.
+    Keeps its tensors alive."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "device", "c")
+
+    def __init__(self, codes, scales, cols=None):
+        import torch
+        rows, width, ld = _rows_of("codes", codes, (torch.uint8,))
+        srows, swidth, lds = _rows_of("scales", scales, (torch.uint8,))
+        cols = 2 * width if cols is None else int(cols)
+        if not 0 < cols <= 2 * width:
+            raise ValueError(f"cols {cols} is not in 1..{2 * width}")
+        blocks = -(-cols // AZ_FP4_BLOCK)
+        if srows != rows or swidth < blocks:
+            raise ValueError(f"scales {[srows, swidth]} are not [{rows}, {blocks} or more]")
+        if rows <= 1:
+            ld, lds = -(-ld // 16) * 16, -(-lds // 4) * 4
+        if rows and codes.untyped_storage().nbytes() - codes.storage_offset() < (rows - 1) * ld + 16 * blocks:
+            raise ValueError("codes must hold whole chunks of 16 bytes in every row")
+        if rows and scales.untyped_storage().nbytes() - scales.storage_offset() < (rows - 1) * lds + -(-blocks // 4) * 4:
+            raise ValueError("scales must hold whole words of 4 bytes in every row")
+        if scales.device != codes.device:
+            raise ValueError("codes and scales are on different devices")
+        self.codes, self.scales, self.rows, self.cols, self.device = codes, scales, rows, cols, codes.device
+        self.c = az_fp4_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, lds)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda"):
+        """A matrix of these sizes on memory of its own, codes and scales not yet written."""
+        import torch
+        codes = torch.empty((rows, -(-cols // 32) * 16), dtype=torch.uint8, device=device)
+        scales = torch.empty((rows, -(-cols // (4 * AZ_FP4_BLOCK)) * 4), dtype=torch.uint8, device=device)
+        return cls(codes, scales, cols)
+
+
 def _on(device, stream, *others):
     """The call's stream as the library takes it (torch's current one by default), for operands that are all
     on `device`."""
@@ -460,30 +597,35 @@ def _float_type(t) -> int:
     return AZ_BF16 if t.dtype == torch.bfloat16 else AZ_F32
 
 
-def quantize_tensors(x, q: CodeMatrix, transposed: CodeMatrix = None, stream=None) -> int:
-    """az_codes_quantize of x (float32 or bfloat16 [rows][cols]) into q and, for matrices with
-    scale_rows 128, its transposed copy; stream defaults to torch's current one."""
+def quantize_tensors(x, q, transposed=None, stream=None) -> int:
+    """az_codes_quantize of x (float32 or bfloat16 [rows][cols]) into the CodeMatrix q and, for matrices with
+    scale_rows 128, its transposed copy, or az_nibbles_quantize into the Fp4Matrix q and the transposed
+    one; stream defaults to torch's current one."""
     import torch
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
+    if transposed is not None and type(transposed) is not type(q):
+        raise ValueError("the transposed matrix is of another kind")
     s = _on(x.device, stream, q, transposed)
-    return _call(x.device, az_codes_quantize, x.data_ptr(), _float_type(x), ld, q.c,
+    return _call(x.device, az_nibbles_quantize if type(q) is Fp4Matrix else az_codes_quantize, x.data_ptr(), _float_type(x), ld, q.c,
                  transposed.c if transposed is not None else None, s)
 
 
-def dequantize_tensors(q: CodeMatrix, x, stream=None) -> int:
-    """az_codes_dequantize of q into x (float32 or bfloat16 [rows][cols])."""
+def dequantize_tensors(q, x, stream=None) -> int:
+    """az_codes_dequantize (az_nibbles_dequantize) of the CodeMatrix (Fp4Matrix) q into x (float32 or bfloat16
+    [rows][cols])."""
     import torch
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
     s = _on(x.device, stream, q)
-    return _call(x.device, az_codes_dequantize, q.c, x.data_ptr(), _float_type(x), ld, s)
+    return _call(x.device, az_nibbles_dequantize if type(q) is Fp4Matrix else az_codes_dequantize, q.c, x.data_ptr(), _float_type(x), ld, s)
 
 
-def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, workspace=None, stream=None) -> int:
-    """az_codes_matmul: out [a.rows][b.rows] (bfloat16 or float32) = a b^T + bias (float32 [b.rows]).
+def matmul_tensors(a, b, out, bias=None, workspace=None, stream=None) -> int:
+    """out [a.rows][b.rows] (bfloat16 or float32) = a b^T + bias (float32 [b.rows]): az_codes_matmul of two CodeMatrix,
+    az_nibbles_matmul of two Fp4Matrix, az_codes_nibbles_matmul of a CodeMatrix and an Fp4Matrix b.
     A workspace is made for the call (torch's allocator, on the call's stream) unless a tensor is
     given."""
     import torch
@@ -492,9 +634,17 @@ def matmul_tensors(a: CodeMatrix, b: CodeMatrix, out, bias=None, workspace=None,
         raise ValueError(f"out is {[m, n]}, the product {[a.rows, b.rows]}")
     if bias is not None:
         _vector_of("bias", bias, torch.float32, n)
+    if type(b) is not Fp4Matrix:
+        if type(a) is Fp4Matrix:
+            raise ValueError("a 4-bit matrix is multiplied by a 4-bit one")
+        size_of, multiply = az_codes_matmul_workspace, az_codes_matmul
+    elif type(a) is Fp4Matrix:
+        size_of, multiply = az_nibbles_matmul_workspace, az_nibbles_matmul
+    else:
+        size_of, multiply = az_codes_nibbles_matmul_workspace, az_codes_nibbles_matmul
     s, dt = _on(out.device, stream, a, b, bias), _float_type(out)
-    ws, size, keep = _workspace(workspace, az_codes_matmul_workspace(a.c, b.c, dt), out.device, stream)
-    return _call(out.device, az_codes_matmul, a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), dt,
+    ws, size, keep = _workspace(workspace, size_of(a.c, b.c, dt), out.device, stream)
+    return _call(out.device, multiply, a.c, b.c, bias.data_ptr() if bias is not None else None, out.data_ptr(), dt,
                  ld, ws, size, s)
 
 
@@ -563,6 +713,72 @@ def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None
     rows = az_logits(p(logits), _float_type(logits), b, v, ld, p(mask), kind, ldm, p(bias), ldb, p(history), ldh, t,
                      p(lengths), p(penalties))
     return _call(logits.device, az_logits_policy, rows, probabilities, out.data_ptr(), ldo, ws, size, s)
+
+
+def _like(name, t, like, rows, cols):
+    """(pointer, elements from row to row) of an optional matrix of the type and sizes of another."""
+    if t is None:
+        return None, 0
+    r, c, ld = _rows_of(name, t, (like.dtype,))
+    if (r, c) != (rows, cols):
+        raise ValueError(f"{name} is {[r, c]}, not {[rows, cols]}")
+    return t.data_ptr(), ld
+
+
+def norm_tensors(x, y=None, q: CodeMatrix = None, residual=None, sum=None, weight=None, eps: float = 1e-6, stream=None) -> int:
+    """az_rms_norm of x (float32 or bfloat16 [rows][cols]) plus residual, with weight (float32 [cols]), into y and the
+    coded matrix q; sum receives x + residual (it may be either's own tensor).  residual, sum and y are like x."""
+    import torch
+    rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
+    pr, ldr = _like("residual", residual, x, rows, cols)
+    ps, lds = _like("sum", sum, x, rows, cols)
+    py, ldy = _like("y", y, x, rows, cols)
+    if weight is not None:
+        _vector_of("weight", weight, torch.float32, cols)
+    if q is not None and (q.rows, q.cols) != (rows, cols):
+        raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
+    s = _on(x.device, stream, residual, sum, y, weight, q)
+    n = az_norm(rows, cols, x.data_ptr(), _float_type(x), eps, ld, pr, ldr, weight.data_ptr() if weight is not None else None,
+                ps, lds, py, ldy, ctypes.pointer(q.c) if q is not None else None)
+    return _call(x.device, az_rms_norm, n, s)
+
+
+def norm_grad_tensors(dy, h, dx=None, dsum=None, weight=None, dw=None, eps: float = 1e-6, accumulate: bool = False,
+                      workspace=None, stream=None) -> int:
+    """az_rms_norm_grad: dx (the gradient of x and of the residual) and dw (float32 [cols]) from dy and h (float32 or bfloat16
+    [rows][cols]), h the sum that the norm gave; dsum: what else reaches h.  dy, dsum and dx are like
+    h.  A workspace is made for the call (torch's allocator, on the call's stream) unless a tensor is given."""
+    import torch
+    rows, cols, ld = _rows_of("h", h, (torch.float32, torch.bfloat16))
+    pd, ldd = _like("dy", dy, h, rows, cols)
+    pr, ldr = _like("dsum", dsum, h, rows, cols)
+    px, ldx = _like("dx", dx, h, rows, cols)
+    for name, v in (("weight", weight), ("dw", dw)):
+        if v is not None:
+            _vector_of(name, v, torch.float32, cols)
+    s = _on(h.device, stream, dy, dsum, dx, weight, dw)
+    need = az_rms_norm_grad_workspace(rows, cols) if dw is not None else 0
+    ws, size, keep = _workspace(workspace, need, h.device, stream)
+    g = az_norm_grad(rows, cols, pd, _float_type(h), eps, ldd, h.data_ptr(), ld, weight.data_ptr() if weight is not None else None,
+                     pr, ldr, px, ldx, dw.data_ptr() if dw is not None else None, accumulate)
+    return _call(h.device, az_rms_norm_grad, g, ws, size, s)
+
+
+def sample_tensors(logits, u, out, prob=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None) -> int:
+    """az_logits_sample: an entry of each row of logits (float32 or bfloat16 [rows][vocab]) into out (int32 [rows]) and its
+    probability into prob (float32 [rows]), from random numbers u in [0, 1); u, temperature, top_p and min_p
+    float32 [rows], top_k int32 [rows]."""
+    import torch
+    b, v, ld = _rows_of("logits", logits, (torch.float32, torch.bfloat16))
+    for name, t, dtype in (("u", u, torch.float32), ("out", out, torch.int32), ("prob", prob, torch.float32),
+                           ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is not None:
+            _vector_of(name, t, dtype, b)
+    s = _on(logits.device, stream, u, out, prob, temperature, top_k, top_p, min_p)
+    p = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
+    rows = az_sampling(p(logits), _float_type(logits), b, v, ld, p(u), p(temperature), p(top_k), p(top_p), p(min_p))
+    return _call(logits.device, az_logits_sample, rows, p(out), p(prob), s)
 
 
 AZ_PIPE_GRAPHS = 1

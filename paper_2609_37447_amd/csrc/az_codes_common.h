@@ -120,4 +120,126 @@ __device__ __forceinline__ cm_i32x4 code_chunk(const uint8_t* row, int c, int co
 __device__ __forceinline__ uint16_t bf16_of(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 __device__ __forceinline__ float f32_of_bf16(uint32_t bits) { return __uint_as_float(bits << 16); }
 
+constexpr uint32_t INF_BITS = 0x7f800000u;
+
+// Scale byte of a block whose largest finite |x| has these bits: 448 = 1.75 * 2^8, so
+// ceil(log2(a / 448)) is a's exponent less 8, and one more where its significand is past
+// 1.75.  The clamp keeps every value 2^(s - 127) times a code a normal finite float.
+__device__ __forceinline__ int scale_byte(uint32_t a) {
+  if (a == 0) return 127;
+  const int e = (int)(a >> 23) - 127 - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return min(max(e, -117), 119) + 127;
+}
+
+// Four codes of four values.
+__device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) y[i] = __builtin_amdgcn_fmed3f(x[i] * inv, -448.0f, 448.0f);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  uint32_t u = (uint32_t)w;
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    if ((__float_as_uint(x[i]) & INF_BITS) == INF_BITS) u = (u & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
+  return u;
+}
+
+__device__ __forceinline__ uint32_t finite_size(float x) {
+  const uint32_t a = __float_as_uint(x) & 0x7fffffffu;
+  return a >= INF_BITS ? 0u : a;
+}
+
+// 16 elements of a row of `cols` from column c on, as fp32; zero at and past cols.  Memory is read 16
+// bytes at a time at any alignment of the elements; where the row ends before the 16 do, its last
+// 16 are read and moved down, so that no load waits for another.
+template <bool BF16>
+__device__ __forceinline__ void load16(const void* x, int64_t row, int c, int cols, float (&v)[16]) {
+  if (cols >= 16) {
+    const int at = min(c, cols - 16), down = min(c - at, 16);
+    if constexpr (BF16) {
+      cm_i32x4 w[2];
+      __builtin_memcpy(w, (const uint16_t*)x + row + at, 32);
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        v[2 * i] = __uint_as_float((uint32_t)w[i >> 2][i & 3] << 16);
+        v[2 * i + 1] = __uint_as_float((uint32_t)w[i >> 2][i & 3] & 0xffff0000u);
+      }
+    } else {
+      __builtin_memcpy(v, (const float*)x + row + at, 64);
+    }
+    if (down) {
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1)
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+          if (down & s) v[i] = i + s < 16 ? v[(i + s) & 15] : 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      v[i] = 0.0f;
+      if (c + i < cols) {
+        if constexpr (BF16) v[i] = f32_of_bf16(((const uint16_t*)x)[row + c + i]);
+        else v[i] = ((const float*)x)[row + c + i];
+      }
+    }
+  }
+}
+
+// Writes the codes of 16 columns from c on, none past cols.
+__device__ __forceinline__ void store16(uint8_t* row, int c, int cols, const cm_i32x4& w) {
+  uint8_t* to = row + c;
+  const int left = cols - c;
+  if (left >= 16) {
+    *reinterpret_cast<cm_i32x4*>(to) = w;
+  } else if (left > 0) {
+    uint64_t u = (uint32_t)w[0] | (uint64_t)(uint32_t)w[1] << 32;
+    if (left & 8) {
+      *reinterpret_cast<uint64_t*>(to) = u;
+      u = (uint32_t)w[2] | (uint64_t)(uint32_t)w[3] << 32;
+      to += 8;
+    }
+    if (left & 4) {
+      *reinterpret_cast<uint32_t*>(to) = (uint32_t)u;
+      u >>= 32;
+      to += 4;
+    }
+    if (left & 2) {
+      *reinterpret_cast<uint16_t*>(to) = (uint16_t)u;
+      u >>= 16;
+      to += 2;
+    }
+    if (left & 1) *to = (uint8_t)u;
+  }
+}
+
+// Writes 16 values to a dense row from column c on, none past cols.
+template <bool BF16>
+__device__ __forceinline__ void put16(void* x, int64_t row, int c, int cols, const float (&v)[16]) {
+  if constexpr (BF16) {
+    uint16_t* o = (uint16_t*)x + row + c;
+    if (c + 16 <= cols) {
+      cm_i32x4 u[2];
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        u[i >> 2][i & 3] = (int)((uint32_t)bf16_of(v[2 * i]) | ((uint32_t)bf16_of(v[2 * i + 1]) << 16));
+      __builtin_memcpy(o, u, 32);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i++)
+        if (c + i < cols) o[i] = bf16_of(v[i]);
+    }
+  } else {
+    float* o = (float*)x + row + c;
+    if (c + 16 <= cols) {
+      __builtin_memcpy(o, v, 64);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i++)
+        if (c + i < cols) o[i] = v[i];
+    }
+  }
+}
+
 }  // namespace
