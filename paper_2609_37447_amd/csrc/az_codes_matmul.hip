@@ -10,11 +10,9 @@
 //
 // In both, D's rows are the n of b and its columns the m of a, so that a lane holds
 // four neighbouring n of one m and stores them together.
-#include "az_codes_common.h"
+#include "az_matmul_common.h"
 
 namespace {
-
-typedef __attribute__((address_space(3))) uint8_t lds_bytes;
 
 // 32 consecutive codes of a row for K step kb, the operand of a lane (row l % 16,
 // columns 32 (l / 16) on).
@@ -131,19 +129,6 @@ __global__ __launch_bounds__(DW * 64) void az_matmul_direct(CodeView a, CodeView
   }
 }
 
-// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an
-// L2 of its own: an XCD gets a run of neighbouring tiles, in groups of eight rows of
-// tiles, so that the panels that its tiles share are read once into its L2.
-__device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, int& tn) {
-  const uint32_t total = (uint32_t)mt * (uint32_t)nt;
-  const uint32_t xcd = id & 7u, per = total >> 3, more = total & 7u;
-  const uint32_t at = xcd * per + min(xcd, more) + (id >> 3);
-  const uint32_t group = 8u * (uint32_t)nt, g = at / group, in = at - g * group;
-  const uint32_t high = min(8u, (uint32_t)mt - 8u * g);
-  tm = (int)(8u * g + in % high);
-  tn = (int)(in / high);
-}
-
 // More rows of a.  Four waves own a tile of TM rows of a and TN rows of b, WM x WN parts of FA x FB
 // blocks of 32 x 32.  K steps of 128 columns go straight from memory into LDS, two steps in
 // turn (four were no faster); a wave reads fragments of half a step (64 columns) while the
@@ -154,7 +139,7 @@ __device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, in
 // LDS puts lanes side by side, so that the exchange is made on the source address.
 template <int FA_, int FB_, int WM, int WN, bool EXACT>
 struct Tiled {
-  static constexpr int FA = FA_, FB = FB_, TM = 32 * FA * WM, TN = 32 * FB * WN;
+  static constexpr int FA = FA_, FB = FB_, ACROSS = WM, TM = 32 * FA * WM, TN = 32 * FB * WN;
   static constexpr int ASTEP = TM * CB, BSTEP = TN * CB;  // LDS bytes of an operand's step
   static constexpr int SCALES = ASTEP + BSTEP;  // where a word of scale bytes for each row of a, then of b, begins
   static constexpr int SA = TM < 64 ? 64 : TM;  // words of a (a wave copies 64)
@@ -222,19 +207,6 @@ struct Tiled {
       }
     }
   }
-};
-
-// Scale bytes of a matrix as aligned words.  Row r's byte of step kb is byte (start + kb) & 3 of
-// the word that holds it, start = place(r).
-struct ScaleWords {
-  __amdgpu_buffer_rsrc_t words;
-  uint32_t skip;
-  __device__ __forceinline__ explicit ScaleWords(const CodeView& m) {
-    skip = (uint32_t)((uintptr_t)m.scales & 3u);
-    const uint32_t rows = (uint32_t)((m.rows - 1) >> m.shift) + 1u;
-    words = __builtin_amdgcn_make_buffer_rsrc(m.scales - skip, 0, (int)((skip + rows * (uint32_t)m.nb + 3u) & ~3u), 0x00027000);
-  }
-  __device__ __forceinline__ uint32_t place(const CodeView& m, int row) const { return skip + (uint32_t)(row >> m.shift) * (uint32_t)m.nb; }
 };
 
 // 8192^3: 460-482 us (2,280-2,390 TFLOP/s); 333 x 1880 x 10240 with exact products, four parts: 28 us.
@@ -362,76 +334,7 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(Co
       K::multiply(acc, f0, sa, sb);
     }
   }
-  // Results leave through LDS, so that whole rows of the tile are written: a lane's four neighbours
-  // would be 16 bytes of each of 32 rows.  Chunks are exchanged by the row, as above.
-  constexpr int ES = F32 ? 4 : 2, OROW = K::TN * ES, RC = OROW / 16;  // bytes and chunks of a row
-  constexpr int PASSES = K::LDS >= K::TM * OROW ? 1 : 2;  // fp32 of the largest tile: half of each wave's rows at a time
-  constexpr int PF = K::FA / PASSES, PROWS = K::TM / PASSES;
-#pragma unroll
-  for (int p = 0; p < PASSES; p++) {
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < K::FB; j++)
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const int n = wn + 32 * j + 8 * q + 4 * h;
-        float add[4] = {};
-        if (bias) {
-#pragma unroll
-          for (int e = 0; e < 4; e++) add[e] = bias[n0 + min(n + e, ns - 1)];
-        }
-#pragma unroll
-        for (int i = 0; i < PF; i++) {
-          const int row = (wave % WM) * 32 * PF + 32 * i + r;
-          cm_f32x4 v;
-#pragma unroll
-          for (int e = 0; e < 4; e++) v[e] = acc[PF * p + i][j][4 * q + e] + add[e];
-          if constexpr (F32) {
-            *reinterpret_cast<cm_f32x4*>(smem + row * OROW + (((n >> 2) ^ r) * 16)) = v;
-          } else {
-            const cm_i32x2 w = {(int)((uint32_t)bf16_of(v[0]) | ((uint32_t)bf16_of(v[1]) << 16)),
-                                (int)((uint32_t)bf16_of(v[2]) | ((uint32_t)bf16_of(v[3]) << 16))};
-            *reinterpret_cast<cm_i32x2*>(smem + row * OROW + (((n >> 3) ^ (r & (RC - 1))) * 16) + (n & 4) * 2) = w;
-          }
-        }
-      }
-    __syncthreads();
-    uint8_t* const to = (uint8_t*)out + (blockIdx.y * part_stride + (int64_t)m0 * ldo + n0) * ES;
-#pragma unroll 8
-    for (int c = t; c < PROWS * RC; c += 256) {
-      const int row = c / RC, in = c % RC;
-      const cm_i32x4 v = *reinterpret_cast<const cm_i32x4*>(smem + row * OROW + ((in ^ (row & 31 & (RC - 1))) * 16));
-      // rows of the waves lie FA blocks apart
-      const int m = row / (32 * PF) * (32 * K::FA) + p * 32 * PF + row % (32 * PF);
-      const int left = ns * ES - in * 16;  // bytes of the row from here on
-      uint8_t* o = to + (int64_t)m * ldo * ES + in * 16;
-      if (m < ms && left >= 16) {
-        __builtin_memcpy(o, &v, 16);
-      } else if (m < ms && left > 0) {
-#pragma unroll
-        for (int e = 0; e < 16 / ES; e++)
-          if (e * ES < left) {
-            if constexpr (F32) reinterpret_cast<int*>(o)[e] = v[e];
-            else reinterpret_cast<uint16_t*>(o)[e] = (uint16_t)((uint32_t)v[e >> 1] >> (16 * (e & 1)));
-          }
-      }
-    }
-  }
-}
-
-// out from the sums over parts of the columns, in the order of the parts.  Four parts of 333 x 1880: 4.6 us.
-template <bool F32>
-__global__ __launch_bounds__(256) void az_join_products(const float* __restrict__ parts, int count, int m, int n,
-                                                        const float* __restrict__ bias, void* __restrict__ out, int64_t ldo) {
-  const int64_t total = (int64_t)m * n;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    float v = 0.0f;
-    for (int p = 0; p < count; p++) v += parts[p * total + i];
-    const int64_t r = i / n, c = i - r * n;
-    if (bias) v += bias[c];
-    if constexpr (F32) ((float*)out)[r * ldo + c] = v;
-    else ((uint16_t*)out)[r * ldo + c] = bf16_of(v);
-  }
+  write_tile<K, F32>(acc, smem, bias, (uint8_t*)out + (blockIdx.y * part_stride + (int64_t)m0 * ldo + n0) * (F32 ? 4 : 2), ldo, n0, ms, ns, wave, r, h);
 }
 
 // How a product runs: the kernel, and `parts` parts of the columns of part_steps K steps each.

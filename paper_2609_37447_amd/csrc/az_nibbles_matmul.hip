@@ -5,18 +5,20 @@
 // their products (multiples of 1/4 up to 36) are summed exactly.  With an e4m3 operand small products are
 // cut (see the products of two e4m3 matrices), so that fp32 results of a coded a run on the bf16 instruction,
 // for which codes times their scale are exact operands.
+#include "az_matmul_common.h"
 #include "az_nibbles_common.h"
 
 namespace {
 
 enum { E4M3 = 0, E2M1 = 4 };  // the instruction's format numbers
 
-// Either kind of the left operand.
+// Either kind of the left operand: scale_row(r) begins row r's scale bytes, one for each 32 (e2m1) or 128 columns.
 struct LeftView {
-  const uint8_t* codes;
-  const uint8_t* scales;
+  uint8_t* codes;
+  uint8_t* scales;
   int64_t ld, ld_scales;
   int rows, cols, shift;
+  __device__ __forceinline__ const uint8_t* scale_row(int64_t r) const { return scales + (r >> shift) * ld_scales; }
 };
 
 // A lane's 32 columns of step k (128 columns), zeros past cols.  The 16 x 16 x 128 instruction has lane group g's
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleVi
   const int m0 = (int)(blockIdx.x / (uint32_t)nt) * 16, n0 = (int)(blockIdx.x % (uint32_t)nt) * 16;
   const int64_t am = min((int64_t)m0 + r, (int64_t)a.rows - 1), bn = min((int64_t)n0 + r, (int64_t)b.rows - 1);
   const uint8_t *ar = a.codes + am * a.ld, *br = b.codes + bn * b.ld;
-  const uint8_t *as = a.scales + (am >> a.shift) * a.ld_scales, *bs = b.scales + bn * b.ld_scales;
+  const uint8_t *as = a.scale_row(am), *bs = b.scales + bn * b.ld_scales;
   const int blocks = (a.cols + NB - 1) / NB, steps = (blocks + 3) / 4;
   cm_f32x4 acc = {0, 0, 0, 0};
   for (int k = wave; k < steps; k += DW) {
@@ -95,12 +97,320 @@ __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleVi
   }
 }
 
+// More rows of a.  Four waves own a tile of TM rows of a and TN rows of b, WM x WN parts of FA x FB blocks of 32 x 32.
+// A K step is 128 bytes of a row of a: 256 columns in 4 bits, 128 in e4m3 (64 bytes of b).  Steps go straight from memory into
+// LDS, two in turn; a wave reads the fragments of the next 64 columns while the matrix unit works on these.
+//
+// LDS rows' 16-byte chunks are exchanged by the row's place (chunk ^ (row / 2) % chunks), which spreads the
+// rows that are read together over all banks; the copy into LDS puts lanes side by side, so that the exchange is
+// made on the source address.
+template <int A, int FA_, int FB_, int WM, int WN, bool EXACT, bool F32>
+struct Tiled {
+  static constexpr int FA = FA_, FB = FB_, ACROSS = WM, TM = 32 * FA * WM, TN = 32 * FB * WN;
+  static constexpr int STEP = A == E2M1 ? 256 : 128, SUBS = STEP / 64;  // columns, and matrix instructions a block
+  static constexpr int BROW = STEP / 2;                                 // bytes of a row of b; a's are 128
+  static constexpr int ASTEP = TM * 128, BSTEP = TN * BROW;
+  static constexpr int AW = A == E2M1 ? 2 : 1, BW = STEP / 128;         // words of scale bytes of a row
+  static constexpr int SA = TM < 64 ? 64 : TM;                          // a wave copies 64 rows' words
+  static constexpr int SCALES = ASTEP + BSTEP, WORDS = SA * AW + TN * BW;
+  static constexpr int STAGE = SCALES + WORDS * 4;
+  static constexpr int OUT = TM * TN * (F32 ? 4 : 2) / (FA > 1 ? 2 : 1);  // what results need on their way out
+  static constexpr int LDS = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+  static constexpr int AROWS = 32, BROWS = 4096 / BROW;                 // rows that one copy instruction of the workgroup fills
+  static constexpr int TURNS = (WORDS / 64 + 3) / 4;
+  static_assert(WM * WN == 4 && WORDS % 64 == 0 && TM % AROWS == 0 && TN % BROWS == 0, "four waves' work");
+
+  struct Frag {
+    cm_i32x8 a[FA], b[FB];
+  };
+
+  template <int CHUNKS, int ROWS, int ROW>
+  static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, int ld, uint32_t off, int at, lds_bytes* to) {
+#pragma unroll
+    for (int j = 0; j < CHUNKS; j++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * ROWS * ROW, 16, off, at + j * ROWS * ld, 0, 0);
+  }
+  // Spreads LDS reads and copies over the matrix instructions of 64 columns, reads first.
+  template <bool LAST>
+  static __device__ __forceinline__ void interleave() {
+    if constexpr (!EXACT) {
+#pragma unroll
+      for (int i = 0; i < FA * FB; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
+        if (i < FA + FB) __builtin_amdgcn_sched_group_barrier(0x100, LAST ? 3 : A == E2M1 ? 1 : 2, 0);  // LDS reads
+        else if (LAST) __builtin_amdgcn_sched_group_barrier(0x020, 3, 0);                               // copies
+      }
+    }
+  }
+  // Chunks of a's fragment of 64 columns s: 32 columns of e4m3 are two, where the instruction wants them (16 h and
+  // 32 + 16 h on); for the bf16 instruction they follow each other, as b's.
+  static __device__ __forceinline__ int a_chunk(int s, int h, int i) {
+    return A == E2M1 ? 2 * s + h : EXACT ? 4 * s + 2 * h + i : 4 * s + 2 * i + h;
+  }
+  template <int S>
+  static __device__ __forceinline__ void read(Frag& f, const uint8_t* ap, const uint8_t* bp, int h, int sa, int sb) {
+    const int c0 = (a_chunk(S, h, 0) ^ sa) * 16, c1 = (a_chunk(S, h, 1) ^ sa) * 16, cb = ((2 * S + h) ^ sb) * 16;
+#pragma unroll
+    for (int i = 0; i < FA; i++) {
+      const cm_i32x4 x = *reinterpret_cast<const cm_i32x4*>(ap + i * 32 * 128 + c0);
+      cm_i32x4 y = {};
+      if constexpr (A == E4M3) y = *reinterpret_cast<const cm_i32x4*>(ap + i * 32 * 128 + c1);
+      f.a[i] = cm_i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    }
+#pragma unroll
+    for (int j = 0; j < FB; j++) {
+      const cm_i32x4 x = *reinterpret_cast<const cm_i32x4*>(bp + j * 32 * BROW + cb);
+      f.b[j] = cm_i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+    }
+  }
+  // 64 columns; the scale bytes are byte OA of sa and byte OB of sb.
+  template <int OA, int OB>
+  static __device__ __forceinline__ void multiply(cm_f32x16 (&acc)[FA][FB], const Frag& f, const uint32_t (&sa)[FA], const uint32_t (&sb)[FB]) {
+    if constexpr (!EXACT) {
+#pragma unroll
+      for (int i = 0; i < FA; i++)
+#pragma unroll
+        for (int j = 0; j < FB; j++)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j], f.a[i], acc[i][j], E2M1, A, OB, (int)sb[j], OA, (int)sa[i]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        cm_bf16x8 va[FA], vb[FB];
+#pragma unroll
+        for (int i = 0; i < FA; i++) va[i] = values8<A>(f.a[i], q, scale_value((sa[i] >> (8 * OA)) & 0xffu));
+#pragma unroll
+        for (int j = 0; j < FB; j++) vb[j] = values8<E2M1>(f.b[j], q, scale_value((sb[j] >> (8 * OB)) & 0xffu));
+#pragma unroll
+        for (int i = 0; i < FA; i++)
+#pragma unroll
+          for (int j = 0; j < FB; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[j], va[i], acc[i][j], 0, 0, 0);
+      }
+    }
+  }
+};
+
+template <int A, int FA, int FB, int WM, int WN, bool EXACT, bool F32>
+__global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_nibble_tiled(LeftView a, NibbleView b, const float* __restrict__ bias,
+                                                                              void* __restrict__ out, int64_t ldo, int mt, int nt,
+                                                                              int part_steps, int64_t part_stride) {
+  using K = Tiled<A, FA, FB, WM, WN, EXACT, F32>;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  int tm, tn;
+  tile_of(blockIdx.x, mt, nt, tm, tn);
+  // The last tile of a side ends with the matrix: what it shares with the tile before is computed
+  // twice, to the same bits.  A matrix of fewer rows than a tile is the one tile's beginning.
+  const int m0 = max(min(tm * K::TM, a.rows - K::TM), 0), n0 = max(min(tn * K::TN, b.rows - K::TN), 0);
+  const int ms = min(a.rows, K::TM), ns = min(b.rows, K::TN);
+
+  // Copying: a lane takes one chunk of one row of those that an instruction of its wave fills.  Rows past the
+  // matrix are out of the buffer's range and read as zeros.
+  const int arow = 8 * wave + (lane >> 3), achunk = (lane & 7) ^ ((arow >> 1) & 7);
+  constexpr int BC = K::BROW / 16;  // chunks of a row of b
+  const int brow = K::BROWS / 4 * wave + lane / BC, bchunk = (lane % BC) ^ ((brow >> 1) & (BC - 1));
+  const uint32_t aoff = (uint32_t)arow * (uint32_t)a.ld + achunk * 16, boff = (uint32_t)brow * (uint32_t)b.ld + bchunk * 16;
+  const int blocks = (a.cols + NB - 1) / NB, awidth = A == E2M1 ? blocks * 16 : (a.cols + 15) & ~15;
+  const __amdgpu_buffer_rsrc_t abuf = __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, (ms - 1) * (int)a.ld + awidth, 0x00027000);
+  const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, (ns - 1) * (int)b.ld + blocks * 16, 0x00027000);
+  lds_bytes* const alds = (lds_bytes*)smem + 8 * wave * 128;
+  lds_bytes* const blds = (lds_bytes*)smem + K::ASTEP + K::BROWS / 4 * wave * K::BROW;
+  // The part's steps, of which `whole` is the first that does not fill its columns or is not the part's.
+  const int first = (int)blockIdx.y * part_steps, last = min(first + part_steps, (a.cols + K::STEP - 1) / K::STEP), whole = min(last, a.cols / K::STEP);
+  // Scales, by words, 64 a wave and turn: the first words of a's rows, their second ones, then b's.  Rows of 4-bit scales are whole
+  // words; of e4m3 ones, ScaleWords has the word that holds the byte.
+  const CodeView codes = {a.codes, a.scales, a.ld, a.rows, a.cols, (int)a.ld_scales, a.shift};
+  const ScaleWords aw(codes);
+  const __amdgpu_buffer_rsrc_t awords = A == E2M1 ? __builtin_amdgcn_make_buffer_rsrc(a.scales + m0 * a.ld_scales, 0, (ms - 1) * (int)a.ld_scales + ((blocks + 3) & ~3), 0x00027000) : aw.words;
+  const __amdgpu_buffer_rsrc_t bwords = __builtin_amdgcn_make_buffer_rsrc(b.scales + n0 * b.ld_scales, 0, (ns - 1) * (int)b.ld_scales + ((blocks + 3) & ~3), 0x00027000);
+  uint32_t srow[K::TURNS];
+#pragma unroll
+  for (int i = 0; i < K::TURNS; i++) {
+    const int w = i * 256 + t;
+    if (w < K::SA * K::AW) {
+      const int row = min(w % K::SA, ms - 1);
+      srow[i] = A == E2M1 ? (uint32_t)row * (uint32_t)a.ld_scales + 4 * (w / K::SA) : aw.place(codes, m0 + row);
+    } else {
+      const int v = w - K::SA * K::AW;
+      srow[i] = (uint32_t)min(v % K::TN, ns - 1) * (uint32_t)b.ld_scales + 4 * (v / K::TN);
+    }
+  }
+  lds_bytes* const slds = (lds_bytes*)smem + K::SCALES + wave * 64 * 4;
+  // (past the last step: that step again, which nothing reads)
+  auto fetch = [&](int kb) {
+    const int stage = (kb & 1) * K::STAGE;
+    kb = min(kb, whole - 1);
+    K::template copy<K::TM / K::AROWS, K::AROWS, 128>(abuf, (int)a.ld, aoff, kb * 128, alds + stage);
+    K::template copy<K::TN / K::BROWS, K::BROWS, K::BROW>(bbuf, (int)b.ld, boff, kb * K::BROW, blds + stage);
+#pragma unroll
+    for (int i = 0; i < K::TURNS; i++)
+      if (K::WORDS % 256 == 0 || i * 4 + wave < K::WORDS / 64) {
+        if (i * 4 + wave < K::SA * K::AW / 64)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(awords, slds + stage + i * 1024, 4, A == E2M1 ? srow[i] + 8 * kb : (srow[i] + kb) & ~3u, 0, 0, 0);
+        else
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(bwords, slds + stage + i * 1024, 4, srow[i] + 4 * K::BW * kb, 0, 0, 0);
+      }
+  };
+
+  // Reading: a lane holds row l % 32 of a block, its block of 32 columns l / 32.
+  const int r = lane & 31, h = lane >> 5, wm = (wave % WM) * 32 * FA, wn = (wave / WM) * 32 * FB;
+  const int sa_ = (r >> 1) & 7, sb_ = (r >> 1) & (BC - 1);
+  const uint8_t* ap = smem + (wm + r) * 128;
+  const uint8_t* bp = smem + K::ASTEP + (wn + r) * K::BROW;
+  uint32_t ac[FA];  // e4m3: eight times the places of the lane's rows' scales
+#pragma unroll
+  for (int i = 0; i < FA; i++) ac[i] = A == E2M1 ? 0 : 8 * aw.place(codes, m0 + min(wm + 32 * i + r, ms - 1));
+  // A 4-bit operand's words are moved down by its lane's byte, so that 64 columns s have theirs at byte 2 (s % 2) of word s / 2.
+  uint32_t sa[K::AW][FA], sb[K::BW][FB], na[K::AW][FA], nb[K::BW][FB];
+  auto scale_words = [&](int kb) {
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(smem + (kb & 1) * K::STAGE + K::SCALES) + r;
+#pragma unroll
+    for (int w = 0; w < K::AW; w++)
+#pragma unroll
+      for (int i = 0; i < FA; i++) na[w][i] = from[w * K::SA + wm + 32 * i];
+#pragma unroll
+    for (int w = 0; w < K::BW; w++)
+#pragma unroll
+      for (int j = 0; j < FB; j++) nb[w][j] = from[K::SA * K::AW + w * K::TN + wn + 32 * j];
+  };
+  auto scales = [&](int kb) {
+#pragma unroll
+    for (int w = 0; w < K::AW; w++)
+#pragma unroll
+      for (int i = 0; i < FA; i++) sa[w][i] = na[w][i] >> (A == E2M1 ? 8 * h : (int)((ac[i] + 8 * kb) & 31));
+#pragma unroll
+    for (int w = 0; w < K::BW; w++)
+#pragma unroll
+      for (int j = 0; j < FB; j++) sb[w][j] = nb[w][j] >> (8 * h);
+  };
+
+  cm_f32x16 acc[FA][FB];
+#pragma unroll
+  for (int i = 0; i < FA; i++)
+#pragma unroll
+    for (int j = 0; j < FB; j++) acc[i][j] = cm_f32x16{};
+  typename K::Frag f[2];
+  if (whole > first) {
+    const int stage = (first & 1) * K::STAGE;
+    fetch(first);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    fetch(first + 1);
+    scale_words(first);
+    scales(first);
+    K::template read<0>(f[0], ap + stage, bp + stage, h, sa_, sb_);
+  }
+  constexpr bool FOUR = A == E2M1;
+  for (int kb = first; kb < whole; kb++) {
+    const int stage = (kb & 1) * K::STAGE, next = K::STAGE - stage;
+    K::template read<1>(f[1], ap + stage, bp + stage, h, sa_, sb_);
+    K::template multiply<0, 0>(acc, f[0], sa[0], sb[0]);
+    K::template interleave<false>();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (K::SUBS == 4) {
+      K::template read<2>(f[0], ap + stage, bp + stage, h, sa_, sb_);
+      K::template multiply<2, 2>(acc, f[1], sa[0], sb[0]);
+      K::template interleave<false>();
+      __builtin_amdgcn_sched_barrier(0);
+      K::template read<3>(f[1], ap + stage, bp + stage, h, sa_, sb_);
+      K::template multiply<0, 0>(acc, f[0], sa[K::AW - 1], sb[K::BW - 1]);
+      K::template interleave<false>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // This wave's reads of step kb are done and its copies of step kb + 1 have landed; after the
+    // barrier that holds for every wave.
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    // (after the last step these are the bytes of the step before: read, not used)
+    K::template read<0>(f[0], ap + next, bp + next, h, sa_, sb_);
+    scale_words(kb + 1);
+    fetch(kb + 2);
+    K::template multiply<FOUR ? 2 : 0, 2>(acc, f[1], sa[K::AW - 1], sb[K::BW - 1]);
+    K::template interleave<true>();
+    scales(kb + 1);
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // no copy into LDS is under way when the workgroup ends
+  if (whole < last) {  // the columns that do not fill a step, straight from memory
+    for (int s = 0; s < K::SUBS; s++) {
+      const int kb = whole * (K::STEP / NB) + 2 * s + h, at = min(kb, blocks - 1);  // (past cols: zeros, with the last block's scale)
+      uint32_t ta[FA], tb[FB];
+#pragma unroll
+      for (int i = 0; i < FA; i++) {
+        const int64_t row = m0 + min(wm + 32 * i + r, ms - 1);
+        ta[i] = a.scale_row(row)[FOUR ? at : whole];
+        if constexpr (FOUR) {
+          const cm_i32x4 x = nibble_chunk(a.codes + row * a.ld, kb, a.cols);
+          f[0].a[i] = cm_i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+        } else {
+          const cm_i32x4 x = code_chunk(a.codes + row * a.ld, whole * CB + 16 * K::a_chunk(s, h, 0), a.cols);
+          const cm_i32x4 y = code_chunk(a.codes + row * a.ld, whole * CB + 16 * K::a_chunk(s, h, 1), a.cols);
+          f[0].a[i] = cm_i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < FB; j++) {
+        const int64_t row = n0 + min(wn + 32 * j + r, ns - 1);
+        tb[j] = b.scales[row * b.ld_scales + at];
+        const cm_i32x4 x = nibble_chunk(b.codes + row * b.ld, kb, a.cols);
+        f[0].b[j] = cm_i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+      }
+      K::template multiply<0, 0>(acc, f[0], ta, tb);
+    }
+  }
+  write_tile<K, F32>(acc, smem, bias, (uint8_t*)out + (blockIdx.y * part_stride + (int64_t)m0 * ldo + n0) * (F32 ? 4 : 2), ldo, n0, ms, ns, wave, r, h);
+}
+
+// How a product runs: the kernel, and `parts` parts of the columns of part_steps K steps each.
+enum { DIRECT = 0, TILE32 = 1, TILE64 = 2, TILE128 = 3, TILE256 = 4 };
+struct Plan {
+  int kind, parts, part_steps;
+};
+
+// What a product multiplies with: two 4-bit operands, an e4m3 one on the scaled instruction, or on the bf16 one.
+enum Mode { FOURS = 0, MIXED = 1, EXACT = 2 };
+
+// The plan with the least estimated time, in microseconds; a tile kernel's K step takes a workgroup `one` alone on a
+// compute unit and `all` with `occ` of them there.
+Plan choose_plan(int64_t m, int64_t n, int64_t k, Mode mode, bool f32, bool fits) {
+  struct Tile {
+    int kind, tm, tn, occ;
+    double one[3], all[3];
+  };
+  static const Tile tiles[] = {{TILE32, 32, 128, 3, {0.53, 0.53, 0.55}, {0.70, 0.70, 0.80}},
+                               {TILE64, 64, 128, 3, {0.60, 0.60, 0.63}, {0.87, 0.87, 1.35}},
+                               {TILE128, 128, 128, 2, {0.69, 0.69, 0.80}, {0.90, 0.90, 1.50}},
+                               {TILE256, 256, 256, 1, {1.45, 1.45, 2.75}, {1.72, 1.72, 3.30}}};
+  const int columns = mode == FOURS ? 256 : 128, nb = (int)((k + columns - 1) / columns);
+  const double write = 1.0 / 4.5e6;  // microseconds a byte
+  const double out = (double)m * (double)n * (f32 ? 4 : 2) * write;
+  auto rounds = [](int64_t groups, int64_t slots) { return (double)((groups + slots - 1) / slots); };
+  Plan best = {DIRECT, 1, nb};
+  // eight waves take every eighth step of 128 columns each
+  double least = 3.0 + rounds((n + 15) / 16 * ((m + 15) / 16), 256) * ((k + 127) / 128 / 8.0 * 0.55 + 0.6) + out;
+  if (!fits) return best;
+  for (const Tile& t : tiles) {
+    const int64_t count = ((m + t.tm - 1) / t.tm) * ((n + t.tn - 1) / t.tn);
+    for (int parts = 1; parts <= 8 && (parts == 1 || 2 * parts <= nb); parts *= 2) {
+      const int64_t groups = count * parts, per = (groups + 255) / 256;
+      const int steps = (nb + parts - 1) / parts;
+      const int occ = per < t.occ ? (int)per : t.occ;
+      const double step = t.occ == 1 ? (per > 1 ? t.all[mode] : t.one[mode]) : t.one[mode] + (t.all[mode] - t.one[mode]) * (occ - 1) / (t.occ - 1);
+      double cost = 4.0 + rounds(groups, 256 * t.occ) * (steps * step + 2.0) + out;
+      if (parts > 1) cost += 3.5 + (double)parts * (double)m * (double)n * 8 * write;
+      if (cost < least) {
+        least = cost;
+        best = {t.kind, (nb + steps - 1) / steps, steps};
+      }
+    }
+  }
+  return best;
+}
+
 struct Operands {
   LeftView a;
   NibbleView b;
   const float* bias;
   void* out;
-  int64_t ldo;
+  int64_t ldo, part_stride;
   hipStream_t stream;
 };
 
@@ -112,24 +422,103 @@ int launch_direct(const Operands& o) {
   return AZ_OK;
 }
 
-int matmul(const LeftView& a, int format, const az_fp4_matrix& b, const float* bias, void* out, int32_t dtype, int64_t ld_out,
+template <int A, int FA, int FB, int WM, int WN, bool EXACT, bool F32>
+int launch_tiled(const Plan& p, const Operands& o) {
+  using K = Tiled<A, FA, FB, WM, WN, EXACT, F32>;
+  const int64_t mt = ((int64_t)o.a.rows + K::TM - 1) / K::TM, nt = ((int64_t)o.b.rows + K::TN - 1) / K::TN;
+  if (!grid_fits(mt * nt, 256)) return AZ_ERR_UNSUPPORTED;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(az_nibble_tiled<A, FA, FB, WM, WN, EXACT, F32>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS);
+  if (e != hipSuccess) return AZ_ERR_DEVICE;
+  hipLaunchKernelGGL((az_nibble_tiled<A, FA, FB, WM, WN, EXACT, F32>), dim3((unsigned)(mt * nt), p.parts), dim3(256), K::LDS, o.stream,
+                     o.a, o.b, o.bias, o.out, o.ldo, (int)mt, (int)nt, p.part_steps, o.part_stride);
+  return AZ_OK;
+}
+
+template <int A, bool EXACT, bool F32>
+int launch_tiles(const Plan& p, const Operands& o) {
+  return p.kind == TILE256   ? launch_tiled<A, 4, 4, 2, 2, EXACT, F32>(p, o)
+         : p.kind == TILE128 ? launch_tiled<A, 2, 2, 2, 2, EXACT, F32>(p, o)
+         : p.kind == TILE64  ? launch_tiled<A, 1, 2, 2, 2, EXACT, F32>(p, o)
+                             : launch_tiled<A, 1, 1, 1, 4, EXACT, F32>(p, o);
+}
+
+// A tile's offsets stay below 2^30.
+bool tile_fits(const LeftView& a, const NibbleView& b) {
+  constexpr int64_t most = 1 << 22;
+  return a.ld < most && a.ld_scales < most && b.ld < most && b.ld_scales < most;
+}
+
+Plan plan_of(const LeftView& a, const NibbleView& b, int format, int32_t dtype) {
+  return choose_plan(a.rows, b.rows, a.cols, format == E2M1 ? FOURS : dtype == AZ_F32 ? EXACT : MIXED, dtype == AZ_F32, tile_fits(a, b));
+}
+
+size_t workspace_of(const LeftView& a, const NibbleView& b, int format, int32_t dtype) {
+  const Plan p = plan_of(a, b, format, dtype);
+  return p.parts > 1 ? (size_t)p.parts * (size_t)a.rows * (size_t)b.rows * sizeof(float) : 0;
+}
+
+// The product by its plan, out or the parts' fp32 sums.  F32 of MIXED operands is for parts only: whole fp32 results are EXACT.
+int run_plan(const Plan& p, const Operands& o, int format, bool exact, bool f32) {
+  if (p.kind == DIRECT) {
+    if (format == E2M1) return f32 ? launch_direct<E2M1, false, true>(o) : launch_direct<E2M1, false, false>(o);
+    return f32 ? launch_direct<E4M3, true, true>(o) : launch_direct<E4M3, false, false>(o);
+  }
+  if (format == E2M1) return f32 ? launch_tiles<E2M1, false, true>(p, o) : launch_tiles<E2M1, false, false>(p, o);
+  if (exact) return launch_tiles<E4M3, true, true>(p, o);
+  return f32 ? launch_tiles<E4M3, false, true>(p, o) : launch_tiles<E4M3, false, false>(p, o);
+}
+
+int matmul(const LeftView& a, int format, const NibbleView& b, const float* bias, void* out, int32_t dtype, int64_t ld_out,
            void* workspace, size_t workspace_bytes, void* stream, const char* who) {
+  if (a.cols != b.cols) return code_fail(AZ_ERR_INVALID_ARG, who, "a and b differ in cols");
   if (dtype != AZ_F32 && dtype != AZ_BF16) return code_fail(AZ_ERR_INVALID_ARG, who, "dtype is neither AZ_F32 nor AZ_BF16");
   if (a.rows == 0 || b.rows == 0) return AZ_OK;
-  const int st = dense_check(out, dtype, ld_out, b.rows, who);
+  int st = dense_check(out, dtype, ld_out, b.rows, who);
   if (st != AZ_OK) return st;
   if ((uintptr_t)bias & 3u) return code_fail(AZ_ERR_INVALID_ARG, who, "bias must be 4-byte aligned");
-  if (a.ld >= (1 << 27) || b.ld >= (1 << 27) || b.ld_scales >= (1 << 26)) return code_fail(AZ_ERR_UNSUPPORTED, who, "rows of 2^27 bytes or scales of 2^26 or more");
-  const Operands o = {a, nibble_view(b), bias, out, ld_out, static_cast<hipStream_t>(stream)};
+  if (a.ld >= (1 << 27) || b.ld >= (1 << 27) || (format == E2M1 && a.ld_scales >= (1 << 26)) || b.ld_scales >= (1 << 26))
+    return code_fail(AZ_ERR_UNSUPPORTED, who, "rows of 2^27 bytes or scales of 2^26 or more");
+  const size_t need = workspace_of(a, b, format, dtype);
+  if (workspace_bytes < need || (need && !workspace)) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace is too small");
+  if ((uintptr_t)workspace & 15u) return code_fail(AZ_ERR_INVALID_ARG, who, "the workspace must be 16-byte aligned");
+  const Plan p = plan_of(a, b, format, dtype);
+  const bool f32 = dtype == AZ_F32;
+  Operands o = {a, b, bias, out, ld_out, 0, static_cast<hipStream_t>(stream)};
   (void)hipGetLastError();
-  if (format == E2M1) return launched(who, dtype == AZ_F32 ? launch_direct<E2M1, false, true>(o) : launch_direct<E2M1, false, false>(o));
-  return launched(who, dtype == AZ_F32 ? launch_direct<E4M3, true, true>(o) : launch_direct<E4M3, false, false>(o));
+  if (p.parts == 1) return launched(who, run_plan(p, o, format, f32, f32));
+  o.bias = nullptr;
+  o.out = workspace;
+  o.ldo = b.rows;
+  o.part_stride = (int64_t)a.rows * b.rows;
+  if ((st = launched(who, run_plan(p, o, format, f32, true))) != AZ_OK) return st;
+  const int64_t groups = (o.part_stride + 255) / 256;
+  const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
+  const float* parts = static_cast<const float*>(workspace);
+  if (f32) hipLaunchKernelGGL((az_join_products<true>), g, dim3(256), 0, o.stream, parts, p.parts, a.rows, b.rows, bias, out, ld_out);
+  else hipLaunchKernelGGL((az_join_products<false>), g, dim3(256), 0, o.stream, parts, p.parts, a.rows, b.rows, bias, out, ld_out);
+  return launch_status(who);
 }
+
+LeftView left_view(const az_fp4_matrix& a) { return LeftView{a.codes, a.scales, a.ld, a.ld_scales, (int)a.rows, (int)a.cols, 0}; }
+LeftView left_view(const az_code_matrix& a) {
+  const CodeView c = code_view(a);
+  return LeftView{c.codes, c.scales, c.ld, c.nb, c.rows, c.cols, c.shift};
+}
+
+// Whether sizes have a workspace to ask for: those that a call takes.
+template <class Matrix>
+bool sized(const Matrix* m) { return m && m->rows > 0 && m->cols > 0 && code_sizes(m->rows, m->cols); }
 
 }  // namespace
 
-extern "C" size_t az_nibbles_matmul_workspace(const az_fp4_matrix*, const az_fp4_matrix*, int32_t) { return 0; }
-extern "C" size_t az_codes_nibbles_matmul_workspace(const az_code_matrix*, const az_fp4_matrix*, int32_t) { return 0; }
+extern "C" size_t az_nibbles_matmul_workspace(const az_fp4_matrix* a, const az_fp4_matrix* b, int32_t dtype) {
+  return sized(a) && sized(b) ? workspace_of(left_view(*a), nibble_view(*b), E2M1, dtype) : 0;
+}
+
+extern "C" size_t az_codes_nibbles_matmul_workspace(const az_code_matrix* a, const az_fp4_matrix* b, int32_t dtype) {
+  return sized(a) && sized(b) ? workspace_of(left_view(*a), nibble_view(*b), E4M3, dtype) : 0;
+}
 
 extern "C" int az_nibbles_matmul(const az_fp4_matrix* a, const az_fp4_matrix* b, const float* bias, void* out, int32_t dtype,
                                  int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
@@ -137,10 +526,7 @@ extern "C" int az_nibbles_matmul(const az_fp4_matrix* a, const az_fp4_matrix* b,
   int st = nibble_check(a, who);
   if (st == AZ_OK) st = nibble_check(b, who);
   if (st != AZ_OK) return st;
-  if (a->cols != b->cols) return code_fail(AZ_ERR_INVALID_ARG, who, "a and b differ in cols");
-  if (a->ld_scales >= (1 << 26)) return code_fail(AZ_ERR_UNSUPPORTED, who, "scales of 2^26 bytes or more a row");
-  const LeftView v = {a->codes, a->scales, a->ld, a->ld_scales, (int)a->rows, (int)a->cols, 0};
-  return matmul(v, E2M1, *b, bias, out, dtype, ld_out, workspace, workspace_bytes, stream, who);
+  return matmul(left_view(*a), E2M1, nibble_view(*b), bias, out, dtype, ld_out, workspace, workspace_bytes, stream, who);
 }
 
 extern "C" int az_codes_nibbles_matmul(const az_code_matrix* a, const az_fp4_matrix* b, const float* bias, void* out, int32_t dtype,
@@ -149,8 +535,5 @@ extern "C" int az_codes_nibbles_matmul(const az_code_matrix* a, const az_fp4_mat
   int st = code_check(a, who);
   if (st == AZ_OK) st = nibble_check(b, who);
   if (st != AZ_OK) return st;
-  if (a->cols != b->cols) return code_fail(AZ_ERR_INVALID_ARG, who, "a and b differ in cols");
-  const CodeView c = code_view(*a);
-  const LeftView v = {c.codes, c.scales, c.ld, c.nb, c.rows, c.cols, c.shift};
-  return matmul(v, E4M3, *b, bias, out, dtype, ld_out, workspace, workspace_bytes, stream, who);
+  return matmul(left_view(*a), E4M3, nibble_view(*b), bias, out, dtype, ld_out, workspace, workspace_bytes, stream, who);
 }
