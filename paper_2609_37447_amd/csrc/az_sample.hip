@@ -3,10 +3,12 @@
 // All three keep a beginning of the entries in the order of falling logits (equal ones by rising index): nothing
 // is sorted, only the last entry that stays is looked for.  A weight exp((l - largest) / T) is a whole
 // multiple of 2^-S, so that sums of weights are exact whole numbers in any order, and LDS atomics may build
-// them: a histogram over a key (the logit's distance from the largest, its bits, or the index) says in which
-// of its bins the wanted sum is reached, and that bin is cut up in turn until it is one key.
+// them.  A histogram over the distance from the largest says in which bin the wanted count or sum is reached; if
+// few entries are in it, their order among each other is found by comparing all with all, otherwise the bin
+// is cut up by the logits' bits until it is few, or one value.  The draw is the same over the index.
 //
-// One workgroup a row.  Where what may stay fits LDS it is copied there, and the rest is done without memory.
+// One workgroup a row: the row is read for its largest logit, for the histogram, and a third time for what may
+// stay, which is copied to LDS where it fits: the rest is done without memory.
 #include <math.h>
 
 #include "az_codes_common.h"
@@ -39,35 +41,50 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 }
 constexpr uint32_t NONE = 0x007fffffu;  // the key of -inf: what is not above it is not allowed
 
-// Whole weights.
+// 2^f in f ln 2 by the Taylor series to the twelfth power, |f| <= 1/2: 1.7e-16.
+__device__ __forceinline__ double power_of_two(double f) {
+  const double t = f * 0.6931471805599453;
+  double x = 1.0 / 479001600;
+  x = fma(x, t, 1.0 / 39916800);
+  x = fma(x, t, 1.0 / 3628800);
+  x = fma(x, t, 1.0 / 362880);
+  x = fma(x, t, 1.0 / 40320);
+  x = fma(x, t, 1.0 / 5040);
+  x = fma(x, t, 1.0 / 720);
+  x = fma(x, t, 1.0 / 120);
+  x = fma(x, t, 1.0 / 24);
+  x = fma(x, t, 1.0 / 6);
+  x = fma(x, t, 0.5);
+  x = fma(x, t, 1.0);
+  return fma(x, t, 1.0);
+}
+
+// Whole weights: exp((l - top) / T) 2^S by 2^(e + S) 2^(j / 32) 2^f, 0 <= j < 32, |f| <= 1/64, with a table of 2^(j / 32) and the
+// Taylor series of 2^f to its fifth power (2.3e-15).
+constexpr int PARTS = 32;
 struct Weights {
-  double top, inv, floor;
+  double top, scale, floor;  // scale: 32 log2(e) / T; floor: min-p times 2^S
+  const double* table;
   int shift;
-  // exp((l - top) / T) by 2^n 2^f, |f| <= 1/2, and the Taylor series of 2^f in f ln 2 to its twelfth power (1.7e-16).
-  __device__ __forceinline__ double of(float l) const {
-    const double y = fmax(((double)l - top) * inv * 1.4426950408889634, -1100.0), n = rint(y), t = (y - n) * 0.6931471805599453;
-    double x = 1.0 / 479001600;
-    x = fma(x, t, 1.0 / 39916800);
-    x = fma(x, t, 1.0 / 3628800);
-    x = fma(x, t, 1.0 / 362880);
-    x = fma(x, t, 1.0 / 40320);
-    x = fma(x, t, 1.0 / 5040);
-    x = fma(x, t, 1.0 / 720);
-    x = fma(x, t, 1.0 / 120);
-    x = fma(x, t, 1.0 / 24);
-    x = fma(x, t, 1.0 / 6);
-    x = fma(x, t, 0.5);
-    x = fma(x, t, 1.0);
-    x = fma(x, t, 1.0);
-    return ldexp(x, (int)n);
+  // exp((l - top) / T) 2^S; what is below 2^-64 (-inf too) counts as that
+  __device__ __forceinline__ double scaled(float l) const {
+    constexpr double ROUND = 0x1.8p52, LN = 0.6931471805599453 / PARTS;
+    const double y = fmax(((double)l - top) * scale, -64.0 * PARTS), m = y + ROUND, f = y - (m - ROUND);
+    const int n = (int)__double_as_longlong(m);  // the nearest whole number to y
+    double x = LN * LN * LN * LN * LN / 120;
+    x = fma(x, f, LN * LN * LN * LN / 24);
+    x = fma(x, f, LN * LN * LN / 6);
+    x = fma(x, f, LN * LN / 2);
+    x = fma(x, f, LN);
+    x = fma(x, f, 1.0) * table[n & (PARTS - 1)];
+    return __longlong_as_double(__double_as_longlong(x) + ((int64_t)((n >> 5) + shift) << 52));
   }
-  __device__ __forceinline__ uint64_t whole(double x) const {
-    return (uint64_t)__double_as_longlong(ldexp(x, shift) + 0x1p52) & 0xfffffffffffffull;  // rounded by the addition
+  static __device__ __forceinline__ uint64_t whole(double x) {
+    return (uint64_t)__double_as_longlong(x + 0x1p52) & 0xfffffffffffffull;  // rounded by the addition
   }
-  __device__ __forceinline__ uint64_t operator()(uint32_t key) const { return key > NONE ? whole(of(value_of(key))) : 0; }
-  __device__ __forceinline__ uint64_t above_floor(uint32_t key) const {
-    if (key <= NONE) return 0;
-    const double x = of(value_of(key));
+  __device__ __forceinline__ uint64_t operator()(float l) const { return whole(scaled(l)); }
+  __device__ __forceinline__ uint64_t above_floor(float l) const {
+    const double x = scaled(l);
     return x >= floor ? whole(x) : 0;
   }
 };
@@ -81,31 +98,24 @@ struct Last {
 
 template <int NT>
 struct Sampler {
-  static constexpr int BINS = 2 * NT, LIST = 4 * NT;
+  static constexpr int BINS = 2 * NT, LIST = NT < 1024 ? 8 * NT : 4 * NT, FEW = 256, SLOTS = 64;
   uint64_t sums[BINS];
-  uint32_t counts[BINS];
-  uint2 list[LIST];  // key, index
+  uint64_t few_order[FEW];   // of the entries that are compared with each other: what orders them,
+  uint64_t few_weight[FEW];  // and their weights
+  uint64_t slots[SLOTS];
   uint64_t waves[NT / 64];
   uint64_t found[3];  // of a search: the bin (BINS: none), the sum before it, the bin's own
   uint64_t total;
-  uint32_t wave_counts[NT / 64];
-  uint32_t before_count;
-  uint32_t length;
+  double table[PARTS];
+  uint32_t counts[BINS];
+  uint2 list[LIST];  // logit, index
+  uint32_t length, few;
   float wave_top[NT / 64];
+  uint32_t wave_allowed[NT / 64];
   int wave_bad[NT / 64];
+  int token;
 
-  __device__ __forceinline__ void clear() {
-    __syncthreads();
-    for (int i = threadIdx.x; i < BINS; i += NT) {
-      sums[i] = 0;
-      counts[i] = 0;
-    }
-    __syncthreads();
-  }
-  __device__ __forceinline__ void add(int bin, uint64_t w) {
-    if (w) atomicAdd(reinterpret_cast<unsigned long long*>(&sums[bin]), (unsigned long long)w);
-  }
-  // The sum of all bins before thread t's two, and of everything into `total`.
+  // The sum of all threads' values before thread t's, and of all of them into `total` (after the next barrier).
   __device__ __forceinline__ uint64_t scan(uint64_t own) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint64_t s = own;
@@ -125,46 +135,47 @@ struct Sampler {
   }
 };
 
-// A row in memory, eight entries a thread at a time.
+// A row in memory.  A thread takes eight entries at a time, AHEAD of which are on their way together.
 template <bool BF16, int NT>
 struct RowSource {
+  static constexpr int AHEAD = BF16 ? 4 : 2, WORDS = BF16 ? 4 : 8;
   const void* row;
   int vocab;
+  __device__ __forceinline__ void load(int i, uint32_t (&w)[WORDS]) const {
+    __builtin_memcpy(w, (const uint8_t*)row + (int64_t)i * (BF16 ? 2 : 4), WORDS * 4);
+  }
+  static __device__ __forceinline__ float entry(const uint32_t (&w)[WORDS], int j) {
+    return __uint_as_float(!BF16 ? w[j & (WORDS - 1)] : j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+  }
+  __device__ __forceinline__ float single(int i) const {
+    return BF16 ? f32_of_bf16(((const uint16_t*)row)[i]) : ((const float*)row)[i];
+  }
   // f(index, logit) for the entries lo..hi - 1
   template <class F>
   __device__ __forceinline__ void each(int lo, int hi, F&& f) const {
-    for (int64_t i0 = (int64_t)(lo & ~7) + threadIdx.x * 8; i0 < hi; i0 += NT * 8) {
-      const int i = (int)i0;
-      float l[8];
-      if (i + 8 <= vocab) {
-        if constexpr (BF16) {
-          cm_i32x4 w;
-          __builtin_memcpy(&w, (const uint16_t*)row + i, 16);
+    int64_t i0 = (int64_t)(lo & ~7) + threadIdx.x * 8;
+    for (; i0 + (AHEAD - 1) * NT * 8 + 8 <= hi; i0 += AHEAD * NT * 8) {
+      uint32_t w[AHEAD][WORDS];
 #pragma unroll
-          for (int j = 0; j < 4; j++) {
-            l[2 * j] = __uint_as_float((uint32_t)w[j] << 16);
-            l[2 * j + 1] = __uint_as_float((uint32_t)w[j] & 0xffff0000u);
-          }
-        } else {
-          __builtin_memcpy(l, (const float*)row + i, 32);
-        }
-      } else {
+      for (int a = 0; a < AHEAD; a++) load((int)i0 + a * NT * 8, w[a]);
+#pragma unroll
+      for (int a = 0; a < AHEAD; a++)
 #pragma unroll
         for (int j = 0; j < 8; j++)
-          l[j] = i + j >= vocab ? -INFINITY : BF16 ? f32_of_bf16(((const uint16_t*)row)[i + j]) : ((const float*)row)[i + j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; j++)
-        if (i + j >= lo && i + j < hi) f(i + j, l[j]);
+          if ((int)i0 + a * NT * 8 + j >= lo) f((int)i0 + a * NT * 8 + j, entry(w[a], j));
     }
-  }
-  template <class F>
-  __device__ __forceinline__ void keys(F&& f) const {
-    each(0, vocab, [&](int i, float l) { f(i, key_of(l)); });
-  }
-  template <class F>
-  __device__ __forceinline__ void keys(int lo, int hi, F&& f) const {
-    each(lo, hi, [&](int i, float l) { f(i, key_of(l)); });
+    for (; i0 < hi; i0 += NT * 8) {
+      const int i = (int)i0;
+      if (i + 8 <= vocab) {
+        uint32_t w[WORDS];
+        load(i, w);
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          if (i + j >= lo && i + j < hi) f(i + j, entry(w, j));
+      } else {
+        for (int j = max(i, lo); j < hi; j++) f(j, single(j));
+      }
+    }
   }
 };
 
@@ -173,15 +184,20 @@ struct ListSource {
   const uint2* list;
   uint32_t length;
   template <class F>
-  __device__ __forceinline__ void keys(F&& f) const {
-    for (uint32_t i = threadIdx.x; i < length; i += NT) f((int)list[i].y, list[i].x);
+  __device__ __forceinline__ void each(int lo, int hi, F&& f) const {
+    for (uint32_t n = threadIdx.x; n < length; n += NT) {
+      const int i = (int)list[n].y;
+      if (i >= lo && i < hi) f(i, __uint_as_float(list[n].x));
+    }
   }
-  template <class F>
-  __device__ __forceinline__ void keys(int lo, int hi, F&& f) const {
-    keys([&](int i, uint32_t k) {
-      if (i >= lo && i < hi) f(i, k);
-    });
-  }
+};
+
+// Where a limit is reached: a bin of the distance from the largest, what is left of the limit in it, and the entries in it
+// and up to its end.
+struct Reached {
+  int bin;
+  uint64_t limit;
+  uint32_t entries, upto;
 };
 
 template <bool BF16, int NT>
@@ -193,32 +209,37 @@ struct Row {
   float top, step;  // step: bins of distance a unit of the logit
   uint32_t top_key;
 
-  // The first bin at which the running sum of the bins reaches `limit` (> 0): what `found` holds afterwards.
-  __device__ __forceinline__ void reach(uint64_t limit) {
+  __device__ __forceinline__ void clear(bool count) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::BINS; i += NT) {
+      s.sums[i] = 0;
+      if (count) s.counts[i] = 0;
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ void add(int bin, uint64_t w) {
+    atomicAdd(reinterpret_cast<unsigned long long*>(&s.sums[bin]), (unsigned long long)w);
+  }
+  // The first bin at which the running sum of the bins reaches limit(their whole sum) (> 0), into `found`.
+  template <class L>
+  __device__ __forceinline__ void reach(L&& limit_of) {
     __syncthreads();
     const int t = threadIdx.x;
     const uint64_t a = s.sums[2 * t], b = s.sums[2 * t + 1];
     if (t == 0) s.found[0] = S::BINS;
     const uint64_t before = s.scan(a + b);
+    __syncthreads();
+    const uint64_t limit = limit_of(s.total);
     if (before < limit && limit <= before + a + b) {
       const bool first = limit <= before + a;
       s.found[0] = 2 * t + (first ? 0 : 1);
-      s.found[1] = first ? before : before + a;
+      s.found[1] = limit - (first ? before : before + a);
       s.found[2] = first ? a : b;
     }
     __syncthreads();
   }
-  __device__ __forceinline__ uint64_t whole_sum() {
-    __syncthreads();
-    s.scan(s.sums[2 * threadIdx.x] + s.sums[2 * threadIdx.x + 1]);
-    __syncthreads();
-    return s.total;
-  }
   // Bin of a logit by its distance from the largest; the last bin holds what has no weight.
-  __device__ __forceinline__ int bin_of(float l) const {
-    const float d = top - l;
-    return d == 0.0f ? 0 : (int)fminf(d * step, (float)(S::BINS - 1));
-  }
+  __device__ __forceinline__ int bin_of(float l) const { return (int)fminf((top - l) * step, (float)(S::BINS - 1)); }
   // The keys of a bin: bin_of falls as the key rises.
   __device__ __forceinline__ void bin_keys(int bin, uint32_t& lo, uint32_t& hi) const {
     auto first_at_most = [&](int b) {  // the smallest key whose bin is at most b
@@ -234,113 +255,264 @@ struct Row {
     hi = bin == 0 ? top_key : first_at_most(bin - 1) - 1;
   }
 
-  // The index at which the running sum of w(index, key), by rising index, reaches `limit`.
-  template <class Src, class W>
-  __device__ __forceinline__ int by_index(const Src& src, uint64_t limit, W&& w) {
-    int lo = 0, hi = p.vocab, shift = 0;
-    while (((hi - 1) >> shift) >= S::BINS) shift++;
-    for (;;) {
-      s.clear();
-      src.keys(lo, hi, [&](int i, uint32_t k) { s.add((i - lo) >> shift, w(i, k)); });
-      reach(limit);
-      const int bin = (int)s.found[0];
-      limit -= s.found[1];
-      lo += bin << shift;
-      if (shift == 0) return lo;
-      hi = min(hi, lo + (1 << shift));
-      shift = 0;
+  // The index at which the running sum of w(index, logit), by rising index, reaches limit(their whole sum), and that sum.
+  template <class Src, class W, class L>
+  __device__ __forceinline__ int by_index(const Src& src, W&& w, L&& limit_of, uint64_t& all) {
+    int lo = 0, hi = p.vocab;
+    uint64_t limit = 0;
+    bool known = false;  // the limit
+    auto limit_now = [&](uint64_t sum) { return known ? limit : limit_of(sum); };
+    while (hi - lo > S::SLOTS) {
+      int shift = 0;
       while (((hi - lo - 1) >> shift) >= S::BINS) shift++;
+      clear(false);
+      int bin = 0;  // neighbours go to the same bin together
+      uint64_t sum = 0;
+      src.each(lo, hi, [&](int i, float l) {
+        const uint64_t x = w(i, l);
+        const int to = (i - lo) >> shift;
+        if (to != bin) {
+          if (sum) add(bin, sum);
+          bin = to;
+          sum = 0;
+        }
+        sum += x;
+      });
+      if (sum) add(bin, sum);
+      reach(limit_now);
+      if (!known) all = s.total;
+      known = true;
+      limit = s.found[1];
+      lo += (int)s.found[0] << shift;
+      hi = min(hi, lo + (1 << shift));
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::SLOTS; i += NT) s.slots[i] = 0;
+    __syncthreads();
+    src.each(lo, hi, [&](int i, float l) { s.slots[i - lo] = w(i, l); });
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const uint64_t own = s.slots[threadIdx.x];
+      uint64_t sum = own;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint64_t x = __shfl_up((unsigned long long)sum, o);
+        if ((int)threadIdx.x >= o) sum += x;
+      }
+      const uint64_t whole = __shfl((unsigned long long)sum, 63), want = limit_now(whole);
+      if (sum - own < want && want <= sum) s.token = lo + (int)threadIdx.x;
+      if (threadIdx.x == 0) s.total = whole;
+    }
+    __syncthreads();
+    if (!known) all = s.total;
+    return s.token;
   }
 
-  // The last entry that stays where entries do as long as the sum of w(key) before them is below `limit`, among
-  // those that `last` keeps; lo..hi: keys that it is among, `limit` less what is above them.
-  template <class Src, class W>
-  __device__ __forceinline__ Last by_key(const Src& src, Last last, uint32_t lo, uint32_t hi, uint64_t limit, W&& w) {
+  // The last entry that stays where entries do as long as the sum of the weights (COUNT: the number) of those before it is below
+  // the limit, in two steps: the bin that it is in, among what `last` keeps,
+  template <bool COUNT, class Src, class L>
+  __device__ __forceinline__ Reached find_bin(const Src& src, Last last, L&& limit_of) {
+    clear(!COUNT);
+    src.each(0, p.vocab, [&](int i, float l) {
+      const int bin = bin_of(l);
+      if (bin < S::BINS - 1 && last.keeps(key_of(l), i)) {
+        add(bin, COUNT ? 1 : weight(l));
+        if (!COUNT) atomicAdd(&s.counts[bin], 1u);
+      }
+    });
+    reach(limit_of);
+    Reached r;
+    r.bin = (int)s.found[0];
+    r.limit = s.found[1];
+    if (r.bin == S::BINS) return r;
+    if constexpr (COUNT) {
+      r.entries = (uint32_t)s.found[2];
+      r.upto = (uint32_t)(limit_of(0) - r.limit) + r.entries;
+    } else {
+      r.entries = s.counts[r.bin];
+      const int t = threadIdx.x;
+      s.scan((2 * t <= r.bin ? s.counts[2 * t] : 0) + (2 * t + 1 <= r.bin ? s.counts[2 * t + 1] : 0));
+      __syncthreads();
+      r.upto = (uint32_t)s.total;
+    }
+    return r;
+  }
+  // and the entry in it.
+  template <bool COUNT, class Src>
+  __device__ __forceinline__ Last find_last(const Src& src, Last last, const Reached& r) {
+    auto w = [&](float l) -> uint64_t { return COUNT ? 1 : weight(l); };
+    if (r.entries <= S::FEW)
+      return find_among(src, r.limit, [&](int i, float l) { return bin_of(l) == r.bin && last.keeps(key_of(l), i); }, w);
+    uint32_t lo, hi;
+    bin_keys(r.bin, lo, hi);
+    uint64_t limit = r.limit;
     for (;;) {
       int shift = 0;
       while (((hi - lo) >> shift) >= (uint32_t)S::BINS) shift++;
-      s.clear();
-      src.keys([&](int i, uint32_t k) {
-        if (k >= lo && k <= hi && last.keeps(k, i)) s.add((int)((hi - k) >> shift), w(k));
+      clear(true);
+      src.each(0, p.vocab, [&](int i, float l) {
+        const uint32_t k = key_of(l);
+        if (k >= lo && k <= hi && last.keeps(k, i)) {
+          add((int)((hi - k) >> shift), w(l));
+          atomicAdd(&s.counts[(hi - k) >> shift], 1u);
+        }
       });
-      reach(limit);
-      if (s.found[0] == (uint64_t)S::BINS) return last;  // everything stays
-      limit -= s.found[1];
-      const uint64_t bin = s.found[0], own = s.found[2];
-      hi -= (uint32_t)(bin << shift);
+      reach([&](uint64_t) { return limit; });
+      const uint32_t bin = (uint32_t)s.found[0], entries = s.counts[bin];
+      limit = s.found[1];
+      hi -= bin << shift;
       lo = hi - lo >= (1u << shift) ? hi - ((1u << shift) - 1) : lo;
-      if (lo == hi) {
-        const uint64_t one = w(lo), ties = own / one, stay = (limit + one - 1) / one;
-        if (stay >= ties) return Last{lo, lo == last.key ? last.index : 0x7fffffff};
+      if (entries <= S::FEW)
+        return find_among(src, limit, [&](int i, float l) { const uint32_t k = key_of(l); return k >= lo && k <= hi && last.keeps(k, i); }, w);
+      if (lo == hi) {  // equal logits: the number of them that stay, by rising index
+        const uint64_t one = s.found[2] / entries, stay = (limit + one - 1) / one;
+        uint64_t all;
         const uint32_t key = lo;
-        return Last{key, by_index(src, stay, [&](int i, uint32_t k) -> uint64_t { return k == key && last.keeps(k, i); })};
+        return Last{key, by_index(src, [&](int i, float l) -> uint64_t { return key_of(l) == key && last.keeps(key, i); },
+                                  [&](uint64_t) { return stay; }, all)};
       }
     }
   }
+  // Of at most FEW entries in(index, logit), by comparing all with all.
+  template <class Src, class In, class W>
+  __device__ __forceinline__ Last find_among(const Src& src, uint64_t limit, In&& in, W&& w) {
+    __syncthreads();
+    if (threadIdx.x == 0) s.few = 0;
+    __syncthreads();
+    src.each(0, p.vocab, [&](int i, float l) {
+      if (in(i, l)) {
+        const uint32_t at = atomicAdd(&s.few, 1u);
+        s.few_order[at] = (uint64_t)key_of(l) << 32 | (uint32_t)~i;
+        s.few_weight[at] = w(l);
+      }
+    });
+    __syncthreads();
+    const int n = (int)s.few;
+    if ((int)threadIdx.x < n) {
+      const uint64_t me = s.few_order[threadIdx.x];
+      uint64_t before = 0;
+      for (int i = 0; i < n; i++) before += s.few_order[i] > me ? s.few_weight[i] : 0;
+      if (before < limit && limit <= before + s.few_weight[threadIdx.x]) s.found[0] = me;
+    }
+    __syncthreads();
+    const uint64_t got = s.found[0];
+    return Last{(uint32_t)(got >> 32), (int)~(uint32_t)got};
+  }
 
-  // Draws among what `last` keeps.
+  // Copies in(index, logit), at most LIST entries, to LDS.
+  template <class Src, class In>
+  __device__ __forceinline__ ListSource<NT> gather(const Src& src, In&& in) {
+    __syncthreads();
+    if (threadIdx.x == 0) s.length = 0;
+    __syncthreads();
+    src.each(0, p.vocab, [&](int i, float l) {
+      if (in(i, l)) s.list[atomicAdd(&s.length, 1u)] = make_uint2(__float_as_uint(l), (uint32_t)i);
+    });
+    __syncthreads();
+    return ListSource<NT>{s.list, s.length};
+  }
+
+  // The entry that u falls on, among what `last` keeps.
   template <class Src>
   __device__ __forceinline__ void draw(const Src& src, Last last, float u, int64_t b) {
-    auto w = [&](int i, uint32_t k) -> uint64_t { return last.keeps(k, i) ? weight.above_floor(k) : 0; };
-    // the whole sum, over bins that mean nothing
-    s.clear();
-    uint64_t own = 0;
-    src.keys([&](int i, uint32_t k) { own += w(i, k); });
-    s.scan(own);
-    __syncthreads();
-    const uint64_t all = s.total;
-    const uint64_t target = min((uint64_t)((double)u * (double)all), all - 1);
-    const int token = by_index(src, target + 1, w);
+    uint64_t all = 0;
+    const int token = by_index(
+        src, [&](int i, float l) -> uint64_t { return last.keeps(key_of(l), i) ? weight.above_floor(l) : 0; },
+        [&](uint64_t sum) { return min((uint64_t)((double)u * (double)sum), sum - 1) + 1; }, all);
     if (threadIdx.x == 0) {
       p.out[b] = token;
       if (p.prob) {
         const float l = BF16 ? f32_of_bf16(((const uint16_t*)p.logits)[b * p.ld + token]) : ((const float*)p.logits)[b * p.ld + token];
-        p.prob[b] = (float)((double)weight(key_of(l)) / (double)all);
+        p.prob[b] = (float)((double)weight(l) / (double)all);
       }
     }
   }
 
-  // Top-p, min-p and the draw among what `last` keeps.
-  template <class Src>
-  __device__ __forceinline__ void rest(const Src& src, Last last, float top_p, float u, int64_t b) {
-    if (top_p < 1.0f) {
-      s.clear();
-      uint64_t own = 0;
-      src.keys([&](int i, uint32_t k) { own += last.keeps(k, i) ? weight(k) : 0; });
-      s.scan(own);
-      __syncthreads();
-      const uint64_t limit = (uint64_t)fmax(ceil((double)top_p * (double)s.total), 1.0);
-      last = by_key(src, last, NONE + 1, top_key, limit, [&](uint32_t k) { return weight(k); });
+  __device__ __forceinline__ auto number(int k) const {
+    return [k](uint64_t) { return (uint64_t)k; };
+  }
+  __device__ __forceinline__ auto share(float top_p) const {
+    return [top_p](uint64_t sum) { return (uint64_t)fmax(ceil((double)top_p * (double)sum), 1.0); };
+  }
+
+  // Filters and draw.  `allowed` entries are above -inf.
+  __device__ __forceinline__ void run(const RowSource<BF16, NT>& row, uint32_t allowed, int k, float top_p, float u, int64_t b) {
+    Last last = {NONE + 1, 0x7fffffff};
+    if (allowed <= S::LIST) {
+      const auto list = gather(row, [&](int, float l) { return l > -INFINITY; });
+      if (k < p.vocab) {
+        const Reached r = find_bin<true>(list, last, number(k));
+        if (r.bin < S::BINS) last = find_last<true>(list, last, r);
+      }
+      if (top_p < 1.0f) {
+        const Reached r = find_bin<false>(list, last, share(top_p));
+        last = find_last<false>(list, last, r);
+      }
+      draw(list, last, u, b);
+      return;
     }
-    draw(src, last, u, b);
+    if (k < p.vocab) {
+      const Reached r = find_bin<true>(row, last, number(k));
+      if (r.bin < S::BINS && r.upto <= S::LIST) {
+        const auto list = gather(row, [&](int, float l) { return bin_of(l) <= r.bin; });
+        last = find_last<true>(list, last, r);
+        if (top_p < 1.0f) {
+          const Reached q = find_bin<false>(list, last, share(top_p));
+          last = find_last<false>(list, last, q);
+        }
+        draw(list, last, u, b);
+        return;
+      }
+      if (r.bin < S::BINS) last = find_last<true>(row, last, r);
+    }
+    if (top_p < 1.0f) {
+      const Reached r = find_bin<false>(row, last, share(top_p));
+      if (r.upto <= S::LIST) {
+        const auto list = gather(row, [&](int i, float l) { return bin_of(l) <= r.bin && last.keeps(key_of(l), i); });
+        draw(list, find_last<false>(list, last, r), u, b);
+        return;
+      }
+      last = find_last<false>(row, last, r);
+    }
+    draw(row, last, u, b);
   }
 };
 
 template <bool BF16, int NT>
-__global__ __launch_bounds__(NT) void az_sample_rows(SampleView p) {
+__global__ __launch_bounds__(NT, 4) void az_sample_rows(SampleView p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   Sampler<NT>& s = *reinterpret_cast<Sampler<NT>*>(smem);
   const int64_t b = blockIdx.x;
   const RowSource<BF16, NT> src = {(const uint8_t*)p.logits + b * p.ld * (BF16 ? 2 : 4), p.vocab};
   float top = -INFINITY;
   bool bad = false;
+  uint32_t allowed = 0;
   src.each(0, p.vocab, [&](int, float l) {
     top = fmaxf(top, l);
     bad |= !(l < INFINITY);
+    allowed += l > -INFINITY;
   });
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  for (int o = 32; o > 0; o >>= 1) {
+    top = fmaxf(top, __shfl_xor(top, o));
+    allowed += __shfl_xor(allowed, o);
+  }
   bad = __any(bad);
   if ((threadIdx.x & 63) == 0) {
     s.wave_top[threadIdx.x >> 6] = top;
+    s.wave_allowed[threadIdx.x >> 6] = allowed;
     s.wave_bad[threadIdx.x >> 6] = bad;
   }
+  if (threadIdx.x < PARTS) {
+    const double f = (double)threadIdx.x / PARTS;
+    s.table[threadIdx.x] = f < 0.5 ? power_of_two(f) : 2.0 * power_of_two(f - 1.0);
+  }
   __syncthreads();
+  allowed = 0;
   for (int w = 0; w < NT / 64; w++) {
     top = fmaxf(top, s.wave_top[w]);
+    allowed += s.wave_allowed[w];
     bad |= s.wave_bad[w] != 0;
   }
-  if (bad || top == -INFINITY) {
+  if (bad || allowed == 0) {
     if (threadIdx.x == 0) {
       p.out[b] = -1;
       if (p.prob) p.prob[b] = 0.0f;
@@ -348,14 +520,15 @@ __global__ __launch_bounds__(NT) void az_sample_rows(SampleView p) {
     return;
   }
   const float t = p.temperature ? p.temperature[b] : 1.0f;
-  const uint32_t top_key = key_of(top);
   const bool greedy = !(t > 0.0f);
   const float step = greedy ? 1.0f : fminf((float)Sampler<NT>::BINS / REACH / t, 0x1p100f);
   float floor = p.min_p ? p.min_p[b] : 0.0f;
   floor = floor > 0.0f ? fminf(floor, 1.0f) : 0.0f;
-  Row<BF16, NT> row = {s, p, {(double)top, greedy ? 1.0 : 1.0 / (double)t, (double)floor, p.shift}, top, step, top_key};
+  Row<BF16, NT> row = {s, p, {(double)top, greedy ? 1.0 : 46.166241308446828 / (double)t, ldexp((double)floor, p.shift), s.table, p.shift},
+                       top, step, key_of(top)};
   if (greedy) {
-    const int token = row.by_index(src, 1, [&](int, uint32_t k) -> uint64_t { return k == top_key; });
+    uint64_t all;
+    const int token = row.by_index(src, [&](int, float l) -> uint64_t { return l == top; }, row.number(1), all);
     if (threadIdx.x == 0) {
       p.out[b] = token;
       if (p.prob) p.prob[b] = 1.0f;
@@ -367,9 +540,7 @@ __global__ __launch_bounds__(NT) void az_sample_rows(SampleView p) {
   const float top_p = p.top_p && p.top_p[b] < 1.0f ? p.top_p[b] : 1.0f;
   float u = p.u[b];
   u = u > 0.0f ? fminf(u, 1.0f) : 0.0f;
-  Last last = {NONE + 1, 0x7fffffff};
-  if (k < p.vocab) last = row.by_key(src, last, NONE + 1, top_key, (uint64_t)k, [&](uint32_t) -> uint64_t { return 1; });
-  row.rest(src, last, top_p, u, b);
+  row.run(src, allowed, k, top_p, u, b);
 }
 
 template <bool BF16, int NT>
@@ -401,5 +572,6 @@ extern "C" int az_logits_sample(const az_sampling* in, int32_t* out, float* prob
                         shift < 51 ? shift : 51};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  if (in->vocab <= 8192) return launched(who, in->dtype == AZ_BF16 ? launch<true, 256>(p, s) : launch<false, 256>(p, s));
   return launched(who, in->dtype == AZ_BF16 ? launch<true, 1024>(p, s) : launch<false, 1024>(p, s));
 }
