@@ -84,7 +84,7 @@ class az_norm(ctypes.Structure):
                 ("eps", ctypes.c_float), ("ld_x", ctypes.c_int64), ("residual", ctypes.c_void_p),
                 ("ld_residual", ctypes.c_int64), ("weight", ctypes.c_void_p), ("sum", ctypes.c_void_p),
                 ("ld_sum", ctypes.c_int64), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64),
-                ("q", ctypes.POINTER(az_code_matrix))]
+                ("q", ctypes.c_void_p)]  # address of an az_code_matrix
 
 
 class az_norm_grad(ctypes.Structure):
@@ -715,13 +715,14 @@ def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None
     return _call(logits.device, az_logits_policy, rows, probabilities, out.data_ptr(), ldo, ws, size, s)
 
 
-def _like(name, t, like, rows, cols):
-    """(pointer, elements from row to row) of an optional matrix of the type and sizes of another."""
+def _like(name, t, like, rows, cols, ld):
+    """(pointer, elements from row to row) of an optional matrix of the type and sizes of another, whose rows are ld apart."""
     if t is None:
         return None, 0
-    r, c, ld = _rows_of(name, t, (like.dtype,))
-    if (r, c) != (rows, cols):
-        raise ValueError(f"{name} is {[r, c]}, not {[rows, cols]}")
+    if t.dtype != like.dtype or t.shape != like.shape or t.stride() != like.stride() or not t.is_cuda:
+        r, c, ld = _rows_of(name, t, (like.dtype,))
+        if (r, c) != (rows, cols):
+            raise ValueError(f"{name} is {[r, c]}, not {[rows, cols]}")
     return t.data_ptr(), ld
 
 
@@ -730,16 +731,16 @@ def norm_tensors(x, y=None, q: CodeMatrix = None, residual=None, sum=None, weigh
     coded matrix q; sum receives x + residual (it may be either's own tensor).  residual, sum and y are like x."""
     import torch
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
-    pr, ldr = _like("residual", residual, x, rows, cols)
-    ps, lds = _like("sum", sum, x, rows, cols)
-    py, ldy = _like("y", y, x, rows, cols)
+    pr, ldr = _like("residual", residual, x, rows, cols, ld)
+    ps, lds = _like("sum", sum, x, rows, cols, ld)
+    py, ldy = _like("y", y, x, rows, cols, ld)
     if weight is not None:
         _vector_of("weight", weight, torch.float32, cols)
     if q is not None and (q.rows, q.cols) != (rows, cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
     s = _on(x.device, stream, residual, sum, y, weight, q)
     n = az_norm(rows, cols, x.data_ptr(), _float_type(x), eps, ld, pr, ldr, weight.data_ptr() if weight is not None else None,
-                ps, lds, py, ldy, ctypes.pointer(q.c) if q is not None else None)
+                ps, lds, py, ldy, ctypes.addressof(q.c) if q is not None else None)
     return _call(x.device, az_rms_norm, n, s)
 
 
@@ -750,9 +751,9 @@ def norm_grad_tensors(dy, h, dx=None, dsum=None, weight=None, dw=None, eps: floa
     h.  A workspace is made for the call (torch's allocator, on the call's stream) unless a tensor is given."""
     import torch
     rows, cols, ld = _rows_of("h", h, (torch.float32, torch.bfloat16))
-    pd, ldd = _like("dy", dy, h, rows, cols)
-    pr, ldr = _like("dsum", dsum, h, rows, cols)
-    px, ldx = _like("dx", dx, h, rows, cols)
+    pd, ldd = _like("dy", dy, h, rows, cols, ld)
+    pr, ldr = _like("dsum", dsum, h, rows, cols, ld)
+    px, ldx = _like("dx", dx, h, rows, cols, ld)
     for name, v in (("weight", weight), ("dw", dw)):
         if v is not None:
             _vector_of(name, v, torch.float32, cols)

@@ -150,41 +150,54 @@ __device__ __forceinline__ uint32_t finite_size(float x) {
   return a >= INF_BITS ? 0u : a;
 }
 
-// 16 elements of a row of `cols` from column c on, as fp32; zero at and past cols.  Memory is read 16
-// bytes at a time at any alignment of the elements; where the row ends before the 16 do, its last
-// 16 are read and moved down, so that no load waits for another.
-template <bool BF16>
-__device__ __forceinline__ void load16(const void* x, int64_t row, int c, int cols, float (&v)[16]) {
-  if (cols >= 16) {
-    const int at = min(c, cols - 16), down = min(c - at, 16);
-    if constexpr (BF16) {
-      cm_i32x4 w[2];
-      __builtin_memcpy(w, (const uint16_t*)x + row + at, 32);
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        v[2 * i] = __uint_as_float((uint32_t)w[i >> 2][i & 3] << 16);
-        v[2 * i + 1] = __uint_as_float((uint32_t)w[i >> 2][i & 3] & 0xffff0000u);
-      }
+// N elements of a row of `cols` from column c on, as they lie in memory.  It is read 16 bytes at a time at any alignment
+// of the elements; where the row ends before the N do, its last N are read, and moved down when they are looked
+// at, so that no load waits for another.  WHOLE_CHUNKS: cols is a multiple of N, and what is read from cols on is the row's last
+// N as they are: without branches.
+template <bool BF16, int N, bool WHOLE_CHUNKS = false>
+struct Raw {
+  static constexpr int WORDS = BF16 ? N / 2 : N;
+  uint32_t w[WORDS];
+  int down;
+  __device__ __forceinline__ void load(const void* x, int64_t row, int c, int cols) {
+    down = 0;
+    if (WHOLE_CHUNKS || cols >= N) {
+      const int at = min(c, cols - N);
+      if constexpr (!WHOLE_CHUNKS) down = min(c - at, N);
+      __builtin_memcpy(w, (const uint8_t*)x + (row + at) * (BF16 ? 2 : 4), WORDS * 4);
     } else {
-      __builtin_memcpy(v, (const float*)x + row + at, 64);
-    }
-    if (down) {
 #pragma unroll
-      for (int s = 16; s > 0; s >>= 1)
+      for (int i = 0; i < WORDS; i++) w[i] = 0;
 #pragma unroll
-        for (int i = 0; i < 16; i++)
-          if (down & s) v[i] = i + s < 16 ? v[(i + s) & 15] : 0.0f;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-      v[i] = 0.0f;
-      if (c + i < cols) {
-        if constexpr (BF16) v[i] = f32_of_bf16(((const uint16_t*)x)[row + c + i]);
-        else v[i] = ((const float*)x)[row + c + i];
-      }
+      for (int i = 0; i < N; i++)
+        if (c + i < cols) {
+          if constexpr (BF16) w[i >> 1] |= (uint32_t)((const uint16_t*)x)[row + c + i] << (16 * (i & 1));
+          else w[i] = ((const uint32_t*)x)[row + c + i];
+        }
     }
   }
+  // These as fp32; zero at and past the row's end.
+  __device__ __forceinline__ void settle(float (&v)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      if constexpr (BF16) v[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+      else v[i] = __uint_as_float(w[i]);
+    }
+    if (!WHOLE_CHUNKS && down) {
+#pragma unroll
+      for (int s = N; s > 0; s >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; i++)
+          if (down & s) v[i] = i + s < N ? v[(i + s) & (N - 1)] : 0.0f;
+    }
+  }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void load16(const void* x, int64_t row, int c, int cols, float (&v)[16]) {
+  Raw<BF16, 16> w;
+  w.load(x, row, c, cols);
+  w.settle(v);
 }
 
 // Writes the codes of 16 columns from c on, none past cols.
@@ -214,32 +227,39 @@ __device__ __forceinline__ void store16(uint8_t* row, int c, int cols, const cm_
   }
 }
 
-// Writes 16 values to a dense row from column c on, none past cols.
-template <bool BF16>
-__device__ __forceinline__ void put16(void* x, int64_t row, int c, int cols, const float (&v)[16]) {
-  if constexpr (BF16) {
-    uint16_t* o = (uint16_t*)x + row + c;
-    if (c + 16 <= cols) {
-      cm_i32x4 u[2];
+// Writes N values to a dense row from column c on, none past cols (WHOLE_CHUNKS: all N are before it).
+template <bool BF16, int N, bool WHOLE_CHUNKS = false>
+__device__ __forceinline__ void put(void* x, int64_t row, int c, int cols, const float (&v)[N]) {
+  if (WHOLE_CHUNKS || c + N <= cols) {
+    if constexpr (BF16) {
+      uint32_t u[N / 2];
 #pragma unroll
-      for (int i = 0; i < 8; i++)
-        u[i >> 2][i & 3] = (int)((uint32_t)bf16_of(v[2 * i]) | ((uint32_t)bf16_of(v[2 * i + 1]) << 16));
-      __builtin_memcpy(o, u, 32);
+      for (int i = 0; i < N / 2; i++) u[i] = (uint32_t)bf16_of(v[2 * i]) | ((uint32_t)bf16_of(v[2 * i + 1]) << 16);
+      __builtin_memcpy((uint16_t*)x + row + c, u, 2 * N);
     } else {
-#pragma unroll
-      for (int i = 0; i < 16; i++)
-        if (c + i < cols) o[i] = bf16_of(v[i]);
+      __builtin_memcpy((float*)x + row + c, v, 4 * N);
     }
   } else {
-    float* o = (float*)x + row + c;
-    if (c + 16 <= cols) {
-      __builtin_memcpy(o, v, 64);
-    } else {
 #pragma unroll
-      for (int i = 0; i < 16; i++)
-        if (c + i < cols) o[i] = v[i];
-    }
+    for (int i = 0; i < N; i++)
+      if (c + i < cols) {
+        if constexpr (BF16) ((uint16_t*)x)[row + c + i] = bf16_of(v[i]);
+        else ((float*)x)[row + c + i] = v[i];
+      }
   }
+}
+
+// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an
+// L2 of its own: an XCD gets a run of neighbouring tiles, in groups of eight rows of
+// tiles, so that the panels that its tiles share are read once into its L2.
+__device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, int& tn) {
+  const uint32_t total = (uint32_t)mt * (uint32_t)nt;
+  const uint32_t xcd = id & 7u, per = total >> 3, more = total & 7u;
+  const uint32_t at = xcd * per + min(xcd, more) + (id >> 3);
+  const uint32_t group = 8u * (uint32_t)nt, g = at / group, in = at - g * group;
+  const uint32_t high = min(8u, (uint32_t)mt - 8u * g);
+  tm = (int)(8u * g + in % high);
+  tn = (int)(in / high);
 }
 
 }  // namespace

@@ -1,5 +1,5 @@
-// Shared by the tiled products: which tile a workgroup takes, how its results leave, and how parts of the summed
-// dimension are joined.  Private to the library.
+// Shared by the tiled products: how a tile's results leave, and how parts of the summed dimension are joined.  Private to
+// the library.
 #pragma once
 
 #include "az_codes_common.h"
@@ -7,19 +7,6 @@
 namespace {
 
 typedef __attribute__((address_space(3))) uint8_t lds_bytes;
-
-// Which tile a workgroup takes.  Workgroups go to the eight XCDs in turn, each with an
-// L2 of its own: an XCD gets a run of neighbouring tiles, in groups of eight rows of
-// tiles, so that the panels that its tiles share are read once into its L2.
-__device__ __forceinline__ void tile_of(uint32_t id, int mt, int nt, int& tm, int& tn) {
-  const uint32_t total = (uint32_t)mt * (uint32_t)nt;
-  const uint32_t xcd = id & 7u, per = total >> 3, more = total & 7u;
-  const uint32_t at = xcd * per + min(xcd, more) + (id >> 3);
-  const uint32_t group = 8u * (uint32_t)nt, g = at / group, in = at - g * group;
-  const uint32_t high = min(8u, (uint32_t)mt - 8u * g);
-  tm = (int)(8u * g + in % high);
-  tn = (int)(in / high);
-}
 
 // Scale bytes of a matrix as aligned words.  Row r's byte of step kb is byte (start + kb) & 3 of
 // the word that holds it, start = place(r).

@@ -84,82 +84,134 @@ __global__ __launch_bounds__(NT) void az_nibble_rows(const void* __restrict__ x,
   }
 }
 
-// Tiles of 128 x 128, their rows from registers and their columns through LDS.
+// Tiles of 64 x 128 through LDS: a wave reads whole lines of the rows, and a thread then takes a block of 32
+// columns of a row, and one of 32 rows of a column.  LDS rows' 16-byte chunks are exchanged (place_of), so that
+// none of the three meets a bank twice.  Neighbouring tiles run on one XCD, whose L2 puts the lines of both results
+// together.
+constexpr int TROWS = 64;
+__device__ __forceinline__ int place_of(int row, int chunk) {
+  return row * 32 + (chunk ^ ((chunk >> 4) & 1) ^ ((row & 3) << 1) ^ ((row >> 5) << 3));
+}
+
+// The codes of 32 values and their scale byte.
+__device__ __forceinline__ int nibbles32(const float (&lo)[16], const float (&hi)[16], cm_i32x4& w) {
+  const uint32_t a = max(largest16(lo), largest16(hi));
+  const int s = a >= INF_BITS ? 255 : nibble_scale(a);
+  const uint64_t u = nibbles16(lo, s), v = nibbles16(hi, s);
+  w = cm_i32x4{(int)u, (int)(u >> 32), (int)v, (int)(v >> 32)};
+  return s;
+}
+
+// Writes a block's codes from column c on (a multiple of 32), whole bytes and none past cols.
+__device__ __forceinline__ void store_block(uint8_t* row, int c, int cols, const cm_i32x4& w) {
+  if (c + NB <= cols) {
+    *reinterpret_cast<cm_i32x4*>(row + c / 2) = w;
+  } else {
+    store_nibbles(row, c, cols, (uint32_t)w[0] | (uint64_t)(uint32_t)w[1] << 32);
+    if (c + 16 < cols) store_nibbles(row, c + 16, cols, (uint32_t)w[2] | (uint64_t)(uint32_t)w[3] << 32);
+  }
+}
+
 template <bool BF16>
-__global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x, int64_t ldx, NibbleView q, NibbleView qt) {
-  extern __shared__ __attribute__((aligned(16))) float tile[];  // [128][128]
-  const uint32_t nb = ((uint32_t)q.cols + 127) / 128;
-  const uint32_t rb = blockIdx.x / nb, kb = blockIdx.x - rb * nb;
-  const int t = threadIdx.x, c = (int)kb * 128 + (t & 7) * 16;
-  const int64_t r0 = (int64_t)rb * 128 + (t >> 3);
-  float v[4][16];
+__global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x, int64_t ldx, NibbleView q, NibbleView qt, int mt, int nt) {
+  __shared__ cm_f32x4 tile[TROWS * 32];
+  constexpr int N = BF16 ? 8 : 4, LANES = 128 / N, LOADS = TROWS * LANES / NT;  // columns of a load, and loads of a thread
+  int rb, kb;
+  tile_of(blockIdx.x, mt, nt, rb, kb);
+  const int t = threadIdx.x, r0 = rb * TROWS, c0 = kb * 128, rows = min(q.rows - r0, TROWS), cl = t % LANES * N;
+  Raw<BF16, N> raw[LOADS];
 #pragma unroll
-  for (int p = 0; p < 4; p++) load16<BF16>(x, min(r0 + 32 * p, (int64_t)q.rows - 1) * ldx, c, q.cols, v[p]);
+  for (int i = 0; i < LOADS; i++) {
+    const int r = min(i * (NT / LANES) + t / LANES, rows - 1);
+    raw[i].load(x, (int64_t)(r0 + r) * ldx, c0 + cl, q.cols);
+  }
 #pragma unroll
-  for (int p = 0; p < 4; p++) {
-    const int64_t r = r0 + 32 * p;
-    uint32_t a = largest16(v[p]);
-    a = max(a, (uint32_t)__shfl_xor((int)a, 1));
-    const int s = a >= INF_BITS ? 255 : nibble_scale(a);
-    if (r < q.rows && c < q.cols) {
-      store_nibbles(q.codes + r * q.ld, c, q.cols, nibbles16(v[p], s));
-      if (!(t & 1)) q.scales[r * q.ld_scales + c / NB] = (uint8_t)s;
-    }
-    cm_f32x4* to = reinterpret_cast<cm_f32x4*>(tile + ((t >> 3) + 32 * p) * 128 + (t & 7) * 16);
+  for (int i = 0; i < LOADS; i++) {
+    const int r = i * (NT / LANES) + t / LANES;
+    float v[N];
+    raw[i].settle(v);
 #pragma unroll
-    for (int i = 0; i < 4; i++)
-      to[i] = r < q.rows ? cm_f32x4{v[p][4 * i], v[p][4 * i + 1], v[p][4 * i + 2], v[p][4 * i + 3]} : cm_f32x4{0, 0, 0, 0};
+    for (int k = 0; k < N / 4; k++)
+      tile[place_of(r, cl / 4 + k)] = r < rows ? cm_f32x4{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]} : cm_f32x4{0, 0, 0, 0};
   }
   __syncthreads();
-  // A thread takes a column's rows, two blocks of 32.
-  const int j = t & 127;
-  const int64_t rt = (int64_t)kb * 128 + j;
+  float lo[16], hi[16];
+  cm_i32x4 w;
+  {
+    const int r = t >> 2, c = c0 + (t & 3) * NB;
 #pragma unroll
-  for (int p = 0; p < 2; p++) {
-    const int i0 = (t >> 7) * 64 + 32 * p, ct = (int)rb * 128 + i0;
-    if (rt >= qt.rows || ct >= qt.cols) continue;
-    float lo[16], hi[16];
+    for (int k = 0; k < 8; k++) {
+      const cm_f32x4 v = tile[place_of(r, (t & 3) * 8 + k)];
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      lo[i] = tile[(i0 + i) * 128 + j];
-      hi[i] = tile[(i0 + 16 + i) * 128 + j];
+      for (int e = 0; e < 4; e++) (k < 4 ? lo : hi)[4 * (k & 3) + e] = v[e];
     }
-    const uint32_t a = max(largest16(lo), largest16(hi));
-    const int s = a >= INF_BITS ? 255 : nibble_scale(a);
-    uint8_t* row = qt.codes + rt * qt.ld;
-    store_nibbles(row, ct, qt.cols, nibbles16(lo, s));
-    if (ct + 16 < qt.cols) store_nibbles(row, ct + 16, qt.cols, nibbles16(hi, s));
-    qt.scales[rt * qt.ld_scales + ct / NB] = (uint8_t)s;
+    if (r < rows && c < q.cols) {
+      const int s = nibbles32(lo, hi, w);
+      store_block(q.codes + (int64_t)(r0 + r) * q.ld, c, q.cols, w);
+      q.scales[(int64_t)(r0 + r) * q.ld_scales + c / NB] = (uint8_t)s;
+    }
   }
+  {
+    const int j = t >> 1, i0 = (t & 1) * NB, rt = c0 + j, ct = r0 + i0;
+    const float* column = reinterpret_cast<const float*>(tile) + (j & 3);
+#pragma unroll
+    for (int i = 0; i < 32; i++) (i < 16 ? lo : hi)[i & 15] = column[4 * place_of(i0 + i, j >> 2)];
+    if (rt < qt.rows && ct < qt.cols) {
+      const int s = nibbles32(lo, hi, w);
+      store_block(qt.codes + (int64_t)rt * qt.ld, ct, qt.cols, w);
+      qt.scales[(int64_t)rt * qt.ld_scales + ct / NB] = (uint8_t)s;
+    }
+  }
+}
+
+// A thread restores 16 bytes of a row at a time, so that a wave writes whole lines, four of them on their way together.
+// 2^shift threads have a row.
+template <bool BF16>
+__global__ __launch_bounds__(NT) void az_nibble_values(NibbleView q, void* __restrict__ x, int64_t ldx, int shift) {
+  constexpr int N = BF16 ? 8 : 4, AHEAD = 4;
+  const int t = threadIdx.x & ((1 << shift) - 1), step = N << shift, rows = NT >> shift;
+  for (int64_t r = blockIdx.x * (int64_t)rows + (threadIdx.x >> shift); r < q.rows; r += (int64_t)gridDim.x * rows) {
+    const uint8_t* from = q.codes + r * q.ld;
+    const uint8_t* scales = q.scales + r * q.ld_scales;
+    for (int64_t first = t * N; first < q.cols; first += (int64_t)AHEAD * step) {
+      uint32_t w[AHEAD], sb[AHEAD];
+#pragma unroll
+      for (int a = 0; a < AHEAD; a++) {
+        const int c = (int)min(first + (int64_t)a * step, (int64_t)(q.cols - 1) / N * N);  // (past the row: its last ones again)
+        if constexpr (BF16) w[a] = *reinterpret_cast<const uint32_t*>(from + c / 2);
+        else w[a] = *reinterpret_cast<const uint16_t*>(from + c / 2);
+        sb[a] = scales[c / NB];
+      }
+#pragma unroll
+      for (int a = 0; a < AHEAD; a++) {
+        const int64_t c = first + (int64_t)a * step;
+        if (c >= q.cols) break;
+        const float s = scale_value(sb[a]);
+        float v[N];
+        const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 0), f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 1);
+        v[0] = f0[0] * s, v[1] = f0[1] * s, v[2] = f1[0] * s, v[3] = f1[1] * s;
+        if constexpr (BF16) {
+          const auto f2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 2), f3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 3);
+          v[4] = f2[0] * s, v[5] = f2[1] * s, v[6] = f3[0] * s, v[7] = f3[1] * s;
+        }
+        put<BF16, N>(x, r * ldx, (int)c, q.cols, v);
+      }
+    }
+  }
+}
+
+// Workgroups of a pass in which each takes NT / 8 parts of 128 columns at a time.
+dim3 pass_grid(const NibbleView& q) {
+  const int64_t groups = ((int64_t)q.rows * ((q.cols + 127) / 128) + NT / 8 - 1) / (NT / 8);
+  return dim3((unsigned)(groups < 65536 ? groups : 65536));
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(NT) void az_nibble_values(NibbleView q, void* __restrict__ x, int64_t ldx) {
-  const uint32_t nb = ((uint32_t)q.cols + 127) / 128, total = (uint32_t)q.rows * nb, lane8 = threadIdx.x & 7;
-  for (uint64_t id = blockIdx.x * (uint64_t)(NT / 8) + (threadIdx.x >> 3); id < total; id += (uint64_t)gridDim.x * (NT / 8)) {
-    const uint32_t r = (uint32_t)id / nb, kb = (uint32_t)id - r * nb;
-    const int c = (int)(kb * 128 + lane8 * 16);
-    if (c >= q.cols) continue;
-    const float s = scale_value(q.scales[(int64_t)r * q.ld_scales + c / NB]);
-    const uint64_t u = *reinterpret_cast<const uint64_t*>(q.codes + (int64_t)r * q.ld + (c >> 1));
-    float v[16];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-      const uint32_t w = (uint32_t)(u >> (32 * i));
-      const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-      const auto f2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), f3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
-      v[8 * i] = f0[0] * s, v[8 * i + 1] = f0[1] * s, v[8 * i + 2] = f1[0] * s, v[8 * i + 3] = f1[1] * s;
-      v[8 * i + 4] = f2[0] * s, v[8 * i + 5] = f2[1] * s, v[8 * i + 6] = f3[0] * s, v[8 * i + 7] = f3[1] * s;
-    }
-    put16<BF16>(x, (int64_t)r * ldx, c, q.cols, v);
-  }
-}
-
-int64_t parts_of(const NibbleView& q) { return (int64_t)q.rows * ((q.cols + 127) / 128); }
-
-dim3 pass_grid(const NibbleView& q) {
-  const int64_t groups = (parts_of(q) + NT / 8 - 1) / (NT / 8);
-  return dim3((unsigned)(groups < 65536 ? groups : 65536));
+void launch_values(const NibbleView& q, void* x, int64_t ldx, hipStream_t s) {
+  int shift = 3;
+  while (shift < 8 && (int64_t)((BF16 ? 8 : 4) * 4) << shift < q.cols) shift++;
+  const int64_t groups = ((int64_t)q.rows + (NT >> shift) - 1) / (NT >> shift);
+  hipLaunchKernelGGL((az_nibble_values<BF16>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(NT), 0, s, q, x, ldx, shift);
 }
 
 template <bool BF16>
@@ -168,12 +220,9 @@ int launch_quantize(const void* x, int64_t ldx, const NibbleView& q, const Nibbl
     hipLaunchKernelGGL((az_nibble_rows<BF16>), pass_grid(q), dim3(NT), 0, s, x, ldx, q);
     return AZ_OK;
   }
-  const int64_t tiles = ((int64_t)q.rows + 127) / 128 * ((q.cols + 127) / 128);
-  if (!grid_fits(tiles, NT)) return AZ_ERR_UNSUPPORTED;
-  const int lds = 128 * 128 * (int)sizeof(float);
-  if (hipFuncSetAttribute(reinterpret_cast<const void*>(az_nibble_tiles<BF16>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-    return AZ_ERR_DEVICE;
-  hipLaunchKernelGGL((az_nibble_tiles<BF16>), dim3((unsigned)tiles), dim3(NT), lds, s, x, ldx, q, *qt);
+  const int64_t mt = ((int64_t)q.rows + TROWS - 1) / TROWS, nt = (q.cols + 127) / 128;
+  if (!grid_fits(mt * nt, NT)) return AZ_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((az_nibble_tiles<BF16>), dim3((unsigned)(mt * nt)), dim3(NT), 0, s, x, ldx, q, *qt, (int)mt, (int)nt);
   return AZ_OK;
 }
 
@@ -207,7 +256,7 @@ extern "C" int az_nibbles_dequantize(const az_fp4_matrix* q, void* x, int32_t dt
   const NibbleView v = nibble_view(*q);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (dtype == AZ_BF16) hipLaunchKernelGGL((az_nibble_values<true>), pass_grid(v), dim3(NT), 0, s, v, x, ldx);
-  else hipLaunchKernelGGL((az_nibble_values<false>), pass_grid(v), dim3(NT), 0, s, v, x, ldx);
+  if (dtype == AZ_BF16) launch_values<true>(v, x, ldx, s);
+  else launch_values<false>(v, x, ldx, s);
   return launch_status(who);
 }

@@ -1,18 +1,19 @@
 // Root-mean-square norm of rows with a residual's addition, into e4m3 codes or a dense matrix, and its gradients.
 //
-// Both are one pass over memory and bound by it: a row stays in registers, 16 columns a thread, between
-// its sums and its results.  Sums over a row are fp64 (its rate is fp32's on this chip, and no finite row
-// overflows); everything after them is fp32, rounded once.  A block of 128 columns is eight neighbouring
-// lanes, which find its scale by lane exchanges.
+// Both are one pass over memory and bound by it: a row stays in registers between its sums and its results, and the
+// next row of the same threads is on its way meanwhile.  Sums over a row are fp64 (its rate is fp32's on this
+// chip, and no finite row overflows); everything after them is fp32, rounded once.  A block of 128 columns is 16
+// neighbouring lanes, which find its scale by lane exchanges.
 #include <math.h>
 
 #include "az_codes_common.h"
 
 namespace {
 
-constexpr int PER = 16;             // columns of a thread
-constexpr int MOST = 1024 * PER;    // columns of a row that stays in registers
+constexpr int PER = 8;                    // neighbouring columns of a thread: a group
+constexpr int MOST = 1024 * PER;          // columns of a group of every thread of the largest workgroup
 constexpr int MAX_COLS = 1 << 24;
+constexpr int FILL = 256 * 1024;          // threads that fill half of the chip
 
 struct NormView {
   const void* x;
@@ -28,24 +29,47 @@ struct NormView {
   float eps;
 };
 
-// Sum over the T threads of a row (T a power of two), in every thread.  `red`: a place for each wave of the workgroup.
+// T: threads of a row, 16 or 64 with several rows a workgroup of 256, or WHOLE: the workgroup.
+constexpr int WHOLE = 0;
+template <int T>
+__device__ __forceinline__ int threads_of_row() { return T == WHOLE ? (int)blockDim.x : T; }
+
+template <int CTRL>
+__device__ __forceinline__ double lane_move(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, false);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+__device__ __forceinline__ double lane_value(double x, int lane) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+
+// Sums over the threads of a row, in every one of them.  `red`: a place for each wave of the workgroup, another one each
+// time that this is called (turn), so that one barrier does.
 template <int T, int N>
-__device__ __forceinline__ void row_sums(double (&v)[N], double (*red)[N]) {
-  for (int o = (T < 64 ? T : 64) / 2; o > 0; o >>= 1)
+__device__ __forceinline__ void row_sums(double (&v)[N], double (*red)[16][N], int turn) {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] += __shfl_xor(v[i], o);
-  if constexpr (T > 64) {
-    const int wave = threadIdx.x >> 6, first = wave & ~(T / 64 - 1);
-    __syncthreads();  // the last row's sums have been read
+  for (int i = 0; i < N; i++) {
+    v[i] += lane_move<0xb1>(v[i]);   // lane ^ 1
+    v[i] += lane_move<0x4e>(v[i]);   // lane ^ 2
+    v[i] += lane_move<0x141>(v[i]);  // the other four of eight
+    v[i] += lane_move<0x140>(v[i]);  // the other eight of sixteen
+    if constexpr (T != 16) v[i] = (lane_value(v[i], 0) + lane_value(v[i], 16)) + (lane_value(v[i], 32) + lane_value(v[i], 48));
+  }
+  if constexpr (T == WHOLE) {
+    const int wave = threadIdx.x >> 6, waves = (int)blockDim.x / 64;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int i = 0; i < N; i++) red[wave][i] = v[i];
+      for (int i = 0; i < N; i++) red[turn & 1][wave][i] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      v[i] = 0.0;
-      for (int w = 0; w < T / 64; w++) v[i] += red[first + w][i];
-    }
+    for (int i = 0; i < N; i++) v[i] = 0.0;
+    for (int w = 0; w < waves; w++)
+#pragma unroll
+      for (int i = 0; i < N; i++) v[i] += red[turn & 1][w][i];
   }
 }
 
@@ -53,96 +77,128 @@ __device__ __forceinline__ float inverse_root(double squares, int cols, float ep
   return (float)(1.0 / sqrt(squares / cols + (double)eps));
 }
 
-// h of 16 columns from c on.
-template <bool BF16>
-__device__ __forceinline__ void stream16(const NormView& p, int64_t r, int c, float (&v)[16]) {
-  load16<BF16>(p.x, r * p.ld_x, c, p.cols, v);
-  if (p.residual) {
-    float add[16];
-    load16<BF16>(p.residual, r * p.ld_residual, c, p.cols, add);
+// What h comes from, a group from c on: on its way, and added up.  EVEN, here and below: cols is a multiple of a group.
+template <bool BF16, bool EVEN>
+struct Stream {
+  Raw<BF16, PER, EVEN> x, residual;
+  __device__ __forceinline__ void load(const NormView& p, int64_t r, int c) {
+    x.load(p.x, r * p.ld_x, c, p.cols);
+    if (p.residual) residual.load(p.residual, r * p.ld_residual, c, p.cols);
+  }
+  __device__ __forceinline__ void sum(const NormView& p, float (&v)[PER]) const {
+    x.settle(v);
+    if (p.residual) {
+      float add[PER];
+      residual.settle(add);
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      v[i] += add[i];
-      if constexpr (BF16) v[i] = f32_of_bf16(bf16_of(v[i]));
+      for (int i = 0; i < PER; i++) {
+        v[i] += add[i];
+        if constexpr (BF16) v[i] = f32_of_bf16(bf16_of(v[i]));
+      }
     }
   }
-}
+};
 
-// The results of 16 columns; the eight lanes of a block of 128 columns call it together.
-template <bool BF16>
-__device__ __forceinline__ void results16(const NormView& p, int64_t r, int c, float inv, const float (&w)[16], float (&v)[16]) {
+// The results of a group; the 16 lanes of a block of 128 columns call it together.
+template <bool BF16, bool EVEN>
+__device__ __forceinline__ void results8(const NormView& p, int64_t r, int c, float inv, const float (&w)[PER], float (&v)[PER]) {
 #pragma unroll
-  for (int i = 0; i < 16; i++) v[i] = v[i] * inv * w[i];
-  if (p.y && c < p.cols) put16<BF16>(p.y, r * p.ld_y, c, p.cols, v);
+  for (int i = 0; i < PER; i++) v[i] = v[i] * inv * w[i];
+  if (p.y && c < p.cols) put<BF16, PER, EVEN>(p.y, r * p.ld_y, c, p.cols, v);
   if (p.codes) {
     uint32_t a = 0;
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      if (c + i >= p.cols) v[i] = 0.0f;  // (NaN of a NaN row)
+    for (int i = 0; i < PER; i++) {
+      if (!EVEN && c + i >= p.cols) v[i] = 0.0f;  // (NaN of a NaN row)
       a = max(a, finite_size(v[i]));
     }
-    for (int o = 4; o > 0; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o));
+    if (EVEN && c >= p.cols) a = 0;
+    a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xb1, 0xf, 0xf, false));
+    a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4e, 0xf, 0xf, false));
+    a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x141, 0xf, 0xf, false));
+    a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x140, 0xf, 0xf, false));
     const int s = scale_byte(a);
     const float scale = __uint_as_float((uint32_t)(254 - s) << 23);
-    cm_i32x4 u;
-#pragma unroll
-    for (int i = 0; i < 4; i++) u[i] = (int)codes4(v + 4 * i, scale);
     if (c < p.cols) {
-      store16(p.codes + r * p.ld_codes, c, p.cols, u);
-      if ((threadIdx.x & 7) == 0) p.scales[r * p.nb + c / CB] = (uint8_t)s;
+      uint64_t u = codes4(v, scale) | (uint64_t)codes4(v + 4, scale) << 32;
+      uint8_t* to = p.codes + r * p.ld_codes + c;
+      if (EVEN || c + PER <= p.cols) {
+        *reinterpret_cast<uint64_t*>(to) = u;
+      } else {
+        for (int i = c; i < p.cols; i++, u >>= 8) *to++ = (uint8_t)u;
+      }
+      if ((threadIdx.x & 15) == 0) p.scales[r * p.nb + c / CB] = (uint8_t)s;
     }
   }
 }
 
-__device__ __forceinline__ void weights16(const float* weight, int c, int cols, float (&w)[16]) {
+// A group's weights.
+template <bool EVEN>
+__device__ __forceinline__ void weights8(const float* weight, int c, int cols, float (&w)[PER]) {
   if (weight) {
-    load16<false>(weight, 0, c, cols, w);
+    Raw<false, PER, EVEN> raw;
+    raw.load(weight, 0, min(c, cols - 1), cols);
+    raw.settle(w);
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; i++) w[i] = 1.0f;
+    for (int i = 0; i < PER; i++) w[i] = 1.0f;
   }
 }
 
-// T threads a row, 1,024 / T rows (T < 256: 256 / T) a workgroup at a time.
-template <bool BF16, int T>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void az_norm_rows(NormView p) {
-  constexpr int NT = T < 256 ? 256 : T, ROWS = NT / T;
-  __shared__ double red[NT / 64][1];
-  const int c = (int)(threadIdx.x % T) * PER;
-  float w[16];
-  weights16(p.weight, min(c, p.cols - 1), p.cols, w);
-  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < p.rows; r0 += (int64_t)gridDim.x * ROWS) {
-    const int64_t r = r0 + threadIdx.x / T;
-    const bool live = r < p.rows && c < p.cols;
-    float v[16] = {};
-    if (live) stream16<BF16>(p, r, c, v);
-    if (live && p.sum) put16<BF16>(p.sum, r * p.ld_sum, c, p.cols, v);
-    if (!p.y && !p.codes) continue;
+// A thread has G groups, a row's threads' groups side by side.  Threads without a row or a column read one that there is.
+template <bool BF16, bool EVEN, int T, int G>
+__global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_rows(NormView p) {
+  constexpr int ROWS = T == WHOLE ? 1 : 256 / (T ? T : 1);
+  __shared__ double red[2][16][1];
+  const int threads = threads_of_row<T>(), t = T == WHOLE ? (int)threadIdx.x : (int)threadIdx.x % threads;
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < p.rows; r0 += (int64_t)gridDim.x * ROWS, turn++) {
+    const int64_t r = r0 + (T == WHOLE ? 0 : threadIdx.x / threads), at = min(r, p.rows - 1);
+    Stream<BF16, EVEN> x[G];
+    float v[G][PER], w[G][PER];
     double s[1] = {0.0};
 #pragma unroll
-    for (int i = 0; i < 16; i++) s[0] = fma((double)v[i], (double)v[i], s[0]);
-    row_sums<T, 1>(s, red);
-    if (r < p.rows) results16<BF16>(p, r, c, inverse_root(s[0], p.cols, p.eps), w, v);
+    for (int g = 0; g < G; g++) x[g].load(p, at, min((g * threads + t) * PER, p.cols - 1));
+#pragma unroll
+    for (int g = 0; g < G; g++) weights8<EVEN>(p.weight, (g * threads + t) * PER, p.cols, w[g]);
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+      const int c = (g * threads + t) * PER;
+      x[g].sum(p, v[g]);
+      if (r < p.rows && c < p.cols && p.sum) put<BF16, PER, EVEN>(p.sum, r * p.ld_sum, c, p.cols, v[g]);
+      double sum = 0.0;
+#pragma unroll
+      for (int i = 0; i < PER; i++) sum = fma((double)v[g][i], (double)v[g][i], sum);
+      s[0] += c < p.cols ? sum : 0.0;
+    }
+    if (!p.y && !p.codes) continue;
+    row_sums<T, 1>(s, red, turn);
+    const float inv = inverse_root(s[0], p.cols, p.eps);
+    if (r < p.rows) {
+#pragma unroll
+      for (int g = 0; g < G; g++) results8<BF16, EVEN>(p, r, (g * threads + t) * PER, inv, w[g], v[g]);
+    }
   }
 }
 
 // Longer rows are read twice; h comes from `sum` the second time where it was written there.
 template <bool BF16>
 __global__ __launch_bounds__(1024) void az_norm_long(NormView p) {
-  __shared__ double red[16][1];
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+  __shared__ double red[2][16][1];
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn++) {
     double s[1] = {0.0};
-    for (int c0 = 0; c0 < p.cols; c0 += MOST) {
-      const int c = c0 + (int)threadIdx.x * PER;
-      if (c >= p.cols) continue;
-      float v[16];
-      stream16<BF16>(p, r, c, v);
-      if (p.sum) put16<BF16>(p.sum, r * p.ld_sum, c, p.cols, v);
+    for (int c = (int)threadIdx.x * PER; c < p.cols; c += MOST) {
+      Stream<BF16, false> x;
+      float v[PER];
+      x.load(p, r, c);
+      x.sum(p, v);
+      if (p.sum) put<BF16, PER>(p.sum, r * p.ld_sum, c, p.cols, v);
 #pragma unroll
-      for (int i = 0; i < 16; i++) s[0] = fma((double)v[i], (double)v[i], s[0]);
+      for (int i = 0; i < PER; i++) s[0] = fma((double)v[i], (double)v[i], s[0]);
     }
     if (!p.y && !p.codes) continue;
-    row_sums<1024, 1>(s, red);
+    row_sums<WHOLE, 1>(s, red, turn);
     const float inv = inverse_root(s[0], p.cols, p.eps);
     NormView again = p;
     if (p.sum) {
@@ -152,10 +208,14 @@ __global__ __launch_bounds__(1024) void az_norm_long(NormView p) {
     }
     for (int c0 = 0; c0 < p.cols; c0 += MOST) {
       const int c = c0 + (int)threadIdx.x * PER;
-      float v[16] = {}, w[16];
-      weights16(p.weight, min(c, p.cols - 1), p.cols, w);
-      if (c < p.cols) stream16<BF16>(again, r, c, v);
-      results16<BF16>(p, r, c, inv, w, v);
+      float v[PER] = {}, w[PER];
+      weights8<false>(p.weight, c, p.cols, w);
+      if (c < p.cols) {
+        Stream<BF16, false> x;
+        x.load(again, r, c);
+        x.sum(again, v);
+      }
+      results8<BF16, false>(p, r, c, inv, w, v);
     }
   }
 }
@@ -173,87 +233,148 @@ struct GradView {
   float eps;
 };
 
-// dx of 16 columns; d keeps dy.
-template <bool BF16>
-__device__ __forceinline__ void input_grad16(const GradView& p, int64_t r, int c, float inv, float mean, const float (&w)[16],
-                                             const float (&h)[16], const float (&d)[16]) {
-  float o[16];
-  if (p.dsum) load16<BF16>(p.dsum, r * p.ld_dsum, c, p.cols, o);
+// What the gradients of a group come from.
+template <bool BF16, bool EVEN>
+struct GradStream {
+  Raw<BF16, PER, EVEN> h, dy, dsum;
+  __device__ __forceinline__ void load(const GradView& p, int64_t r, int c) {
+    h.load(p.h, r * p.ld_h, c, p.cols);
+    dy.load(p.dy, r * p.ld_dy, c, p.cols);
+    if (p.dsum) dsum.load(p.dsum, r * p.ld_dsum, c, p.cols);
+  }
+};
+
+__device__ __forceinline__ void grad_sums(double (&s)[2], const float (&w)[PER], const float (&h)[PER], const float (&d)[PER]) {
 #pragma unroll
-  for (int i = 0; i < 16; i++) {
+  for (int i = 0; i < PER; i++) {
+    s[0] = fma((double)h[i], (double)h[i], s[0]);
+    s[1] = fma((double)(d[i] * w[i]), (double)h[i], s[1]);
+  }
+}
+
+// dx of a group; o holds dsum.
+template <bool BF16, bool EVEN>
+__device__ __forceinline__ void input_grad8(const GradView& p, int64_t r, int c, float inv, float mean, const float (&w)[PER],
+                                            const float (&h)[PER], const float (&d)[PER], float (&o)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; i++) {
     const float g = inv * (d[i] * w[i] - h[i] * inv * mean);
     o[i] = p.dsum ? g + o[i] : g;
   }
-  put16<BF16>(p.dx, r * p.ld_dx, c, p.cols, o);
+  put<BF16, PER, EVEN>(p.dx, r * p.ld_dx, c, p.cols, o);
 }
 
-// Slot i takes the rows i, i + slots, ...; T threads a slot.
-template <bool BF16, int T>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void az_norm_grad_rows(GradView p) {
-  constexpr int NT = T < 256 ? 256 : T;
-  __shared__ double red[NT / 64][2];
-  const int c = (int)(threadIdx.x % T) * PER, slot = (int)blockIdx.x * (NT / T) + (int)(threadIdx.x / T);
-  float w[16], dw[16] = {};
-  weights16(p.weight, min(c, p.cols - 1), p.cols, w);
-  for (int64_t r0 = 0; r0 < p.rows; r0 += p.slots) {
+// Keeps the compiler from holding what it makes of these words over this point: they are unpacked again.
+template <bool BF16, bool EVEN>
+__device__ __forceinline__ void unpack_again(Raw<BF16, PER, EVEN>& x) {
+#pragma unroll
+  for (int i = 0; i < x.WORDS; i++) asm volatile("" : "+v"(x.w[i]));
+}
+
+// Slot i takes the rows i, i + slots, ...  A row stays as it lies in memory, and is unpacked for its sums and for its results;
+// the next one is on its way meanwhile.
+template <bool BF16, bool EVEN, int T, int G>
+__global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_grad_rows(GradView p) {
+  constexpr bool AHEAD = G == 1;  // (two groups' next row would not fit the registers)
+  __shared__ double red[2][16][2];
+  const int threads = threads_of_row<T>(), t = T == WHOLE ? (int)threadIdx.x : (int)threadIdx.x % threads;
+  const int slot = T == WHOLE ? (int)blockIdx.x : (int)blockIdx.x * (256 / (T ? T : 1)) + (int)(threadIdx.x / threads);
+  GradStream<BF16, EVEN> next[G];
+  float w[G][PER], dw[G][PER] = {};
+  auto fetch = [&](int64_t r) {
+#pragma unroll
+    for (int g = 0; g < G; g++) next[g].load(p, min(r, p.rows - 1), min((g * threads + t) * PER, p.cols - 1));
+  };
+  fetch(slot);
+#pragma unroll
+  for (int g = 0; g < G; g++) weights8<EVEN>(p.weight, (g * threads + t) * PER, p.cols, w[g]);
+  int turn = 0;
+  for (int64_t r0 = 0; r0 < p.rows; r0 += p.slots, turn++) {
     const int64_t r = r0 + slot;
-    const bool live = r < p.rows && slot < p.slots && c < p.cols;
-    float h[16] = {}, d[16] = {};
-    if (live) {
-      load16<BF16>(p.h, r * p.ld_h, c, p.cols, h);
-      load16<BF16>(p.dy, r * p.ld_dy, c, p.cols, d);
-    }
+    GradStream<BF16, EVEN> x[G];
     double s[2] = {0.0, 0.0};
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-      s[0] = fma((double)h[i], (double)h[i], s[0]);
-      s[1] = fma((double)(d[i] * w[i]), (double)h[i], s[1]);
+    if constexpr (!AHEAD) {
+      if (r0 > 0) fetch(r);
     }
-    row_sums<T, 2>(s, red);
-    const float inv = inverse_root(s[0], p.cols, p.eps), mean = (float)(s[1] * (double)inv / p.cols);
-    if (live) {
 #pragma unroll
-      for (int i = 0; i < 16; i++) dw[i] = fmaf(d[i], h[i] * inv, dw[i]);
-      if (p.dx) input_grad16<BF16>(p, r, c, inv, mean, w, h, d);
+    for (int g = 0; g < G; g++) x[g] = next[g];
+    if constexpr (AHEAD) {
+      if (r0 + p.slots < p.rows) fetch(r + p.slots);
+    }
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+      float h[PER], d[PER];
+      double sum[2] = {0.0, 0.0};
+      x[g].h.settle(h);
+      x[g].dy.settle(d);
+      grad_sums(sum, w[g], h, d);
+#pragma unroll
+      for (int i = 0; i < 2; i++) s[i] += (g * threads + t) * PER < p.cols ? sum[i] : 0.0;
+    }
+    row_sums<T, 2>(s, red, turn);
+    const float inv = inverse_root(s[0], p.cols, p.eps), mean = (float)(s[1] * (double)inv / p.cols);
+    if (r < p.rows && slot < p.slots) {
+#pragma unroll
+      for (int g = 0; g < G; g++) {
+        const int c = (g * threads + t) * PER;
+        unpack_again(x[g].h);
+        unpack_again(x[g].dy);
+        float h[PER], d[PER], o[PER];
+        x[g].h.settle(h);
+        x[g].dy.settle(d);
+        if (p.dsum) x[g].dsum.settle(o);
+#pragma unroll
+        for (int i = 0; i < PER; i++) dw[g][i] = fmaf(d[i], h[i] * inv, dw[g][i]);
+        if (p.dx && c < p.cols) input_grad8<BF16, EVEN>(p, r, c, inv, mean, w[g], h, d, o);
+      }
     }
   }
-  if (p.parts && slot < p.slots && c < p.cols) put16<false>(p.parts, (int64_t)slot * p.cols, c, p.cols, dw);
+  if (p.parts && slot < p.slots) {
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+      const int c = (g * threads + t) * PER;
+      if (c < p.cols) put<false, PER, EVEN>(p.parts, (int64_t)slot * p.cols, c, p.cols, dw[g]);
+    }
+  }
 }
 
 // Rows past the registers: the sums first, then the results, and the weight's gradient through the slot's part.
 template <bool BF16>
 __global__ __launch_bounds__(1024) void az_norm_grad_long(GradView p) {
-  __shared__ double red[16][2];
+  __shared__ double red[2][16][2];
+  int turn = 0;
   float* const part = p.parts ? p.parts + (int64_t)blockIdx.x * p.cols : nullptr;
-  for (int64_t r = blockIdx.x; r < p.rows; r += p.slots) {
+  for (int64_t r = blockIdx.x; r < p.rows; r += p.slots, turn++) {
     double s[2] = {0.0, 0.0};
     for (int c = (int)threadIdx.x * PER; c < p.cols; c += MOST) {
-      float h[16], d[16], w[16];
-      weights16(p.weight, c, p.cols, w);
-      load16<BF16>(p.h, r * p.ld_h, c, p.cols, h);
-      load16<BF16>(p.dy, r * p.ld_dy, c, p.cols, d);
-#pragma unroll
-      for (int i = 0; i < 16; i++) {
-        s[0] = fma((double)h[i], (double)h[i], s[0]);
-        s[1] = fma((double)(d[i] * w[i]), (double)h[i], s[1]);
-      }
+      GradStream<BF16, false> x;
+      float h[PER], d[PER], w[PER];
+      x.h.load(p.h, r * p.ld_h, c, p.cols);
+      x.dy.load(p.dy, r * p.ld_dy, c, p.cols);
+      weights8<false>(p.weight, c, p.cols, w);
+      x.h.settle(h);
+      x.dy.settle(d);
+      grad_sums(s, w, h, d);
     }
-    row_sums<1024, 2>(s, red);
+    row_sums<WHOLE, 2>(s, red, turn);
     const float inv = inverse_root(s[0], p.cols, p.eps), mean = (float)(s[1] * (double)inv / p.cols);
     for (int c = (int)threadIdx.x * PER; c < p.cols; c += MOST) {
-      float h[16], d[16], w[16];
-      weights16(p.weight, c, p.cols, w);
-      load16<BF16>(p.h, r * p.ld_h, c, p.cols, h);
-      load16<BF16>(p.dy, r * p.ld_dy, c, p.cols, d);
+      GradStream<BF16, false> x;
+      float h[PER], d[PER], w[PER], o[PER];
+      x.load(p, r, c);
+      weights8<false>(p.weight, c, p.cols, w);
+      x.h.settle(h);
+      x.dy.settle(d);
+      if (p.dsum) x.dsum.settle(o);
       if (part) {
 #pragma unroll
-        for (int i = 0; i < 16; i++)
+        for (int i = 0; i < PER; i++)
           if (c + i < p.cols) {
             const float u = d[i] * (h[i] * inv);
             part[c + i] = r == blockIdx.x ? u : part[c + i] + u;
           }
       }
-      if (p.dx) input_grad16<BF16>(p, r, c, inv, mean, w, h, d);
+      if (p.dx) input_grad8<BF16, false>(p, r, c, inv, mean, w, h, d, o);
     }
   }
 }
@@ -277,56 +398,50 @@ __global__ __launch_bounds__(1024) void az_norm_join(const float* __restrict__ p
   }
 }
 
-// Threads of a row, 16 columns each; 0: the row is longer than a workgroup holds.
-int row_threads(int64_t cols) {
-  if (cols > MOST) return 0;
-  int t = 8;
-  while (t * PER < cols) t *= 2;
-  return t;
+// Threads of a row of `groups` groups each: 16, 64 or whole waves; 0: the row is longer than a workgroup holds, two groups
+// a thread.
+struct Shape {
+  int threads, groups;
+};
+Shape row_shape(int64_t cols) {
+  if (cols > 2 * MOST) return {0, 0};
+  if (cols <= 64 * PER) return {cols <= 16 * PER ? 16 : 64, 1};
+  const int groups = cols > MOST ? 2 : 1, wave = 64 * PER * groups;
+  return {(int)((cols + wave - 1) / wave) * 64, groups};
 }
 
-// Slots that the weight's gradient is summed in: enough threads to fill the chip, and eight rows or more in
+// Slots that the weight's gradient is summed in: enough threads to fill half of the chip, and eight rows or more in
 // each, so that the parts are little beside the rows.
 int grad_slots(int64_t rows, int64_t cols) {
-  const int t = row_threads(cols);
-  const int64_t fill = t ? 262144 / t : 256, few = (rows + 7) / 8 > 256 ? (rows + 7) / 8 : 256;
+  const int t = row_shape(cols).threads;
+  const int64_t fill = t ? FILL / t : 256, few = (rows + 7) / 8 > 256 ? (rows + 7) / 8 : 256;
   const int64_t slots = few < fill ? few : fill;
   return (int)(rows < slots ? rows : slots);
 }
 
-template <bool BF16>
+template <bool BF16, bool EVEN>
 void launch_norm(const NormView& p, hipStream_t s) {
-  const int t = row_threads(p.cols), rows = t && t < 256 ? 256 / t : 1;
+  const Shape f = row_shape(p.cols);
+  const int rows = f.threads == 16 ? 16 : f.threads == 64 ? 4 : 1;
   const int64_t need = (p.rows + rows - 1) / rows;
   const dim3 g((unsigned)(need < (1 << 20) ? need : 1 << 20));
-  switch (t) {
-    case 8: hipLaunchKernelGGL((az_norm_rows<BF16, 8>), g, dim3(256), 0, s, p); break;
-    case 16: hipLaunchKernelGGL((az_norm_rows<BF16, 16>), g, dim3(256), 0, s, p); break;
-    case 32: hipLaunchKernelGGL((az_norm_rows<BF16, 32>), g, dim3(256), 0, s, p); break;
-    case 64: hipLaunchKernelGGL((az_norm_rows<BF16, 64>), g, dim3(256), 0, s, p); break;
-    case 128: hipLaunchKernelGGL((az_norm_rows<BF16, 128>), g, dim3(256), 0, s, p); break;
-    case 256: hipLaunchKernelGGL((az_norm_rows<BF16, 256>), g, dim3(256), 0, s, p); break;
-    case 512: hipLaunchKernelGGL((az_norm_rows<BF16, 512>), g, dim3(512), 0, s, p); break;
-    case 1024: hipLaunchKernelGGL((az_norm_rows<BF16, 1024>), g, dim3(1024), 0, s, p); break;
-    default: hipLaunchKernelGGL((az_norm_long<BF16>), g, dim3(1024), 0, s, p);
-  }
+  if (f.threads == 0) hipLaunchKernelGGL((az_norm_long<BF16>), g, dim3(1024), 0, s, p);
+  else if (f.threads == 16) hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, 16, 1>), g, dim3(256), 0, s, p);
+  else if (f.threads == 64) hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, 64, 1>), g, dim3(256), 0, s, p);
+  else if (f.groups == 1) hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, WHOLE, 1>), g, dim3(f.threads), 0, s, p);
+  else hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, WHOLE, 2>), g, dim3(f.threads), 0, s, p);
 }
 
-template <bool BF16>
+template <bool BF16, bool EVEN>
 void launch_norm_grad(const GradView& p, hipStream_t s) {
-  const int t = row_threads(p.cols), slots = t && t < 256 ? 256 / t : 1;
+  const Shape f = row_shape(p.cols);
+  const int slots = f.threads == 16 ? 16 : f.threads == 64 ? 4 : 1;
   const dim3 g((unsigned)((p.slots + slots - 1) / slots));
-  switch (t) {
-    case 8: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 8>), g, dim3(256), 0, s, p); break;
-    case 16: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 16>), g, dim3(256), 0, s, p); break;
-    case 32: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 32>), g, dim3(256), 0, s, p); break;
-    case 64: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 64>), g, dim3(256), 0, s, p); break;
-    case 128: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 128>), g, dim3(256), 0, s, p); break;
-    case 256: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 256>), g, dim3(256), 0, s, p); break;
-    case 512: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 512>), g, dim3(512), 0, s, p); break;
-    case 1024: hipLaunchKernelGGL((az_norm_grad_rows<BF16, 1024>), g, dim3(1024), 0, s, p); break;
-    default: hipLaunchKernelGGL((az_norm_grad_long<BF16>), g, dim3(1024), 0, s, p);
-  }
+  if (f.threads == 0) hipLaunchKernelGGL((az_norm_grad_long<BF16>), g, dim3(1024), 0, s, p);
+  else if (f.threads == 16) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, 16, 1>), g, dim3(256), 0, s, p);
+  else if (f.threads == 64) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, 64, 1>), g, dim3(256), 0, s, p);
+  else if (f.groups == 1) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, WHOLE, 1>), g, dim3(f.threads), 0, s, p);
+  else hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, WHOLE, 2>), g, dim3(f.threads), 0, s, p);
 }
 
 bool norm_sizes(int64_t rows, int64_t cols) { return rows <= INT32_MAX && cols <= MAX_COLS; }
@@ -362,8 +477,9 @@ extern "C" int az_rms_norm(const az_norm* n, void* stream) {
                       (int)((n->cols + CB - 1) / CB), n->eps};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (n->dtype == AZ_BF16) launch_norm<true>(p, s);
-  else launch_norm<false>(p, s);
+  const bool even = n->cols % PER == 0;
+  if (n->dtype == AZ_BF16) even ? launch_norm<true, true>(p, s) : launch_norm<true, false>(p, s);
+  else even ? launch_norm<false, true>(p, s) : launch_norm<false, false>(p, s);
   return launch_status(who);
 }
 
@@ -395,8 +511,9 @@ extern "C" int az_rms_norm_grad(const az_norm_grad* n, void* workspace, size_t w
   if (n->rows > 0) {
     const GradView p = {n->dy, n->h, n->weight, n->dsum, n->dx, parts, n->ld_dy, n->ld_h, n->ld_dsum, n->ld_dx,
                         n->rows, (int)n->cols, slots, n->eps};
-    if (n->dtype == AZ_BF16) launch_norm_grad<true>(p, s);
-    else launch_norm_grad<false>(p, s);
+    const bool even = n->cols % PER == 0;
+    if (n->dtype == AZ_BF16) even ? launch_norm_grad<true, true>(p, s) : launch_norm_grad<true, false>(p, s);
+    else even ? launch_norm_grad<false, true>(p, s) : launch_norm_grad<false, false>(p, s);
     if ((st = launch_status(who)) != AZ_OK) return st;
   }
   if (n->dweight) {

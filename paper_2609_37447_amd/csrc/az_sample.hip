@@ -572,6 +572,8 @@ extern "C" int az_logits_sample(const az_sampling* in, int32_t* out, float* prob
                         shift < 51 ? shift : 51};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (in->vocab <= 8192) return launched(who, in->dtype == AZ_BF16 ? launch<true, 256>(p, s) : launch<false, 256>(p, s));
+  const int nt = in->vocab <= 8192 ? 256 : in->rows > 256 ? 512 : 1024;
+  if (nt == 256) return launched(who, in->dtype == AZ_BF16 ? launch<true, 256>(p, s) : launch<false, 256>(p, s));
+  if (nt == 512) return launched(who, in->dtype == AZ_BF16 ? launch<true, 512>(p, s) : launch<false, 512>(p, s));
   return launched(who, in->dtype == AZ_BF16 ? launch<true, 1024>(p, s) : launch<false, 1024>(p, s));
 }
