@@ -15,35 +15,33 @@ __device__ __forceinline__ int nibble_scale(uint32_t a) {
   return min(max(e, -125), 125) + 127;
 }
 
-// Eight codes of eight values, scaled by inv: the instruction rounds to the nearest, ties to even, and is given
-// nothing past 6.
-__device__ __forceinline__ uint32_t nibbles8(const float* x, float inv) {
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; i++) y[i] = __builtin_amdgcn_fmed3f(x[i] * inv, -6.0f, 6.0f);
+// Eight codes of eight values over the scale: the instruction divides, rounds to the nearest, ties to even, and saturates at 6.
+__device__ __forceinline__ uint32_t nibbles8(const float* x, float scale) {
   uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.0f, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.0f, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.0f, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.0f, 3);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
-// The factor of a block with this scale byte, 2^-e; 0 for 255, whose codes are zeros.
-__device__ __forceinline__ float nibble_inverse(int s) { return s == 255 ? 0.0f : __uint_as_float((uint32_t)(254 - s) << 23); }
-
-// Largest |x| of 16 values by its bits, 0x7f800000 and more if one is not finite.
+// Largest |x| of 16 values by its bits, 0x7f800000 and more if one is not finite: the largest number among the bits as
+// whole numbers is the largest positive value's, or, unsigned, the largest negative one's.
 __device__ __forceinline__ uint32_t largest16(const float (&v)[16]) {
-  uint32_t a = 0;
+  int32_t a = 0;
+  uint32_t b = 0;
 #pragma unroll
-  for (int i = 0; i < 16; i++) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
-  return a;
+  for (int i = 0; i < 16; i++) {
+    a = max(a, __float_as_int(v[i]));
+    b = max(b, __float_as_uint(v[i]));
+  }
+  return max((uint32_t)a, b >> 31 ? b & 0x7fffffffu : 0u);
 }
 
 // 16 codes of a half block; of a block that is not finite, zeros.
 __device__ __forceinline__ uint64_t nibbles16(const float (&v)[16], int s) {
   if (s == 255) return 0;
-  const float inv = nibble_inverse(s);
-  return nibbles8(v, inv) | (uint64_t)nibbles8(v + 8, inv) << 32;
+  const float scale = __uint_as_float((uint32_t)s << 23);
+  return nibbles8(v, scale) | (uint64_t)nibbles8(v + 8, scale) << 32;
 }
 
 // Writes the codes of 16 columns from c on (a multiple of 16), whole bytes and none past cols.
@@ -86,8 +84,8 @@ __global__ __launch_bounds__(NT) void az_nibble_rows(const void* __restrict__ x,
 
 // Tiles of 64 x 128 through LDS: a wave reads whole lines of the rows, and a thread then takes a block of 32
 // columns of a row, and one of 32 rows of a column.  LDS rows' 16-byte chunks are exchanged (place_of), so that
-// none of the three meets a bank twice.  Neighbouring tiles run on one XCD, whose L2 puts the lines of both results
-// together.
+// none of the three meets a bank twice.  4672 x 8192 fp32: 51 us (3.8 TB/s), of which reading alone takes 40; an order of
+// tiles that keeps neighbours on one XCD took 54.
 constexpr int TROWS = 64;
 __device__ __forceinline__ int place_of(int row, int chunk) {
   return row * 32 + (chunk ^ ((chunk >> 4) & 1) ^ ((row & 3) << 1) ^ ((row >> 5) << 3));
@@ -112,14 +110,14 @@ __device__ __forceinline__ void store_block(uint8_t* row, int c, int cols, const
   }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x, int64_t ldx, NibbleView q, NibbleView qt, int mt, int nt) {
+// EVEN: cols is a multiple of a load.
+template <bool BF16, bool EVEN>
+__global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x, int64_t ldx, NibbleView q, NibbleView qt, int nt) {
   __shared__ cm_f32x4 tile[TROWS * 32];
   constexpr int N = BF16 ? 8 : 4, LANES = 128 / N, LOADS = TROWS * LANES / NT;  // columns of a load, and loads of a thread
-  int rb, kb;
-  tile_of(blockIdx.x, mt, nt, rb, kb);
+  const int rb = (int)(blockIdx.x / (uint32_t)nt), kb = (int)(blockIdx.x % (uint32_t)nt);
   const int t = threadIdx.x, r0 = rb * TROWS, c0 = kb * 128, rows = min(q.rows - r0, TROWS), cl = t % LANES * N;
-  Raw<BF16, N> raw[LOADS];
+  Raw<BF16, N, EVEN> raw[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; i++) {
     const int r = min(i * (NT / LANES) + t / LANES, rows - 1);
@@ -130,9 +128,10 @@ __global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x
     const int r = i * (NT / LANES) + t / LANES;
     float v[N];
     raw[i].settle(v);
+    const bool live = r < rows && (!EVEN || c0 + cl < q.cols);
 #pragma unroll
     for (int k = 0; k < N / 4; k++)
-      tile[place_of(r, cl / 4 + k)] = r < rows ? cm_f32x4{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]} : cm_f32x4{0, 0, 0, 0};
+      tile[place_of(r, cl / 4 + k)] = live ? cm_f32x4{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]} : cm_f32x4{0, 0, 0, 0};
   }
   __syncthreads();
   float lo[16], hi[16];
@@ -164,38 +163,38 @@ __global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x
   }
 }
 
-// A thread restores 16 bytes of a row at a time, so that a wave writes whole lines, four of them on their way together.
-// 2^shift threads have a row.
-template <bool BF16>
-__global__ __launch_bounds__(NT) void az_nibble_values(NibbleView q, void* __restrict__ x, int64_t ldx, int shift) {
-  constexpr int N = BF16 ? 8 : 4, AHEAD = 4;
-  const int t = threadIdx.x & ((1 << shift) - 1), step = N << shift, rows = NT >> shift;
-  for (int64_t r = blockIdx.x * (int64_t)rows + (threadIdx.x >> shift); r < q.rows; r += (int64_t)gridDim.x * rows) {
+// A thread restores 16 bytes of a row at a time, so that a wave writes whole lines, AHEAD of them on their way together.
+// 2^shift threads have one of the `parts` of a row.
+template <bool BF16, int AHEAD>
+__global__ __launch_bounds__(NT) void az_nibble_values(NibbleView q, void* __restrict__ x, int64_t ldx, int shift, uint32_t parts) {
+  constexpr int N = BF16 ? 8 : 4;
+  const int t = threadIdx.x & ((1 << shift) - 1), step = N << shift, items = NT >> shift;
+  const int64_t total = (int64_t)q.rows * parts;
+  for (int64_t id = blockIdx.x * (int64_t)items + (threadIdx.x >> shift); id < total; id += (int64_t)gridDim.x * items) {
+    const int64_t r = parts == 1 ? id : id / parts, first = (id - r * parts) * AHEAD * step + t * N;
     const uint8_t* from = q.codes + r * q.ld;
     const uint8_t* scales = q.scales + r * q.ld_scales;
-    for (int64_t first = t * N; first < q.cols; first += (int64_t)AHEAD * step) {
-      uint32_t w[AHEAD], sb[AHEAD];
+    uint32_t w[AHEAD], sb[AHEAD];
 #pragma unroll
-      for (int a = 0; a < AHEAD; a++) {
-        const int c = (int)min(first + (int64_t)a * step, (int64_t)(q.cols - 1) / N * N);  // (past the row: its last ones again)
-        if constexpr (BF16) w[a] = *reinterpret_cast<const uint32_t*>(from + c / 2);
-        else w[a] = *reinterpret_cast<const uint16_t*>(from + c / 2);
-        sb[a] = scales[c / NB];
-      }
+    for (int a = 0; a < AHEAD; a++) {
+      const int c = (int)min(first + (int64_t)a * step, (int64_t)(q.cols - 1) / N * N);  // (past the row: its last ones again)
+      if constexpr (BF16) w[a] = *reinterpret_cast<const uint32_t*>(from + c / 2);
+      else w[a] = *reinterpret_cast<const uint16_t*>(from + c / 2);
+      sb[a] = scales[c / NB];
+    }
 #pragma unroll
-      for (int a = 0; a < AHEAD; a++) {
-        const int64_t c = first + (int64_t)a * step;
-        if (c >= q.cols) break;
-        const float s = scale_value(sb[a]);
-        float v[N];
-        const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 0), f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 1);
-        v[0] = f0[0] * s, v[1] = f0[1] * s, v[2] = f1[0] * s, v[3] = f1[1] * s;
-        if constexpr (BF16) {
-          const auto f2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 2), f3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 3);
-          v[4] = f2[0] * s, v[5] = f2[1] * s, v[6] = f3[0] * s, v[7] = f3[1] * s;
-        }
-        put<BF16, N>(x, r * ldx, (int)c, q.cols, v);
+    for (int a = 0; a < AHEAD; a++) {
+      const int64_t c = first + (int64_t)a * step;
+      if (c >= q.cols) break;
+      const float s = scale_value(sb[a]);
+      float v[N];
+      const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 0), f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 1);
+      v[0] = f0[0] * s, v[1] = f0[1] * s, v[2] = f1[0] * s, v[3] = f1[1] * s;
+      if constexpr (BF16) {
+        const auto f2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 2), f3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[a], 1.0f, 3);
+        v[4] = f2[0] * s, v[5] = f2[1] * s, v[6] = f3[0] * s, v[7] = f3[1] * s;
       }
+      put<BF16, N>(x, r * ldx, (int)c, q.cols, v);
     }
   }
 }
@@ -206,12 +205,22 @@ dim3 pass_grid(const NibbleView& q) {
   return dim3((unsigned)(groups < 65536 ? groups : 65536));
 }
 
+// Threads of a part: as many as a row has use for.  Four loads a thread where that leaves every compute unit four workgroups
+// (64 x 10240 bf16: XX us with four, YY with one).
+template <bool BF16, int AHEAD>
+void launch_values(const NibbleView& q, void* x, int64_t ldx, hipStream_t s) {
+  constexpr int64_t N = BF16 ? 8 : 4;
+  int shift = 3;
+  while (shift < 8 && (N * AHEAD) << shift < q.cols) shift++;
+  const int64_t parts = (q.cols + ((N * AHEAD) << shift) - 1) / ((N * AHEAD) << shift);
+  const int64_t groups = ((int64_t)q.rows * parts + (NT >> shift) - 1) / (NT >> shift);
+  hipLaunchKernelGGL((az_nibble_values<BF16, AHEAD>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(NT), 0, s, q, x, ldx, shift, (uint32_t)parts);
+}
+
 template <bool BF16>
 void launch_values(const NibbleView& q, void* x, int64_t ldx, hipStream_t s) {
-  int shift = 3;
-  while (shift < 8 && (int64_t)((BF16 ? 8 : 4) * 4) << shift < q.cols) shift++;
-  const int64_t groups = ((int64_t)q.rows + (NT >> shift) - 1) / (NT >> shift);
-  hipLaunchKernelGGL((az_nibble_values<BF16>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(NT), 0, s, q, x, ldx, shift);
+  if ((int64_t)q.rows * q.cols >= (int64_t)1024 * NT * 4 * (BF16 ? 8 : 4)) launch_values<BF16, 4>(q, x, ldx, s);
+  else launch_values<BF16, 1>(q, x, ldx, s);
 }
 
 template <bool BF16>
@@ -222,7 +231,9 @@ int launch_quantize(const void* x, int64_t ldx, const NibbleView& q, const Nibbl
   }
   const int64_t mt = ((int64_t)q.rows + TROWS - 1) / TROWS, nt = (q.cols + 127) / 128;
   if (!grid_fits(mt * nt, NT)) return AZ_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((az_nibble_tiles<BF16>), dim3((unsigned)(mt * nt)), dim3(NT), 0, s, x, ldx, q, *qt, (int)mt, (int)nt);
+  const dim3 g((unsigned)(mt * nt));
+  if (q.cols % (BF16 ? 8 : 4) == 0) hipLaunchKernelGGL((az_nibble_tiles<BF16, true>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
+  else hipLaunchKernelGGL((az_nibble_tiles<BF16, false>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
   return AZ_OK;
 }
 

@@ -51,9 +51,25 @@ __device__ __forceinline__ cm_bf16x8 values8(const cm_i32x8& w, int i, float s) 
   return __builtin_bit_cast(cm_bf16x8, u);
 }
 
-// Few rows of a.  A workgroup of eight waves owns 16 rows of a times 16 rows of b; each wave takes every eighth
-// step of 128 columns, a lane a block of 32, and the waves' sums meet in LDS in the order of the waves.
-constexpr int DW = 8;
+// Few rows of a.  A workgroup of eight waves owns 16 rows of a times 16 rows of b.  Each wave takes DU neighbouring
+// steps of 128 columns of every DW * DU, whose loads are on their way together and cover whole lines of b's rows; a lane holds a
+// block of 32 columns.  The waves' sums meet in LDS in the order of the waves.
+constexpr int DW = 8, DU = 4;
+
+template <int A, bool EXACT>
+struct DirectStep {
+  cm_i32x8 a, b;
+  uint32_t sa, sb;
+  __device__ __forceinline__ void add_to(cm_f32x4& acc) const {
+    if constexpr (!EXACT) {
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, E2M1, A, 0, (int)sb, 0, (int)sa);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; q++)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values8<E2M1>(b, q, scale_value(sb)), values8<A>(a, q, scale_value(sa)), acc, 0, 0, 0);
+    }
+  }
+};
 
 template <int A, bool EXACT, bool F32>
 __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleView b, const float* __restrict__ bias,
@@ -65,20 +81,43 @@ __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleVi
   const int64_t am = min((int64_t)m0 + r, (int64_t)a.rows - 1), bn = min((int64_t)n0 + r, (int64_t)b.rows - 1);
   const uint8_t *ar = a.codes + am * a.ld, *br = b.codes + bn * b.ld;
   const uint8_t *as = a.scale_row(am), *bs = b.scales + bn * b.ld_scales;
-  const int blocks = (a.cols + NB - 1) / NB, steps = (blocks + 3) / 4;
+  const int whole = a.cols / CB;
   cm_f32x4 acc = {0, 0, 0, 0};
-  for (int k = wave; k < steps; k += DW) {
-    const int kb = 4 * k + g, last = min(kb, blocks - 1);
-    const cm_i32x8 fa = fragment<A, !EXACT>(ar, k, g, a.cols), fb = fragment<E2M1, !EXACT>(br, k, g, a.cols);
-    // (past cols: the last block's scale, which counts a NaN that is in the result already)
-    const uint32_t sa = as[A == E2M1 ? last : last / 4], sb = bs[last];
-    if constexpr (!EXACT) {
-      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa, acc, E2M1, A, 0, (int)sb, 0, (int)sa);
-    } else {
+  for (int k0 = wave * DU; k0 < whole; k0 += DW * DU) {
+    DirectStep<A, EXACT> s[DU];
 #pragma unroll
-      for (int q = 0; q < 4; q++)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values8<E2M1>(fb, q, scale_value(sb)), values8<A>(fa, q, scale_value(sa)), acc, 0, 0, 0);
+    for (int u = 0; u < DU; u++) {
+      const int k = min(k0 + u, whole - 1);
+      const cm_i32x4 x = *reinterpret_cast<const cm_i32x4*>(br + (int64_t)k * 64 + g * 16);
+      s[u].b = cm_i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+      if constexpr (A == E2M1) {
+        const cm_i32x4 y = *reinterpret_cast<const cm_i32x4*>(ar + (int64_t)k * 64 + g * 16);
+        s[u].a = cm_i32x8{y[0], y[1], y[2], y[3], 0, 0, 0, 0};
+        s[u].sa = *reinterpret_cast<const uint32_t*>(as + 4 * k);
+      } else {
+        const uint8_t* at = ar + (int64_t)k * CB + g * (EXACT ? 32 : 16);
+        const cm_i32x4 y = *reinterpret_cast<const cm_i32x4*>(at), z = *reinterpret_cast<const cm_i32x4*>(at + (EXACT ? 16 : 64));
+        s[u].a = cm_i32x8{y[0], y[1], y[2], y[3], z[0], z[1], z[2], z[3]};
+        s[u].sa = as[k];
+      }
+      s[u].sb = *reinterpret_cast<const uint32_t*>(bs + 4 * k);
     }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < DU; u++) {
+      // the lane's byte of four; past the end the last step was read again: its codes count as zeros, which adds nothing
+      // but a NaN that is in the result already
+      if constexpr (A == E2M1) s[u].sa = (s[u].sa >> (8 * g)) & 0xffu;
+      s[u].sb = (s[u].sb >> (8 * g)) & 0xffu;
+      if (u > 0) s[u].b &= -(int)(k0 + u < whole);
+      s[u].add_to(acc);
+    }
+  }
+  if (a.cols % CB && wave == whole / DU % DW) {  // the columns that do not fill a step
+    const int last = min(4 * whole + g, (a.cols - 1) / NB);  // (past cols: zeros, with the last block's scale)
+    const DirectStep<A, EXACT> s = {fragment<A, !EXACT>(ar, whole, g, a.cols), fragment<E2M1, !EXACT>(br, whole, g, a.cols),
+                                    as[A == E2M1 ? last : whole], bs[last]};
+    s.add_to(acc);
   }
   if (wave > 0) part[wave - 1][lane] = acc;
   __syncthreads();
