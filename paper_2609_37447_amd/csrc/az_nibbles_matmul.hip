@@ -52,9 +52,11 @@ __device__ __forceinline__ cm_bf16x8 values8(const cm_i32x8& w, int i, float s) 
 }
 
 // Few rows of a.  A workgroup of eight waves owns 16 rows of a times 16 rows of b.  Each wave takes DU neighbouring
-// steps of 128 columns of every DW * DU, whose loads are on their way together and cover whole lines of b's rows; a lane holds a
-// block of 32 columns.  The waves' sums meet in LDS in the order of the waves.
-constexpr int DW = 8, DU = 4;
+// steps of 128 columns of every DW * DU: b's codes go through LDS of its own, copied as 512 neighbouring bytes of a row (chunks
+// exchanged by the row against bank conflicts), a row's scale bytes are loaded by four lanes and handed to the
+// others, a's codes come straight.  The waves' sums meet in LDS in the order of the waves.
+// 1 x 4672 x 8192, e4m3 a: XX us; with each lane loading its own blocks and scales of b 12.3.
+constexpr int DW = 8, DU = 8, DROW = DU * 64;  // bytes of a row of b that a wave has
 
 template <int A, bool EXACT>
 struct DirectStep {
@@ -74,7 +76,7 @@ struct DirectStep {
 template <int A, bool EXACT, bool F32>
 __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleView b, const float* __restrict__ bias,
                                                             void* __restrict__ out, int64_t ldo, int nt) {
-  __shared__ cm_f32x4 part[DW - 1][64];
+  __shared__ __attribute__((aligned(16))) uint8_t tiles[DW][16 * DROW];  // and the waves' sums, afterwards
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int m0 = (int)(blockIdx.x / (uint32_t)nt) * 16, n0 = (int)(blockIdx.x % (uint32_t)nt) * 16;
@@ -82,36 +84,58 @@ __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleVi
   const uint8_t *ar = a.codes + am * a.ld, *br = b.codes + bn * b.ld;
   const uint8_t *as = a.scale_row(am), *bs = b.scales + bn * b.ld_scales;
   const int whole = a.cols / CB;
-  cm_f32x4 acc = {0, 0, 0, 0};
+  // Rows past the matrix are out of the buffer's range and read as zeros.
+  const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(
+      b.codes + n0 * b.ld, 0, (min(b.rows - n0, 16) - 1) * (int)b.ld + (a.cols + NB - 1) / NB * 16, 0x00027000);
+  cm_f32x4 acc = {0, 0, 0, 0}, add = {0, 0, 0, 0};
+  if (bias && wave == 0) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) add[e] = bias[min((int64_t)n0 + 4 * g + e, (int64_t)b.rows - 1)];
+  }
   for (int k0 = wave * DU; k0 < whole; k0 += DW * DU) {
+    constexpr int CHUNKS = DROW / 16, ROWS = 64 / CHUNKS;  // of a row, and rows of a copy
+#pragma unroll
+    for (int j = 0; j < 16 / ROWS; j++) {
+      const int row = j * ROWS + lane / CHUNKS, chunk = lane % CHUNKS ^ row;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(bbuf, (lds_bytes*)&tiles[wave][j * 1024], 16, row * (int)b.ld + chunk * 16, k0 * 64, 0, 0);
+    }
+    // Steps 2 g and 2 g + 1 of the row; past the end the last one.
+    uint32_t sa[2], sb[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const int k = min(k0 + 2 * g + i, whole - 1);
+      sb[i] = *reinterpret_cast<const uint32_t*>(bs + 4 * k);
+      if constexpr (A == E2M1) sa[i] = *reinterpret_cast<const uint32_t*>(as + 4 * k);
+      else sa[i] = as[k];
+    }
     DirectStep<A, EXACT> s[DU];
 #pragma unroll
     for (int u = 0; u < DU; u++) {
       const int k = min(k0 + u, whole - 1);
-      const cm_i32x4 x = *reinterpret_cast<const cm_i32x4*>(br + (int64_t)k * 64 + g * 16);
-      s[u].b = cm_i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0};
       if constexpr (A == E2M1) {
         const cm_i32x4 y = *reinterpret_cast<const cm_i32x4*>(ar + (int64_t)k * 64 + g * 16);
         s[u].a = cm_i32x8{y[0], y[1], y[2], y[3], 0, 0, 0, 0};
-        s[u].sa = *reinterpret_cast<const uint32_t*>(as + 4 * k);
       } else {
         const uint8_t* at = ar + (int64_t)k * CB + g * (EXACT ? 32 : 16);
         const cm_i32x4 y = *reinterpret_cast<const cm_i32x4*>(at), z = *reinterpret_cast<const cm_i32x4*>(at + (EXACT ? 16 : 64));
         s[u].a = cm_i32x8{y[0], y[1], y[2], y[3], z[0], z[1], z[2], z[3]};
-        s[u].sa = as[k];
       }
-      s[u].sb = *reinterpret_cast<const uint32_t*>(bs + 4 * k);
     }
+    __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < DU; u++) {
-      // the lane's byte of four; past the end the last step was read again: its codes count as zeros, which adds nothing
-      // but a NaN that is in the result already
-      if constexpr (A == E2M1) s[u].sa = (s[u].sa >> (8 * g)) & 0xffu;
-      s[u].sb = (s[u].sb >> (8 * g)) & 0xffu;
+      const cm_i32x4 x = *reinterpret_cast<const cm_i32x4*>(&tiles[wave][r * DROW + (((4 * u + g) ^ r) * 16)]);
+      s[u].b = cm_i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+      // (past the end the codes count as zeros, which adds nothing but a NaN that is in the result already)
       if (u > 0) s[u].b &= -(int)(k0 + u < whole);
+      s[u].sb = (__shfl(sb[u & 1], r + 16 * (u >> 1)) >> (8 * g)) & 0xffu;
+      s[u].sa = __shfl(sa[u & 1], r + 16 * (u >> 1));
+      if constexpr (A == E2M1) s[u].sa = (s[u].sa >> (8 * g)) & 0xffu;
       s[u].add_to(acc);
     }
+    __builtin_amdgcn_s_waitcnt(0);  // the reads are back before the next copies overwrite what they read
+    __builtin_amdgcn_sched_barrier(0);
   }
   if (a.cols % CB && wave == whole / DU % DW) {  // the columns that do not fill a step
     const int last = min(4 * whole + g, (a.cols - 1) / NB);  // (past cols: zeros, with the last block's scale)
@@ -119,18 +143,21 @@ __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleVi
                                     as[A == E2M1 ? last : whole], bs[last]};
     s.add_to(acc);
   }
-  if (wave > 0) part[wave - 1][lane] = acc;
+  __syncthreads();  // every wave is done with its tile
+  cm_f32x4* const part = reinterpret_cast<cm_f32x4*>(&tiles[0][0]);
+  if (wave > 0) part[(wave - 1) * 64 + lane] = acc;
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
-  for (int w = 0; w < DW - 1; w++) acc += part[w][lane];
+  for (int w = 0; w < DW - 1; w++) acc += part[w * 64 + lane];
+  acc += add;
   const int64_t m = (int64_t)m0 + r;
   if (m >= a.rows) return;
 #pragma unroll
   for (int e = 0; e < 4; e++) {
     const int64_t n = (int64_t)n0 + 4 * g + e;
     if (n >= b.rows) continue;
-    const float v = acc[e] + (bias ? bias[n] : 0.0f);
+    const float v = acc[e];
     if constexpr (F32) ((float*)out)[m * ldo + n] = v;
     else ((uint16_t*)out)[m * ldo + n] = bf16_of(v);
   }
