@@ -170,26 +170,36 @@ __global__ __launch_bounds__(DW * 64) void az_nibble_direct(LeftView a, NibbleVi
 // LDS rows' 16-byte chunks are exchanged by the row's place (chunk ^ (row / 2) % chunks), which spreads the
 // rows that are read together over all banks; the copy into LDS puts lanes side by side, so that the exchange is
 // made on the source address.
+//
+// Scale bytes are copied for 512 columns at a time, 16 bytes of a row: a step's own 8 bytes of each row would be twice as many
+// requests as its codes.
 template <int A, int FA_, int FB_, int WM, int WN, bool EXACT, bool F32>
 struct Tiled {
   static constexpr int FA = FA_, FB = FB_, ACROSS = WM, TM = 32 * FA * WM, TN = 32 * FB * WN;
   static constexpr int STEP = A == E2M1 ? 256 : 128, SUBS = STEP / 64;  // columns, and matrix instructions a block
   static constexpr int BROW = STEP / 2;                                 // bytes of a row of b; a's are 128
   static constexpr int ASTEP = TM * 128, BSTEP = TN * BROW;
-  static constexpr int AW = A == E2M1 ? 2 : 1, BW = STEP / 128;         // words of scale bytes of a row
-  static constexpr int SA = TM < 64 ? 64 : TM;                          // a wave copies 64 rows' words
-  static constexpr int SCALES = ASTEP + BSTEP, WORDS = SA * AW + TN * BW;
-  static constexpr int STAGE = SCALES + WORDS * 4;
+  static constexpr int AW = A == E2M1 ? 2 : 1, BW = STEP / 128;         // words of scale bytes of a row that a step takes
+  static constexpr int GROUP = 512 / STEP;                              // steps that scales are copied for together
+  static constexpr int SROW = A == E2M1 ? 16 : 8;                       // bytes of a row of a's: e4m3's are two words, of which it has four bytes
+  static constexpr int SA = TM < 64 ? 64 : TM, ACOPIES = SA * SROW / (A == E2M1 ? 1024 : 256), COPIES = ACOPIES + TN / 64;
+  static constexpr int STAGE = ASTEP + BSTEP, SCALES = 2 * STAGE, SGROUP = SA * SROW + TN * 16;
+  static constexpr int USED = SCALES + 2 * SGROUP;
   static constexpr int OUT = TM * TN * (F32 ? 4 : 2) / (FA > 1 ? 2 : 1);  // what results need on their way out
-  static constexpr int LDS = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+  static constexpr int LDS = USED > OUT ? USED : OUT;
   static constexpr int AROWS = 32, BROWS = 4096 / BROW;                 // rows that one copy instruction of the workgroup fills
-  static constexpr int TURNS = (WORDS / 64 + 3) / 4;
-  static_assert(WM * WN == 4 && WORDS % 64 == 0 && TM % AROWS == 0 && TN % BROWS == 0, "four waves' work");
+  static constexpr int TURNS = (COPIES + 3) / 4;
+  static_assert(WM * WN == 4 && TM % AROWS == 0 && TN % BROWS == 0, "four waves' work");
 
   struct Frag {
     cm_i32x8 a[FA], b[FB];
   };
 
+  template <int BYTES>
+  static __device__ __forceinline__ void copy_scales(__amdgpu_buffer_rsrc_t rows, uint32_t off, int at, lds_bytes* to) {
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to, 16, off, at, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to, 4, off, at, 0, 0);
+  }
   template <int CHUNKS, int ROWS, int ROW>
   static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, int ld, uint32_t off, int at, lds_bytes* to) {
 #pragma unroll
@@ -282,8 +292,8 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_nibble_tiled(Le
   lds_bytes* const blds = (lds_bytes*)smem + K::ASTEP + K::BROWS / 4 * wave * K::BROW;
   // The part's steps, of which `whole` is the first that does not fill its columns or is not the part's.
   const int first = (int)blockIdx.y * part_steps, last = min(first + part_steps, (a.cols + K::STEP - 1) / K::STEP), whole = min(last, a.cols / K::STEP);
-  // Scales, by words, 64 a wave and turn: the first words of a's rows, their second ones, then b's.  Rows of 4-bit scales are whole
-  // words; of e4m3 ones, ScaleWords has the word that holds the byte.
+  // Scales: copies of 64 rows' 16 bytes, or of 32 rows' two words of an e4m3 matrix (ScaleWords: the word that holds a byte), a's
+  // and then b's, dealt to the waves in turn.
   const CodeView codes = {a.codes, a.scales, a.ld, a.rows, a.cols, (int)a.ld_scales, a.shift};
   const ScaleWords aw(codes);
   const __amdgpu_buffer_rsrc_t awords = A == E2M1 ? __builtin_amdgcn_make_buffer_rsrc(a.scales + m0 * a.ld_scales, 0, (ms - 1) * (int)a.ld_scales + ((blocks + 3) & ~3), 0x00027000) : aw.words;
@@ -291,30 +301,32 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_nibble_tiled(Le
   uint32_t srow[K::TURNS];
 #pragma unroll
   for (int i = 0; i < K::TURNS; i++) {
-    const int w = i * 256 + t;
-    if (w < K::SA * K::AW) {
-      const int row = min(w % K::SA, ms - 1);
-      srow[i] = A == E2M1 ? (uint32_t)row * (uint32_t)a.ld_scales + 4 * (w / K::SA) : aw.place(codes, m0 + row);
-    } else {
-      const int v = w - K::SA * K::AW;
-      srow[i] = (uint32_t)min(v % K::TN, ns - 1) * (uint32_t)b.ld_scales + 4 * (v / K::TN);
-    }
+    const int copy = i * 4 + wave;
+    if (copy >= K::ACOPIES) srow[i] = (uint32_t)min((copy - K::ACOPIES) * 64 + lane, ns - 1) * (uint32_t)b.ld_scales;
+    else if (A == E2M1) srow[i] = (uint32_t)min(copy * 64 + lane, ms - 1) * (uint32_t)a.ld_scales;
+    else srow[i] = (aw.place(codes, m0 + min(copy * 32 + lane / 2, ms - 1)) & ~3u) + 4 * (lane & 1);
   }
-  lds_bytes* const slds = (lds_bytes*)smem + K::SCALES + wave * 64 * 4;
+  lds_bytes* const slds = (lds_bytes*)smem + K::SCALES;
   // (past the last step: that step again, which nothing reads)
   auto fetch = [&](int kb) {
     const int stage = (kb & 1) * K::STAGE;
+    if (kb < whole && (kb % K::GROUP == 0 || kb == first)) {
+      const int group = kb / K::GROUP;
+      lds_bytes* const to = slds + (group & 1) * K::SGROUP;
+#pragma unroll
+      for (int i = 0; i < K::TURNS; i++) {
+        const int copy = i * 4 + wave;
+        if (copy < K::ACOPIES) {
+          if constexpr (A == E2M1) K::template copy_scales<16>(awords, srow[i], group * 16, to + copy * 1024);
+          else K::template copy_scales<4>(awords, srow[i], group * 4, to + copy * 256);
+        } else if (copy < K::COPIES) {
+          K::template copy_scales<16>(bwords, srow[i], group * 16, to + K::SA * K::SROW + (copy - K::ACOPIES) * 1024);
+        }
+      }
+    }
     kb = min(kb, whole - 1);
     K::template copy<K::TM / K::AROWS, K::AROWS, 128>(abuf, (int)a.ld, aoff, kb * 128, alds + stage);
     K::template copy<K::TN / K::BROWS, K::BROWS, K::BROW>(bbuf, (int)b.ld, boff, kb * K::BROW, blds + stage);
-#pragma unroll
-    for (int i = 0; i < K::TURNS; i++)
-      if (K::WORDS % 256 == 0 || i * 4 + wave < K::WORDS / 64) {
-        if (i * 4 + wave < K::SA * K::AW / 64)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(awords, slds + stage + i * 1024, 4, A == E2M1 ? srow[i] + 8 * kb : (srow[i] + kb) & ~3u, 0, 0, 0);
-        else
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(bwords, slds + stage + i * 1024, 4, srow[i] + 4 * K::BW * kb, 0, 0, 0);
-      }
   };
 
   // Reading: a lane holds row l % 32 of a block, its block of 32 columns l / 32.
@@ -322,27 +334,42 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_nibble_tiled(Le
   const int sa_ = (r >> 1) & 7, sb_ = (r >> 1) & (BC - 1);
   const uint8_t* ap = smem + (wm + r) * 128;
   const uint8_t* bp = smem + K::ASTEP + (wn + r) * K::BROW;
-  uint32_t ac[FA];  // e4m3: eight times the places of the lane's rows' scales
+  uint32_t ac[FA];  // e4m3: which byte of its first word the lane's row of scales begins with
 #pragma unroll
-  for (int i = 0; i < FA; i++) ac[i] = A == E2M1 ? 0 : 8 * aw.place(codes, m0 + min(wm + 32 * i + r, ms - 1));
+  for (int i = 0; i < FA; i++) ac[i] = A == E2M1 ? 0 : aw.place(codes, m0 + min(wm + 32 * i + r, ms - 1)) & 3;
   // A 4-bit operand's words are moved down by its lane's byte, so that 64 columns s have theirs at byte 2 (s % 2) of word s / 2.
   uint32_t sa[K::AW][FA], sb[K::BW][FB], na[K::AW][FA], nb[K::BW][FB];
   auto scale_words = [&](int kb) {
-    const uint32_t* from = reinterpret_cast<const uint32_t*>(smem + (kb & 1) * K::STAGE + K::SCALES) + r;
+    const uint8_t* from = smem + K::SCALES + (kb / K::GROUP & 1) * K::SGROUP;
+    const int at = kb % K::GROUP;
 #pragma unroll
-    for (int w = 0; w < K::AW; w++)
+    for (int i = 0; i < FA; i++) {
+      const uint8_t* row = from + (wm + 32 * i + r) * K::SROW;
+      if constexpr (A == E2M1) {
+        const cm_i32x2 w = *reinterpret_cast<const cm_i32x2*>(row + at * 8);
+        na[0][i] = (uint32_t)w[0];
+        na[K::AW - 1][i] = (uint32_t)w[1];
+      } else {
+        na[0][i] = *reinterpret_cast<const uint32_t*>(row + ((ac[i] + at) & 4));
+      }
+    }
 #pragma unroll
-      for (int i = 0; i < FA; i++) na[w][i] = from[w * K::SA + wm + 32 * i];
-#pragma unroll
-    for (int w = 0; w < K::BW; w++)
-#pragma unroll
-      for (int j = 0; j < FB; j++) nb[w][j] = from[K::SA * K::AW + w * K::TN + wn + 32 * j];
+    for (int j = 0; j < FB; j++) {
+      const uint8_t* row = from + K::SA * K::SROW + (wn + 32 * j + r) * 16;
+      if constexpr (K::BW == 2) {
+        const cm_i32x2 w = *reinterpret_cast<const cm_i32x2*>(row + at * 8);
+        nb[0][j] = (uint32_t)w[0];
+        nb[K::BW - 1][j] = (uint32_t)w[1];
+      } else {
+        nb[0][j] = *reinterpret_cast<const uint32_t*>(row + at * 4);
+      }
+    }
   };
   auto scales = [&](int kb) {
 #pragma unroll
     for (int w = 0; w < K::AW; w++)
 #pragma unroll
-      for (int i = 0; i < FA; i++) sa[w][i] = na[w][i] >> (A == E2M1 ? 8 * h : (int)((ac[i] + 8 * kb) & 31));
+      for (int i = 0; i < FA; i++) sa[w][i] = na[w][i] >> (A == E2M1 ? 8 * h : (int)(8 * (ac[i] + kb) & 31));
 #pragma unroll
     for (int w = 0; w < K::BW; w++)
 #pragma unroll
