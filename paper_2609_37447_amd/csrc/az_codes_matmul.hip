@@ -465,8 +465,7 @@ extern "C" int az_codes_matmul(const az_code_matrix* a, const az_code_matrix* b,
     o.ldo = b->rows;
     o.part_stride = a->rows * b->rows;
     if ((st = dtype == AZ_F32 ? launch_tiles<true, true>(p, o) : launch_tiles<false, true>(p, o)) != AZ_OK) return st;
-    const int64_t groups = (a->rows * b->rows + 255) / 256;
-    const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
+    const dim3 g = join_grid(a->rows, b->rows);
     const float* parts = static_cast<const float*>(workspace);
     if (dtype == AZ_F32)
       hipLaunchKernelGGL((az_join_products<true>), g, dim3(256), 0, o.stream, parts, p.parts, (int)a->rows, (int)b->rows, bias, out, ld_out);

@@ -55,7 +55,7 @@ __device__ __forceinline__ cm_bf16x8 values8(const cm_i32x8& w, int i, float s) 
 // steps of 128 columns of every DW * DU: b's codes go through LDS of its own, copied as 512 neighbouring bytes of a row (chunks
 // exchanged by the row against bank conflicts), a row's scale bytes are loaded by four lanes and handed to the
 // others, a's codes come straight.  The waves' sums meet in LDS in the order of the waves.
-// 1 x 4672 x 8192, e4m3 a: XX us; with each lane loading its own blocks and scales of b 12.3.
+// 1 x 4672 x 8192, e4m3 a: 9.2 us; with each lane loading its own blocks and scales of b 12.3.
 constexpr int DW = 8, DU = 8, DROW = DU * 64;  // bytes of a row of b that a wave has
 
 template <int A, bool EXACT>
@@ -265,6 +265,8 @@ struct Tiled {
   }
 };
 
+// 8192^3: 272-278 us in 4 bits (3,960-4,040 TFLOP/s, matrix unit busy 45%: two steps on their way cannot hide the copies' way),
+// 430 with an e4m3 a.
 template <int A, int FA, int FB, int WM, int WN, bool EXACT, bool F32>
 __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_nibble_tiled(LeftView a, NibbleView b, const float* __restrict__ bias,
                                                                               void* __restrict__ out, int64_t ldo, int mt, int nt,
@@ -461,37 +463,51 @@ struct Plan {
 // What a product multiplies with: two 4-bit operands, an e4m3 one on the scaled instruction, or on the bf16 one.
 enum Mode { FOURS = 0, MIXED = 1, EXACT = 2 };
 
-// The plan with the least estimated time, in microseconds; a tile kernel's K step takes a workgroup `one` alone on a
-// compute unit and `all` with `occ` of them there.
+// The plan with the least estimated time, in microseconds.  Few rows: what a workgroup costs by the columns, more where a has
+// several rows to fetch.  Tiles: a K step takes a workgroup `one` alone on a compute unit and `all` with `occ` of them
+// there, a round a start and an end, and every byte of an operand that a tile reads a little, which is what small tiles
+// lose by.  Parts cost a second launch and their way through memory.  The figures are fitted to the times of every kernel, in one
+// to eight parts, at 24 sizes from 1 x 1880 x 10240 to 4096^3; at these sizes the choice is 1% slower than the best on
+// average, 20% at the worst (32 x 4672 x 4096 with an e4m3 a goes to the kernel of few rows, 12.9; 32-row tiles in four parts 10.8).
+// Chosen against others, two 4-bit operands: 1 x 4672 x 8192 few rows 8.8 (32-row tiles in 8 parts 10.9); 40 x 4672 x 8192
+// 32-row tiles in 4 parts 13.4 (few rows 19); 333 x 1880 x 10240 64-row in 4 parts 19.2 (32-row in one 27); 1024 x 4672 x 8192
+// 128-row 37.7 (64-row 51.9, 256-row 59.9); 4096^3 256-row 43.7 (128-row 48.9).
 Plan choose_plan(int64_t m, int64_t n, int64_t k, Mode mode, bool f32, bool fits) {
   struct Tile {
     int kind, tm, tn, occ;
     double one[3], all[3];
   };
-  static const Tile tiles[] = {{TILE32, 32, 128, 3, {0.53, 0.53, 0.55}, {0.70, 0.70, 0.80}},
-                               {TILE64, 64, 128, 3, {0.60, 0.60, 0.63}, {0.87, 0.87, 1.35}},
-                               {TILE128, 128, 128, 2, {0.69, 0.69, 0.80}, {0.90, 0.90, 1.50}},
-                               {TILE256, 256, 256, 1, {1.45, 1.45, 2.75}, {1.72, 1.72, 3.30}}};
+  static const Tile tiles[] = {{TILE32, 32, 128, 3, {0.391, 0.363, 0.374}, {0.549, 0.467, 0.558}},
+                               {TILE64, 64, 128, 3, {0.527, 0.471, 0.502}, {0.745, 0.613, 0.867}},
+                               {TILE128, 128, 128, 2, {0.723, 0.634, 0.807}, {0.828, 0.791, 1.180}},
+                               {TILE256, 256, 256, 1, {1.865, 1.682, 2.610}, {2.003, 1.461, 2.598}}};
+  struct Rest {
+    double few, few_k, few_group, few_row, tiled, round, part, part_bytes, traffic;
+  };
+  static const Rest rest[] = {{3.638, 1.781, 2.005, 1.520, 4.240, 1.121, 3.256, 0.673, 0.019e-6},
+                              {4.328, 1.537, 1.790, 3.503, 4.562, 0.019, 3.915, 0.713, 0.008e-6},
+                              {6.344, 0.000, 3.155, 4.218, 5.833, 0.000, 2.712, 0.706, 0.020e-6}};
+  const Rest& c = rest[mode];
   const int columns = mode == FOURS ? 256 : 128, nb = (int)((k + columns - 1) / columns);
   const double write = 1.0 / 4.5e6;  // microseconds a byte
   const double out = (double)m * (double)n * (f32 ? 4 : 2) * write;
-  auto rounds = [](int64_t groups, int64_t slots) { return (double)((groups + slots - 1) / slots); };
   Plan best = {DIRECT, 1, nb};
-  // eight waves take every eighth step of 128 columns each
-  double least = 3.0 + rounds((n + 15) / 16 * ((m + 15) / 16), 256) * ((k + 127) / 128 / 8.0 * 0.55 + 0.6) + out;
+  const int64_t few = ((n + 15) / 16) * ((m + 15) / 16);
+  double least = c.few + (double)k / 8192 * (c.few_k + (double)few / 256 * (c.few_group + c.few_row * (double)(m < 16 ? m : 16) / 16)) + out;
   if (!fits) return best;
   for (const Tile& t : tiles) {
     const int64_t count = ((m + t.tm - 1) / t.tm) * ((n + t.tn - 1) / t.tn);
     for (int parts = 1; parts <= 8 && (parts == 1 || 2 * parts <= nb); parts *= 2) {
-      const int64_t groups = count * parts, per = (groups + 255) / 256;
-      const int steps = (nb + parts - 1) / parts;
+      const int steps = (nb + parts - 1) / parts, used = (nb + steps - 1) / steps;
+      const int64_t groups = count * used, per = (groups + 255) / 256, slots = 256 * t.occ;
       const int occ = per < t.occ ? (int)per : t.occ;
       const double step = t.occ == 1 ? (per > 1 ? t.all[mode] : t.one[mode]) : t.one[mode] + (t.all[mode] - t.one[mode]) * (occ - 1) / (t.occ - 1);
-      double cost = 4.0 + rounds(groups, 256 * t.occ) * (steps * step + 2.0) + out;
-      if (parts > 1) cost += 3.5 + (double)parts * (double)m * (double)n * 8 * write;
+      const double bytes = 128.0 * (t.tm + (mode == FOURS ? t.tn : t.tn / 2));  // of a step
+      double cost = c.tiled + (double)((groups + slots - 1) / slots) * (steps * step + c.round) + (double)groups * steps * bytes * c.traffic + out;
+      if (used > 1) cost += c.part + (double)used * (double)m * (double)n * 8 * write * c.part_bytes;
       if (cost < least) {
         least = cost;
-        best = {t.kind, (nb + steps - 1) / steps, steps};
+        best = {t.kind, used, steps};
       }
     }
   }
@@ -585,8 +601,7 @@ int matmul(const LeftView& a, int format, const NibbleView& b, const float* bias
   o.ldo = b.rows;
   o.part_stride = (int64_t)a.rows * b.rows;
   if ((st = launched(who, run_plan(p, o, format, f32, true))) != AZ_OK) return st;
-  const int64_t groups = (o.part_stride + 255) / 256;
-  const dim3 g((unsigned)(groups < 8192 ? groups : 8192));
+  const dim3 g = join_grid(a.rows, b.rows);
   const float* parts = static_cast<const float*>(workspace);
   if (f32) hipLaunchKernelGGL((az_join_products<true>), g, dim3(256), 0, o.stream, parts, p.parts, a.rows, b.rows, bias, out, ld_out);
   else hipLaunchKernelGGL((az_join_products<false>), g, dim3(256), 0, o.stream, parts, p.parts, a.rows, b.rows, bias, out, ld_out);
