@@ -96,6 +96,22 @@ struct Last {
   __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
 };
 
+// The sums of a wave's values up to each lane, by lane moves: within rows of 16, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t move_add(uint64_t x) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
+  return x + ((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
+  x = move_add<0x111, 0xf>(x);     // from the lane before
+  x = move_add<0x112, 0xf>(x);     // two before
+  x = move_add<0x114, 0xf>(x);     // four
+  x = move_add<0x118, 0xf>(x);     // eight
+  x = move_add<0x142, 0xa>(x);     // the last lane of rows 0 and 2 to rows 1 and 3
+  return move_add<0x143, 0xc>(x);  // lane 31 to the upper half
+}
+
 template <int NT>
 struct Sampler {
   static constexpr int BINS = 2 * NT, LIST = NT < 1024 ? 8 * NT : 4 * NT, FEW = 256, SLOTS = 64;
@@ -106,23 +122,20 @@ struct Sampler {
   uint64_t waves[NT / 64];
   uint64_t found[3];  // of a search: the bin (BINS: none), the sum before it, the bin's own
   uint64_t total;
+  uint64_t token_weight;
   double table[PARTS];
   uint32_t counts[BINS];
   uint2 list[LIST];  // logit, index
   uint32_t length, few;
   float wave_top[NT / 64];
-  uint32_t wave_allowed[NT / 64];
+  uint32_t wave_groups[NT / 64];
   int wave_bad[NT / 64];
   int token;
 
   // The sum of all threads' values before thread t's, and of all of them into `total` (after the next barrier).
   __device__ __forceinline__ uint64_t scan(uint64_t own) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint64_t s = own;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t x = __shfl_up((unsigned long long)s, o);
-      if (lane >= o) s += x;
-    }
+    const uint64_t s = wave_scan(own);
     if (lane == 63) waves[wave] = s;
     __syncthreads();
     uint64_t before = 0, all = 0;
@@ -135,10 +148,43 @@ struct Sampler {
   }
 };
 
+// What a thread has seen of a row: bits of the largest entries as signed numbers (of positive ones, and NaN and +inf above them), the
+// smallest and the largest as unsigned ones (of negative ones the largest, and NaN past -inf), in halves for bf16.
+template <bool BF16>
+struct Seen {
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t NOTHING = BF16 ? 0xff80ff80u : 0xff800000u;  // -inf
+  uint32_t high = BF16 ? 0x80008000u : 0x80000000u, low = NOTHING;
+  __device__ __forceinline__ void add(uint32_t w) {
+    if constexpr (BF16) {
+      high = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, high), __builtin_bit_cast(i16x2, w)));
+      low = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, low), __builtin_bit_cast(u16x2, w)));
+    } else {
+      high = (uint32_t)max((int32_t)high, (int32_t)w);
+      low = min(low, w);
+    }
+  }
+  static __device__ __forceinline__ uint32_t highest(uint32_t a, uint32_t b) {
+    if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    return max(a, b);
+  }
+  // The largest entry's bits in the upper half (bf16), and whether a NaN or +inf is among the entries.
+  __device__ __forceinline__ float largest() const {
+    if constexpr (!BF16) return __uint_as_float((int32_t)high >= 0 ? high : low);
+    const int32_t hi = max((int32_t)high >> 16, (int32_t)(high << 16) >> 16);
+    return __uint_as_float((hi >= 0 ? (uint32_t)hi : min(low >> 16, low & 0xffffu)) << 16);
+  }
+  __device__ __forceinline__ bool bad(uint32_t top) const {  // top: the largest as unsigned numbers
+    if constexpr (!BF16) return (int32_t)high >= 0x7f800000 || top > NOTHING;
+    return max((int32_t)high >> 16, (int32_t)(high << 16) >> 16) >= 0x7f80 || max(top >> 16, top & 0xffffu) > 0xff80u;
+  }
+};
+
 // A row in memory.  A thread takes eight entries at a time, AHEAD of which are on their way together.
 template <bool BF16, int NT>
 struct RowSource {
-  static constexpr int AHEAD = BF16 ? 4 : 2, WORDS = BF16 ? 4 : 8;
+  static constexpr int AHEAD = 4, WORDS = BF16 ? 4 : 8;
   const void* row;
   int vocab;
   __device__ __forceinline__ void load(int i, uint32_t (&w)[WORDS]) const {
@@ -146,6 +192,58 @@ struct RowSource {
   }
   static __device__ __forceinline__ float entry(const uint32_t (&w)[WORDS], int j) {
     return __uint_as_float(!BF16 ? w[j & (WORDS - 1)] : j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+  }
+  // The largest entry of each of the thread's AHEAD parts, whether a NaN or +inf is among them, and how many of its groups of
+  // eight hold anything above -inf (or not a number).
+  __device__ __forceinline__ void look(float (&top)[AHEAD], bool& bad, uint32_t& groups) const {
+    Seen<BF16> seen[AHEAD];
+    uint32_t high = 0;
+    groups = 0;
+    auto eight = [&](const uint32_t (&w)[WORDS], int a) {
+      uint32_t all = ~0u;
+#pragma unroll
+      for (int j = 0; j < WORDS; j++) {
+        seen[a].add(w[j]);
+        high = Seen<BF16>::highest(high, w[j]);
+        all &= w[j];
+      }
+      groups += all != Seen<BF16>::NOTHING;
+    };
+    int64_t i0 = threadIdx.x * 8;
+    for (; i0 + (AHEAD - 1) * NT * 8 + 8 <= vocab; i0 += AHEAD * NT * 8) {
+      uint32_t w[AHEAD][WORDS];
+#pragma unroll
+      for (int a = 0; a < AHEAD; a++) load((int)i0 + a * NT * 8, w[a]);
+#pragma unroll
+      for (int a = 0; a < AHEAD; a++) eight(w[a], a);
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; a++) {
+      if (i0 < vocab) {
+        uint32_t w[WORDS];
+        if (i0 + 8 <= vocab) {
+          load((int)i0, w);
+        } else {
+#pragma unroll
+          for (int j = 0; j < WORDS; j++) w[j] = Seen<BF16>::NOTHING;
+#pragma unroll
+          for (int j = 0; j < 8; j++)
+            if (i0 + j < vocab) {
+              const uint32_t l = __float_as_uint(single((int)i0 + j));
+              if constexpr (!BF16) w[j] = l;
+              else w[j >> 1] = j & 1 ? (w[j >> 1] & 0xffffu) | l : (w[j >> 1] & 0xffff0000u) | l >> 16;
+            }
+        }
+        eight(w, a);
+        i0 += NT * 8;
+      }
+    }
+    bad = false;
+#pragma unroll
+    for (int a = 0; a < AHEAD; a++) {
+      top[a] = seen[a].largest();
+      bad |= seen[a].bad(high);
+    }
   }
   __device__ __forceinline__ float single(int i) const {
     return BF16 ? f32_of_bf16(((const uint16_t*)row)[i]) : ((const float*)row)[i];
@@ -292,14 +390,12 @@ struct Row {
     src.each(lo, hi, [&](int i, float l) { s.slots[i - lo] = w(i, l); });
     __syncthreads();
     if (threadIdx.x < 64) {
-      const uint64_t own = s.slots[threadIdx.x];
-      uint64_t sum = own;
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t x = __shfl_up((unsigned long long)sum, o);
-        if ((int)threadIdx.x >= o) sum += x;
-      }
+      const uint64_t own = s.slots[threadIdx.x], sum = wave_scan(own);
       const uint64_t whole = __shfl((unsigned long long)sum, 63), want = limit_now(whole);
-      if (sum - own < want && want <= sum) s.token = lo + (int)threadIdx.x;
+      if (sum - own < want && want <= sum) {
+        s.token = lo + (int)threadIdx.x;
+        s.token_weight = own;
+      }
       if (threadIdx.x == 0) s.total = whole;
     }
     __syncthreads();
@@ -398,14 +494,17 @@ struct Row {
     return Last{(uint32_t)(got >> 32), (int)~(uint32_t)got};
   }
 
-  // Copies in(index, logit), at most LIST entries, to LDS.
+  // Copies in(index, logit) to LDS; the list's length is past LIST where they do not fit.
   template <class Src, class In>
   __device__ __forceinline__ ListSource<NT> gather(const Src& src, In&& in) {
     __syncthreads();
     if (threadIdx.x == 0) s.length = 0;
     __syncthreads();
     src.each(0, p.vocab, [&](int i, float l) {
-      if (in(i, l)) s.list[atomicAdd(&s.length, 1u)] = make_uint2(__float_as_uint(l), (uint32_t)i);
+      if (in(i, l)) {
+        const uint32_t at = atomicAdd(&s.length, 1u);
+        if (at < (uint32_t)S::LIST) s.list[at] = make_uint2(__float_as_uint(l), (uint32_t)i);
+      }
     });
     __syncthreads();
     return ListSource<NT>{s.list, s.length};
@@ -420,10 +519,7 @@ struct Row {
         [&](uint64_t sum) { return min((uint64_t)((double)u * (double)sum), sum - 1) + 1; }, all);
     if (threadIdx.x == 0) {
       p.out[b] = token;
-      if (p.prob) {
-        const float l = BF16 ? f32_of_bf16(((const uint16_t*)p.logits)[b * p.ld + token]) : ((const float*)p.logits)[b * p.ld + token];
-        p.prob[b] = (float)((double)weight(l) / (double)all);
-      }
+      if (p.prob) p.prob[b] = (float)((double)s.token_weight / (double)all);
     }
   }
 
@@ -434,33 +530,45 @@ struct Row {
     return [top_p](uint64_t sum) { return (uint64_t)fmax(ceil((double)top_p * (double)sum), 1.0); };
   }
 
-  // Filters and draw.  `allowed` entries are above -inf.
-  __device__ __forceinline__ void run(const RowSource<BF16, NT>& row, uint32_t allowed, int k, float top_p, float u, int64_t b) {
+  // Filters and draw over what is in LDS.
+  __device__ __forceinline__ void run_list(const ListSource<NT>& list, int k, float top_p, float u, int64_t b) {
     Last last = {NONE + 1, 0x7fffffff};
-    if (allowed <= S::LIST) {
-      const auto list = gather(row, [&](int, float l) { return l > -INFINITY; });
-      if (k < p.vocab) {
-        const Reached r = find_bin<true>(list, last, number(k));
-        if (r.bin < S::BINS) last = find_last<true>(list, last, r);
+    if (k < p.vocab) {
+      const Reached r = find_bin<true>(list, last, number(k));
+      if (r.bin < S::BINS) last = find_last<true>(list, last, r);
+    }
+    if (top_p < 1.0f) {
+      const Reached r = find_bin<false>(list, last, share(top_p));
+      last = find_last<false>(list, last, r);
+    }
+    draw(list, last, u, b);
+  }
+
+  // Filters and draw.  `part`: the largest entries of the thread's parts of the row; at most `allowed` are above -inf.
+  template <int PARTS_OF>
+  __device__ __forceinline__ void run(const RowSource<BF16, NT>& row, const float (&part)[PARTS_OF], uint32_t allowed, int k, float top_p, float u, int64_t b) {
+    Last last = {NONE + 1, 0x7fffffff};
+    if (allowed <= S::LIST) return run_list(gather(row, [&](int, float l) { return l > -INFINITY; }), k, top_p, u, b);
+    if (k <= PARTS_OF * NT / 2) {
+      // Of the k largest parts' largest entries the smallest is no larger than the k-th entry: what lies below it need not be
+      // looked at.  (Of normal logits some k to 1.4 k are left.)  Its bin's lower end, rounded down, is taken for it.
+      clear(false);
+#pragma unroll
+      for (int a = 0; a < PARTS_OF; a++) {
+        const int bin = bin_of(part[a]);
+        if (bin < S::BINS - 1) add(bin, 1);
       }
-      if (top_p < 1.0f) {
-        const Reached r = find_bin<false>(list, last, share(top_p));
-        last = find_last<false>(list, last, r);
+      reach(number(k));
+      if (s.found[0] < (uint64_t)S::BINS) {
+        const float least = top - (float)(s.found[0] + 1) / step * 1.00001f - fabsf(top) * 1e-6f;
+        const auto list = gather(row, [&](int, float l) { return l >= least && l > -INFINITY; });
+        if (list.length <= (uint32_t)S::LIST) return run_list(list, k, top_p, u, b);
       }
-      draw(list, last, u, b);
-      return;
     }
     if (k < p.vocab) {
       const Reached r = find_bin<true>(row, last, number(k));
       if (r.bin < S::BINS && r.upto <= S::LIST) {
-        const auto list = gather(row, [&](int, float l) { return bin_of(l) <= r.bin; });
-        last = find_last<true>(list, last, r);
-        if (top_p < 1.0f) {
-          const Reached q = find_bin<false>(list, last, share(top_p));
-          last = find_last<false>(list, last, q);
-        }
-        draw(list, last, u, b);
-        return;
+        return run_list(gather(row, [&](int, float l) { return bin_of(l) <= r.bin; }), k, top_p, u, b);
       }
       if (r.bin < S::BINS) last = find_last<true>(row, last, r);
     }
@@ -483,22 +591,23 @@ __global__ __launch_bounds__(NT, 4) void az_sample_rows(SampleView p) {
   Sampler<NT>& s = *reinterpret_cast<Sampler<NT>*>(smem);
   const int64_t b = blockIdx.x;
   const RowSource<BF16, NT> src = {(const uint8_t*)p.logits + b * p.ld * (BF16 ? 2 : 4), p.vocab};
-  float top = -INFINITY;
-  bool bad = false;
-  uint32_t allowed = 0;
-  src.each(0, p.vocab, [&](int, float l) {
-    top = fmaxf(top, l);
-    bad |= !(l < INFINITY);
-    allowed += l > -INFINITY;
-  });
+  // (the row's parameters are on their way while the row is looked at)
+  const float t = p.temperature ? p.temperature[b] : 1.0f, min_p = p.min_p ? p.min_p[b] : 0.0f, given_p = p.top_p ? p.top_p[b] : 1.0f, given_u = p.u[b];
+  const int given_k = p.top_k ? p.top_k[b] : 0;
+  float part[RowSource<BF16, NT>::AHEAD], top = -INFINITY;
+  bool bad;
+  uint32_t groups;
+  src.look(part, bad, groups);
+#pragma unroll
+  for (int a = 0; a < src.AHEAD; a++) top = fmaxf(top, part[a]);
   for (int o = 32; o > 0; o >>= 1) {
     top = fmaxf(top, __shfl_xor(top, o));
-    allowed += __shfl_xor(allowed, o);
+    groups += __shfl_xor(groups, o);
   }
   bad = __any(bad);
   if ((threadIdx.x & 63) == 0) {
     s.wave_top[threadIdx.x >> 6] = top;
-    s.wave_allowed[threadIdx.x >> 6] = allowed;
+    s.wave_groups[threadIdx.x >> 6] = groups;
     s.wave_bad[threadIdx.x >> 6] = bad;
   }
   if (threadIdx.x < PARTS) {
@@ -506,24 +615,22 @@ __global__ __launch_bounds__(NT, 4) void az_sample_rows(SampleView p) {
     s.table[threadIdx.x] = f < 0.5 ? power_of_two(f) : 2.0 * power_of_two(f - 1.0);
   }
   __syncthreads();
-  allowed = 0;
+  groups = 0;
   for (int w = 0; w < NT / 64; w++) {
     top = fmaxf(top, s.wave_top[w]);
-    allowed += s.wave_allowed[w];
+    groups += s.wave_groups[w];
     bad |= s.wave_bad[w] != 0;
   }
-  if (bad || allowed == 0) {
+  if (bad || top == -INFINITY) {
     if (threadIdx.x == 0) {
       p.out[b] = -1;
       if (p.prob) p.prob[b] = 0.0f;
     }
     return;
   }
-  const float t = p.temperature ? p.temperature[b] : 1.0f;
   const bool greedy = !(t > 0.0f);
   const float step = greedy ? 1.0f : fminf((float)Sampler<NT>::BINS / REACH / t, 0x1p100f);
-  float floor = p.min_p ? p.min_p[b] : 0.0f;
-  floor = floor > 0.0f ? fminf(floor, 1.0f) : 0.0f;
+  const float floor = min_p > 0.0f ? fminf(min_p, 1.0f) : 0.0f;
   Row<BF16, NT> row = {s, p, {(double)top, greedy ? 1.0 : 46.166241308446828 / (double)t, ldexp((double)floor, p.shift), s.table, p.shift},
                        top, step, key_of(top)};
   if (greedy) {
@@ -535,12 +642,8 @@ __global__ __launch_bounds__(NT, 4) void az_sample_rows(SampleView p) {
     }
     return;
   }
-  int k = p.top_k ? p.top_k[b] : 0;
-  if (k <= 0 || k > p.vocab) k = p.vocab;
-  const float top_p = p.top_p && p.top_p[b] < 1.0f ? p.top_p[b] : 1.0f;
-  float u = p.u[b];
-  u = u > 0.0f ? fminf(u, 1.0f) : 0.0f;
-  row.run(src, allowed, k, top_p, u, b);
+  const int k = given_k <= 0 || given_k > p.vocab ? p.vocab : given_k;
+  row.run(src, part, groups < 0x10000000u ? groups * 8 : ~0u, k, given_p < 1.0f ? given_p : 1.0f, given_u > 0.0f ? fminf(given_u, 1.0f) : 0.0f, b);
 }
 
 template <bool BF16, int NT>
