@@ -496,7 +496,7 @@ class CodeMatrix:
             raise ValueError("scale_rows is 1 or 128")
         if rows <= 1:
             ld = -(-ld // 16) * 16
-        if rows and codes.untyped_storage().nbytes() - codes.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
+        if rows and width < -(-cols // 16) * 16 and codes.untyped_storage().nbytes() - codes.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
             raise ValueError("codes must hold whole chunks of 16 bytes in every row")
         want = (-(-rows // scale_rows), -(-cols // AZ_CODE_BLOCK))
         if not scales.is_cuda or scales.dtype != torch.uint8 or tuple(scales.shape) != want or not scales.is_contiguous():
@@ -536,9 +536,9 @@ class Fp4Matrix:
             raise ValueError(f"scales {[srows, swidth]} are not [{rows}, {blocks} or more]")
         if rows <= 1:
             ld, lds = -(-ld // 16) * 16, -(-lds // 4) * 4
-        if rows and codes.untyped_storage().nbytes() - codes.storage_offset() < (rows - 1) * ld + 16 * blocks:
+        if rows and width < 16 * blocks and codes.untyped_storage().nbytes() - codes.storage_offset() < (rows - 1) * ld + 16 * blocks:
             raise ValueError("codes must hold whole chunks of 16 bytes in every row")
-        if rows and scales.untyped_storage().nbytes() - scales.storage_offset() < (rows - 1) * lds + -(-blocks // 4) * 4:
+        if rows and swidth % 4 and scales.untyped_storage().nbytes() - scales.storage_offset() < (rows - 1) * lds + -(-blocks // 4) * 4:
             raise ValueError("scales must hold whole words of 4 bytes in every row")
         if scales.device != codes.device:
             raise ValueError("codes and scales are on different devices")
@@ -569,7 +569,7 @@ def _on(device, stream, *others):
 def _call(device, fn, *args) -> int:
     """fn(*args) with `device` as the current one."""
     import torch
-    if device.index == torch.cuda.current_device():
+    if device.index == torch._C._cuda_getDevice():  # (tensors are on the device: CUDA has been initialised)
         return fn(*args)
     with torch.cuda.device(device):
         return fn(*args)
