@@ -471,7 +471,8 @@ enum Mode { FOURS = 0, MIXED = 1, EXACT = 2 };
 // average, 20% at the worst (32 x 4672 x 4096 with an e4m3 a goes to the kernel of few rows, 12.9; 32-row tiles in four parts 10.8).
 // Chosen against others, two 4-bit operands: 1 x 4672 x 8192 few rows 8.8 (32-row tiles in 8 parts 10.9); 40 x 4672 x 8192
 // 32-row tiles in 4 parts 13.4 (few rows 19); 333 x 1880 x 10240 64-row in 4 parts 19.2 (32-row in one 27); 1024 x 4672 x 8192
-// 128-row 37.7 (64-row 51.9, 256-row 59.9); 4096^3 256-row 43.7 (128-row 48.9).
+// 128-row 37.7 (64-row 51.9, 256-row 59.9); 4096^3 256-row 43.7 (128-row 48.9).  The 256-row tile is not used in parts, where it
+// was never the best by more than the noise, nor for fp32 results of an e4m3 a (4096^3: 110, 128-row 115).
 Plan choose_plan(int64_t m, int64_t n, int64_t k, Mode mode, bool f32, bool fits) {
   struct Tile {
     int kind, tm, tn, occ;
@@ -480,7 +481,7 @@ Plan choose_plan(int64_t m, int64_t n, int64_t k, Mode mode, bool f32, bool fits
   static const Tile tiles[] = {{TILE32, 32, 128, 3, {0.391, 0.363, 0.374}, {0.549, 0.467, 0.558}},
                                {TILE64, 64, 128, 3, {0.527, 0.471, 0.502}, {0.745, 0.613, 0.867}},
                                {TILE128, 128, 128, 2, {0.723, 0.634, 0.807}, {0.828, 0.791, 1.180}},
-                               {TILE256, 256, 256, 1, {1.865, 1.682, 2.610}, {2.003, 1.461, 2.598}}};
+                               {TILE256, 256, 256, 1, {1.865, 1.682, 0.0}, {2.003, 1.461, 0.0}}};
   struct Rest {
     double few, few_k, few_group, few_row, tiled, round, part, part_bytes, traffic;
   };
@@ -496,8 +497,9 @@ Plan choose_plan(int64_t m, int64_t n, int64_t k, Mode mode, bool f32, bool fits
   double least = c.few + (double)k / 8192 * (c.few_k + (double)few / 256 * (c.few_group + c.few_row * (double)(m < 16 ? m : 16) / 16)) + out;
   if (!fits) return best;
   for (const Tile& t : tiles) {
+    if (t.kind == TILE256 && mode == EXACT) continue;
     const int64_t count = ((m + t.tm - 1) / t.tm) * ((n + t.tn - 1) / t.tn);
-    for (int parts = 1; parts <= 8 && (parts == 1 || 2 * parts <= nb); parts *= 2) {
+    for (int parts = 1; parts <= (t.kind == TILE256 ? 1 : 8) && (parts == 1 || 2 * parts <= nb); parts *= 2) {
       const int steps = (nb + parts - 1) / parts, used = (nb + steps - 1) / steps;
       const int64_t groups = count * used, per = (groups + 255) / 256, slots = 256 * t.occ;
       const int occ = per < t.occ ? (int)per : t.occ;
@@ -546,10 +548,12 @@ int launch_tiled(const Plan& p, const Operands& o) {
 
 template <int A, bool EXACT, bool F32>
 int launch_tiles(const Plan& p, const Operands& o) {
-  return p.kind == TILE256   ? launch_tiled<A, 4, 4, 2, 2, EXACT, F32>(p, o)
-         : p.kind == TILE128 ? launch_tiled<A, 2, 2, 2, 2, EXACT, F32>(p, o)
-         : p.kind == TILE64  ? launch_tiled<A, 1, 2, 2, 2, EXACT, F32>(p, o)
-                             : launch_tiled<A, 1, 1, 1, 4, EXACT, F32>(p, o);
+  if constexpr (A == E2M1 || !F32) {
+    if (p.kind == TILE256) return launch_tiled<A, 4, 4, 2, 2, EXACT, F32>(p, o);
+  }
+  return p.kind == TILE128  ? launch_tiled<A, 2, 2, 2, 2, EXACT, F32>(p, o)
+         : p.kind == TILE64 ? launch_tiled<A, 1, 2, 2, 2, EXACT, F32>(p, o)
+                            : launch_tiled<A, 1, 1, 1, 4, EXACT, F32>(p, o);
 }
 
 // A tile's offsets stay below 2^30.
