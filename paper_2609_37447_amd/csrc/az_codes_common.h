@@ -152,18 +152,19 @@ __device__ __forceinline__ uint32_t finite_size(float x) {
 
 // N elements of a row of `cols` from column c on, as they lie in memory.  It is read 16 bytes at a time at any alignment
 // of the elements; where the row ends before the N do, its last N are read, and moved down when they are looked
-// at, so that no load waits for another.  WHOLE_CHUNKS: cols is a multiple of N, and what is read from cols on is the row's last
-// N as they are: without branches.
-template <bool BF16, int N, bool WHOLE_CHUNKS = false>
+// at, so that no load waits for another.  EDGE says what cols is: a multiple of N (EVEN: what is read from cols on is the row's
+// last N as they are, without branches), N or more (PARTLY), or anything.
+enum { EVEN = 0, PARTLY = 1, ANY = 2 };
+template <bool BF16, int N, int EDGE = ANY>
 struct Raw {
   static constexpr int WORDS = BF16 ? N / 2 : N;
   uint32_t w[WORDS];
   int down;
   __device__ __forceinline__ void load(const void* x, int64_t row, int c, int cols) {
     down = 0;
-    if (WHOLE_CHUNKS || cols >= N) {
+    if (EDGE != ANY || cols >= N) {
       const int at = min(c, cols - N);
-      if constexpr (!WHOLE_CHUNKS) down = min(c - at, N);
+      if constexpr (EDGE != EVEN) down = min(c - at, N);
       __builtin_memcpy(w, (const uint8_t*)x + (row + at) * (BF16 ? 2 : 4), WORDS * 4);
     } else {
 #pragma unroll
@@ -183,7 +184,7 @@ struct Raw {
       if constexpr (BF16) v[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
       else v[i] = __uint_as_float(w[i]);
     }
-    if (!WHOLE_CHUNKS && down) {
+    if (EDGE != EVEN && down) {
 #pragma unroll
       for (int s = N; s > 0; s >>= 1)
 #pragma unroll
@@ -227,10 +228,10 @@ __device__ __forceinline__ void store16(uint8_t* row, int c, int cols, const cm_
   }
 }
 
-// Writes N values to a dense row from column c on, none past cols (WHOLE_CHUNKS: all N are before it).
-template <bool BF16, int N, bool WHOLE_CHUNKS = false>
+// Writes N values to a dense row from column c on, none past cols.
+template <bool BF16, int N, int EDGE = ANY>
 __device__ __forceinline__ void put(void* x, int64_t row, int c, int cols, const float (&v)[N]) {
-  if (WHOLE_CHUNKS || c + N <= cols) {
+  if (EDGE == EVEN || c + N <= cols) {
     if constexpr (BF16) {
       uint32_t u[N / 2];
 #pragma unroll

@@ -110,14 +110,14 @@ __device__ __forceinline__ void store_block(uint8_t* row, int c, int cols, const
   }
 }
 
-// EVEN: cols is a multiple of a load.
-template <bool BF16, bool EVEN>
+// EDGE: of the loads.
+template <bool BF16, int EDGE>
 __global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x, int64_t ldx, NibbleView q, NibbleView qt, int nt) {
   __shared__ cm_f32x4 tile[TROWS * 32];
   constexpr int N = BF16 ? 8 : 4, LANES = 128 / N, LOADS = TROWS * LANES / NT;  // columns of a load, and loads of a thread
   const int rb = (int)(blockIdx.x / (uint32_t)nt), kb = (int)(blockIdx.x % (uint32_t)nt);
   const int t = threadIdx.x, r0 = rb * TROWS, c0 = kb * 128, rows = min(q.rows - r0, TROWS), cl = t % LANES * N;
-  Raw<BF16, N, EVEN> raw[LOADS];
+  Raw<BF16, N, EDGE> raw[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; i++) {
     const int r = min(i * (NT / LANES) + t / LANES, rows - 1);
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(NT) void az_nibble_tiles(const void* __restrict__ x
     const int r = i * (NT / LANES) + t / LANES;
     float v[N];
     raw[i].settle(v);
-    const bool live = r < rows && (!EVEN || c0 + cl < q.cols);
+    const bool live = r < rows && (EDGE != EVEN || c0 + cl < q.cols);
 #pragma unroll
     for (int k = 0; k < N / 4; k++)
       tile[place_of(r, cl / 4 + k)] = live ? cm_f32x4{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]} : cm_f32x4{0, 0, 0, 0};
@@ -232,8 +232,9 @@ int launch_quantize(const void* x, int64_t ldx, const NibbleView& q, const Nibbl
   const int64_t mt = ((int64_t)q.rows + TROWS - 1) / TROWS, nt = (q.cols + 127) / 128;
   if (!grid_fits(mt * nt, NT)) return AZ_ERR_UNSUPPORTED;
   const dim3 g((unsigned)(mt * nt));
-  if (q.cols % (BF16 ? 8 : 4) == 0) hipLaunchKernelGGL((az_nibble_tiles<BF16, true>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
-  else hipLaunchKernelGGL((az_nibble_tiles<BF16, false>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
+  if (q.cols % (BF16 ? 8 : 4) == 0) hipLaunchKernelGGL((az_nibble_tiles<BF16, EVEN>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
+  else if (q.cols >= 8) hipLaunchKernelGGL((az_nibble_tiles<BF16, PARTLY>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
+  else hipLaunchKernelGGL((az_nibble_tiles<BF16, ANY>), g, dim3(NT), 0, s, x, ldx, q, *qt, (int)nt);
   return AZ_OK;
 }
 

@@ -77,10 +77,10 @@ __device__ __forceinline__ float inverse_root(double squares, int cols, float ep
   return (float)(1.0 / sqrt(squares / cols + (double)eps));
 }
 
-// What h comes from, a group from c on: on its way, and added up.  EVEN, here and below: cols is a multiple of a group.
-template <bool BF16, bool EVEN>
+// What h comes from, a group from c on: on its way, and added up.  EDGE, here and below: of its groups.
+template <bool BF16, int EDGE>
 struct Stream {
-  Raw<BF16, PER, EVEN> x, residual;
+  Raw<BF16, PER, EDGE> x, residual;
   __device__ __forceinline__ void load(const NormView& p, int64_t r, int c) {
     x.load(p.x, r * p.ld_x, c, p.cols);
     if (p.residual) residual.load(p.residual, r * p.ld_residual, c, p.cols);
@@ -100,19 +100,19 @@ struct Stream {
 };
 
 // The results of a group; the 16 lanes of a block of 128 columns call it together.
-template <bool BF16, bool EVEN>
+template <bool BF16, int EDGE>
 __device__ __forceinline__ void results8(const NormView& p, int64_t r, int c, float inv, const float (&w)[PER], float (&v)[PER]) {
 #pragma unroll
   for (int i = 0; i < PER; i++) v[i] = v[i] * inv * w[i];
-  if (p.y && c < p.cols) put<BF16, PER, EVEN>(p.y, r * p.ld_y, c, p.cols, v);
+  if (p.y && c < p.cols) put<BF16, PER, EDGE>(p.y, r * p.ld_y, c, p.cols, v);
   if (p.codes) {
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < PER; i++) {
-      if (!EVEN && c + i >= p.cols) v[i] = 0.0f;  // (NaN of a NaN row)
+      if (EDGE != EVEN && c + i >= p.cols) v[i] = 0.0f;  // (NaN of a NaN row)
       a = max(a, finite_size(v[i]));
     }
-    if (EVEN && c >= p.cols) a = 0;
+    if (EDGE == EVEN && c >= p.cols) a = 0;
     a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xb1, 0xf, 0xf, false));
     a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4e, 0xf, 0xf, false));
     a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x141, 0xf, 0xf, false));
@@ -122,7 +122,7 @@ __device__ __forceinline__ void results8(const NormView& p, int64_t r, int c, fl
     if (c < p.cols) {
       uint64_t u = codes4(v, scale) | (uint64_t)codes4(v + 4, scale) << 32;
       uint8_t* to = p.codes + r * p.ld_codes + c;
-      if (EVEN || c + PER <= p.cols) {
+      if (EDGE == EVEN || c + PER <= p.cols) {
         *reinterpret_cast<uint64_t*>(to) = u;
       } else {
         for (int i = c; i < p.cols; i++, u >>= 8) *to++ = (uint8_t)u;
@@ -133,10 +133,10 @@ __device__ __forceinline__ void results8(const NormView& p, int64_t r, int c, fl
 }
 
 // A group's weights.
-template <bool EVEN>
+template <int EDGE>
 __device__ __forceinline__ void weights8(const float* weight, int c, int cols, float (&w)[PER]) {
   if (weight) {
-    Raw<false, PER, EVEN> raw;
+    Raw<false, PER, EDGE> raw;
     raw.load(weight, 0, min(c, cols - 1), cols);
     raw.settle(w);
   } else {
@@ -146,9 +146,8 @@ __device__ __forceinline__ void weights8(const float* weight, int c, int cols, f
 }
 
 // A thread has G groups, a row's threads' groups side by side.  Threads without a row or a column read one that there is.
-// 16384 x 4096 bf16 with a residual into codes: 85-89 us, 5.3-5.5 TB/s (with branches about a row's end 127-141, as where
-// cols is no multiple of 8); 333 x 10240 fp32: 9.5; one row of 8,192: 4.3.
-template <bool BF16, bool EVEN, int T, int G>
+// 16384 x 4096 bf16 with a residual into codes: 85-89 us, 5.3-5.5 TB/s (16384 x 4095, whose rows begin anywhere: 124); 333 x 10240 fp32: 9.5; one row of 8,192: 4.3.
+template <bool BF16, int EDGE, int T, int G>
 __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_rows(NormView p) {
   constexpr int ROWS = T == WHOLE ? 1 : 256 / (T ? T : 1);
   __shared__ double red[2][16][1];
@@ -156,18 +155,18 @@ __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_rows(NormView
   int turn = 0;
   for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < p.rows; r0 += (int64_t)gridDim.x * ROWS, turn++) {
     const int64_t r = r0 + (T == WHOLE ? 0 : threadIdx.x / threads), at = min(r, p.rows - 1);
-    Stream<BF16, EVEN> x[G];
+    Stream<BF16, EDGE> x[G];
     float v[G][PER], w[G][PER];
     double s[1] = {0.0};
 #pragma unroll
     for (int g = 0; g < G; g++) x[g].load(p, at, min((g * threads + t) * PER, p.cols - 1));
 #pragma unroll
-    for (int g = 0; g < G; g++) weights8<EVEN>(p.weight, (g * threads + t) * PER, p.cols, w[g]);
+    for (int g = 0; g < G; g++) weights8<EDGE>(p.weight, (g * threads + t) * PER, p.cols, w[g]);
 #pragma unroll
     for (int g = 0; g < G; g++) {
       const int c = (g * threads + t) * PER;
       x[g].sum(p, v[g]);
-      if (r < p.rows && c < p.cols && p.sum) put<BF16, PER, EVEN>(p.sum, r * p.ld_sum, c, p.cols, v[g]);
+      if (r < p.rows && c < p.cols && p.sum) put<BF16, PER, EDGE>(p.sum, r * p.ld_sum, c, p.cols, v[g]);
       double sum = 0.0;
 #pragma unroll
       for (int i = 0; i < PER; i++) sum = fma((double)v[g][i], (double)v[g][i], sum);
@@ -178,7 +177,7 @@ __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_rows(NormView
     const float inv = inverse_root(s[0], p.cols, p.eps);
     if (r < p.rows) {
 #pragma unroll
-      for (int g = 0; g < G; g++) results8<BF16, EVEN>(p, r, (g * threads + t) * PER, inv, w[g], v[g]);
+      for (int g = 0; g < G; g++) results8<BF16, EDGE>(p, r, (g * threads + t) * PER, inv, w[g], v[g]);
     }
   }
 }
@@ -191,7 +190,7 @@ __global__ __launch_bounds__(1024) void az_norm_long(NormView p) {
   for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn++) {
     double s[1] = {0.0};
     for (int c = (int)threadIdx.x * PER; c < p.cols; c += MOST) {
-      Stream<BF16, false> x;
+      Stream<BF16, PARTLY> x;
       float v[PER];
       x.load(p, r, c);
       x.sum(p, v);
@@ -211,13 +210,13 @@ __global__ __launch_bounds__(1024) void az_norm_long(NormView p) {
     for (int c0 = 0; c0 < p.cols; c0 += MOST) {
       const int c = c0 + (int)threadIdx.x * PER;
       float v[PER] = {}, w[PER];
-      weights8<false>(p.weight, c, p.cols, w);
+      weights8<PARTLY>(p.weight, c, p.cols, w);
       if (c < p.cols) {
-        Stream<BF16, false> x;
+        Stream<BF16, PARTLY> x;
         x.load(again, r, c);
         x.sum(again, v);
       }
-      results8<BF16, false>(p, r, c, inv, w, v);
+      results8<BF16, PARTLY>(p, r, c, inv, w, v);
     }
   }
 }
@@ -236,9 +235,9 @@ struct GradView {
 };
 
 // What the gradients of a group come from.
-template <bool BF16, bool EVEN>
+template <bool BF16, int EDGE>
 struct GradStream {
-  Raw<BF16, PER, EVEN> h, dy, dsum;
+  Raw<BF16, PER, EDGE> h, dy, dsum;
   __device__ __forceinline__ void load(const GradView& p, int64_t r, int c) {
     h.load(p.h, r * p.ld_h, c, p.cols);
     dy.load(p.dy, r * p.ld_dy, c, p.cols);
@@ -255,7 +254,7 @@ __device__ __forceinline__ void grad_sums(double (&s)[2], const float (&w)[PER],
 }
 
 // dx of a group; o holds dsum.
-template <bool BF16, bool EVEN>
+template <bool BF16, int EDGE>
 __device__ __forceinline__ void input_grad8(const GradView& p, int64_t r, int c, float inv, float mean, const float (&w)[PER],
                                             const float (&h)[PER], const float (&d)[PER], float (&o)[PER]) {
 #pragma unroll
@@ -263,25 +262,26 @@ __device__ __forceinline__ void input_grad8(const GradView& p, int64_t r, int c,
     const float g = inv * (d[i] * w[i] - h[i] * inv * mean);
     o[i] = p.dsum ? g + o[i] : g;
   }
-  put<BF16, PER, EVEN>(p.dx, r * p.ld_dx, c, p.cols, o);
+  put<BF16, PER, EDGE>(p.dx, r * p.ld_dx, c, p.cols, o);
 }
 
 // Keeps the compiler from holding what it makes of these words over this point: they are unpacked again.
-template <bool BF16, bool EVEN>
-__device__ __forceinline__ void unpack_again(Raw<BF16, PER, EVEN>& x) {
+template <bool BF16, int EDGE>
+__device__ __forceinline__ void unpack_again(Raw<BF16, PER, EDGE>& x) {
 #pragma unroll
   for (int i = 0; i < x.WORDS; i++) asm volatile("" : "+v"(x.w[i]));
 }
 
 // Slot i takes the rows i, i + slots, ...  A row stays as it lies in memory, and is unpacked for its sums and for its results;
-// the next one is on its way meanwhile.  16384 x 4096 bf16 with dsum: 110 us and the join 4, 4.8 TB/s; 64 x 10240: 6.3.
-template <bool BF16, bool EVEN, int T, int G>
+// the next one is on its way meanwhile.  16384 x 4096 bf16 with dsum: 110 us with the join (4), 4.8 TB/s; 16384 x 4095: 142;
+// 64 x 10240: 6.3 and the join.
+template <bool BF16, int EDGE, int T, int G>
 __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_grad_rows(GradView p) {
   constexpr bool AHEAD = G == 1;  // (two groups' next row would not fit the registers)
   __shared__ double red[2][16][2];
   const int threads = threads_of_row<T>(), t = T == WHOLE ? (int)threadIdx.x : (int)threadIdx.x % threads;
   const int slot = T == WHOLE ? (int)blockIdx.x : (int)blockIdx.x * (256 / (T ? T : 1)) + (int)(threadIdx.x / threads);
-  GradStream<BF16, EVEN> next[G];
+  GradStream<BF16, EDGE> next[G];
   float w[G][PER], dw[G][PER] = {};
   auto fetch = [&](int64_t r) {
 #pragma unroll
@@ -289,11 +289,11 @@ __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_grad_rows(Gra
   };
   fetch(slot);
 #pragma unroll
-  for (int g = 0; g < G; g++) weights8<EVEN>(p.weight, (g * threads + t) * PER, p.cols, w[g]);
+  for (int g = 0; g < G; g++) weights8<EDGE>(p.weight, (g * threads + t) * PER, p.cols, w[g]);
   int turn = 0;
   for (int64_t r0 = 0; r0 < p.rows; r0 += p.slots, turn++) {
     const int64_t r = r0 + slot;
-    GradStream<BF16, EVEN> x[G];
+    GradStream<BF16, EDGE> x[G];
     double s[2] = {0.0, 0.0};
     if constexpr (!AHEAD) {
       if (r0 > 0) fetch(r);
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_grad_rows(Gra
         if (p.dsum) x[g].dsum.settle(o);
 #pragma unroll
         for (int i = 0; i < PER; i++) dw[g][i] = fmaf(d[i], h[i] * inv, dw[g][i]);
-        if (p.dx && c < p.cols) input_grad8<BF16, EVEN>(p, r, c, inv, mean, w[g], h, d, o);
+        if (p.dx && c < p.cols) input_grad8<BF16, EDGE>(p, r, c, inv, mean, w[g], h, d, o);
       }
     }
   }
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(T == WHOLE ? 1024 : 256) void az_norm_grad_rows(Gra
 #pragma unroll
     for (int g = 0; g < G; g++) {
       const int c = (g * threads + t) * PER;
-      if (c < p.cols) put<false, PER, EVEN>(p.parts, (int64_t)slot * p.cols, c, p.cols, dw[g]);
+      if (c < p.cols) put<false, PER, EDGE>(p.parts, (int64_t)slot * p.cols, c, p.cols, dw[g]);
     }
   }
 }
@@ -349,11 +349,11 @@ __global__ __launch_bounds__(1024) void az_norm_grad_long(GradView p) {
   for (int64_t r = blockIdx.x; r < p.rows; r += p.slots, turn++) {
     double s[2] = {0.0, 0.0};
     for (int c = (int)threadIdx.x * PER; c < p.cols; c += MOST) {
-      GradStream<BF16, false> x;
+      GradStream<BF16, PARTLY> x;
       float h[PER], d[PER], w[PER];
       x.h.load(p.h, r * p.ld_h, c, p.cols);
       x.dy.load(p.dy, r * p.ld_dy, c, p.cols);
-      weights8<false>(p.weight, c, p.cols, w);
+      weights8<PARTLY>(p.weight, c, p.cols, w);
       x.h.settle(h);
       x.dy.settle(d);
       grad_sums(s, w, h, d);
@@ -361,10 +361,10 @@ __global__ __launch_bounds__(1024) void az_norm_grad_long(GradView p) {
     row_sums<WHOLE, 2>(s, red, turn);
     const float inv = inverse_root(s[0], p.cols, p.eps), mean = (float)(s[1] * (double)inv / p.cols);
     for (int c = (int)threadIdx.x * PER; c < p.cols; c += MOST) {
-      GradStream<BF16, false> x;
+      GradStream<BF16, PARTLY> x;
       float h[PER], d[PER], w[PER], o[PER];
       x.load(p, r, c);
-      weights8<false>(p.weight, c, p.cols, w);
+      weights8<PARTLY>(p.weight, c, p.cols, w);
       x.h.settle(h);
       x.dy.settle(d);
       if (p.dsum) x.dsum.settle(o);
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(1024) void az_norm_grad_long(GradView p) {
             part[c + i] = r == blockIdx.x ? u : part[c + i] + u;
           }
       }
-      if (p.dx) input_grad8<BF16, false>(p, r, c, inv, mean, w, h, d, o);
+      if (p.dx) input_grad8<BF16, PARTLY>(p, r, c, inv, mean, w, h, d, o);
     }
   }
 }
@@ -421,29 +421,31 @@ int grad_slots(int64_t rows, int64_t cols) {
   return (int)(rows < slots ? rows : slots);
 }
 
-template <bool BF16, bool EVEN>
+template <bool BF16, int EDGE>
 void launch_norm(const NormView& p, hipStream_t s) {
   const Shape f = row_shape(p.cols);
   const int rows = f.threads == 16 ? 16 : f.threads == 64 ? 4 : 1;
   const int64_t need = (p.rows + rows - 1) / rows;
   const dim3 g((unsigned)(need < (1 << 20) ? need : 1 << 20));
   if (f.threads == 0) hipLaunchKernelGGL((az_norm_long<BF16>), g, dim3(1024), 0, s, p);
-  else if (f.threads == 16) hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, 16, 1>), g, dim3(256), 0, s, p);
-  else if (f.threads == 64) hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, 64, 1>), g, dim3(256), 0, s, p);
-  else if (f.groups == 1) hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, WHOLE, 1>), g, dim3(f.threads), 0, s, p);
-  else hipLaunchKernelGGL((az_norm_rows<BF16, EVEN, WHOLE, 2>), g, dim3(f.threads), 0, s, p);
+  else if (f.threads == 16 && p.cols < PER) hipLaunchKernelGGL((az_norm_rows<BF16, ANY, 16, 1>), g, dim3(256), 0, s, p);
+  else if (f.threads == 16) hipLaunchKernelGGL((az_norm_rows<BF16, EDGE, 16, 1>), g, dim3(256), 0, s, p);
+  else if (f.threads == 64) hipLaunchKernelGGL((az_norm_rows<BF16, EDGE, 64, 1>), g, dim3(256), 0, s, p);
+  else if (f.groups == 1) hipLaunchKernelGGL((az_norm_rows<BF16, EDGE, WHOLE, 1>), g, dim3(f.threads), 0, s, p);
+  else hipLaunchKernelGGL((az_norm_rows<BF16, EDGE, WHOLE, 2>), g, dim3(f.threads), 0, s, p);
 }
 
-template <bool BF16, bool EVEN>
+template <bool BF16, int EDGE>
 void launch_norm_grad(const GradView& p, hipStream_t s) {
   const Shape f = row_shape(p.cols);
   const int slots = f.threads == 16 ? 16 : f.threads == 64 ? 4 : 1;
   const dim3 g((unsigned)((p.slots + slots - 1) / slots));
   if (f.threads == 0) hipLaunchKernelGGL((az_norm_grad_long<BF16>), g, dim3(1024), 0, s, p);
-  else if (f.threads == 16) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, 16, 1>), g, dim3(256), 0, s, p);
-  else if (f.threads == 64) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, 64, 1>), g, dim3(256), 0, s, p);
-  else if (f.groups == 1) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, WHOLE, 1>), g, dim3(f.threads), 0, s, p);
-  else hipLaunchKernelGGL((az_norm_grad_rows<BF16, EVEN, WHOLE, 2>), g, dim3(f.threads), 0, s, p);
+  else if (f.threads == 16 && p.cols < PER) hipLaunchKernelGGL((az_norm_grad_rows<BF16, ANY, 16, 1>), g, dim3(256), 0, s, p);
+  else if (f.threads == 16) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EDGE, 16, 1>), g, dim3(256), 0, s, p);
+  else if (f.threads == 64) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EDGE, 64, 1>), g, dim3(256), 0, s, p);
+  else if (f.groups == 1) hipLaunchKernelGGL((az_norm_grad_rows<BF16, EDGE, WHOLE, 1>), g, dim3(f.threads), 0, s, p);
+  else hipLaunchKernelGGL((az_norm_grad_rows<BF16, EDGE, WHOLE, 2>), g, dim3(f.threads), 0, s, p);
 }
 
 bool norm_sizes(int64_t rows, int64_t cols) { return rows <= INT32_MAX && cols <= MAX_COLS; }
@@ -480,8 +482,8 @@ extern "C" int az_rms_norm(const az_norm* n, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   const bool even = n->cols % PER == 0;
-  if (n->dtype == AZ_BF16) even ? launch_norm<true, true>(p, s) : launch_norm<true, false>(p, s);
-  else even ? launch_norm<false, true>(p, s) : launch_norm<false, false>(p, s);
+  if (n->dtype == AZ_BF16) even ? launch_norm<true, EVEN>(p, s) : launch_norm<true, PARTLY>(p, s);
+  else even ? launch_norm<false, EVEN>(p, s) : launch_norm<false, PARTLY>(p, s);
   return launch_status(who);
 }
 
@@ -514,8 +516,8 @@ extern "C" int az_rms_norm_grad(const az_norm_grad* n, void* workspace, size_t w
     const GradView p = {n->dy, n->h, n->weight, n->dsum, n->dx, parts, n->ld_dy, n->ld_h, n->ld_dsum, n->ld_dx,
                         n->rows, (int)n->cols, slots, n->eps};
     const bool even = n->cols % PER == 0;
-    if (n->dtype == AZ_BF16) even ? launch_norm_grad<true, true>(p, s) : launch_norm_grad<true, false>(p, s);
-    else even ? launch_norm_grad<false, true>(p, s) : launch_norm_grad<false, false>(p, s);
+    if (n->dtype == AZ_BF16) even ? launch_norm_grad<true, EVEN>(p, s) : launch_norm_grad<true, PARTLY>(p, s);
+    else even ? launch_norm_grad<false, EVEN>(p, s) : launch_norm_grad<false, PARTLY>(p, s);
     if ((st = launch_status(who)) != AZ_OK) return st;
   }
   if (n->dweight) {
