@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from sys import modules as _modules  # (of calls on tensors, whose module is there: an import statement takes five times as long)
 
 import numpy as np
 
@@ -487,7 +488,7 @@ class CodeMatrix:
     __slots__ = ("codes", "scales", "rows", "cols", "scale_rows", "device", "c")
 
     def __init__(self, codes, scales, cols=None, scale_rows: int = 1):
-        import torch
+        torch = _modules["torch"]
         rows, width, ld = _rows_of("codes", codes, (torch.uint8,))
         cols = width if cols is None else int(cols)
         if not 0 < cols <= width:
@@ -525,7 +526,7 @@ class Fp4Matrix:
     __slots__ = ("codes", "scales", "rows", "cols", "device", "c")
 
     def __init__(self, codes, scales, cols=None):
-        import torch
+        torch = _modules["torch"]
         rows, width, ld = _rows_of("codes", codes, (torch.uint8,))
         srows, swidth, lds = _rows_of("scales", scales, (torch.uint8,))
         cols = 2 * width if cols is None else int(cols)
@@ -557,7 +558,7 @@ class Fp4Matrix:
 def _on(device, stream, *others):
     """The call's stream as the library takes it (torch's current one by default), for operands that are all
     on `device`."""
-    import torch
+    torch = _modules["torch"]
     for t in others:
         if t is not None and t.device != device:
             raise ValueError("the operands are on different devices")
@@ -568,7 +569,7 @@ def _on(device, stream, *others):
 
 def _call(device, fn, *args) -> int:
     """fn(*args) with `device` as the current one."""
-    import torch
+    torch = _modules["torch"]
     if device.index == torch._C._cuda_getDevice():  # (tensors are on the device: CUDA has been initialised)
         return fn(*args)
     with torch.cuda.device(device):
@@ -583,7 +584,7 @@ def _workspace(given, need, device, stream):
         return given.data_ptr(), given.numel() * given.element_size(), given
     if need == 0:
         return None, 0, None
-    import torch
+    torch = _modules["torch"]
     if stream is None:
         t = torch.empty((need,), dtype=torch.uint8, device=device)
     else:
@@ -593,7 +594,7 @@ def _workspace(given, need, device, stream):
 
 
 def _float_type(t) -> int:
-    import torch
+    torch = _modules["torch"]
     return AZ_BF16 if t.dtype == torch.bfloat16 else AZ_F32
 
 
@@ -601,7 +602,7 @@ def quantize_tensors(x, q, transposed=None, stream=None) -> int:
     """az_codes_quantize of x (float32 or bfloat16 [rows][cols]) into the CodeMatrix q and, for matrices with
     scale_rows 128, its transposed copy, or az_nibbles_quantize into the Fp4Matrix q and the transposed
     one; stream defaults to torch's current one."""
-    import torch
+    torch = _modules["torch"]
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
@@ -615,7 +616,7 @@ def quantize_tensors(x, q, transposed=None, stream=None) -> int:
 def dequantize_tensors(q, x, stream=None) -> int:
     """az_codes_dequantize (az_nibbles_dequantize) of the CodeMatrix (Fp4Matrix) q into x (float32 or bfloat16
     [rows][cols])."""
-    import torch
+    torch = _modules["torch"]
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     if (rows, cols) != (q.rows, q.cols):
         raise ValueError(f"x is {[rows, cols]}, the coded matrix {[q.rows, q.cols]}")
@@ -628,7 +629,7 @@ def matmul_tensors(a, b, out, bias=None, workspace=None, stream=None) -> int:
     az_nibbles_matmul of two Fp4Matrix, az_codes_nibbles_matmul of a CodeMatrix and an Fp4Matrix b.
     A workspace is made for the call (torch's allocator, on the call's stream) unless a tensor is
     given."""
-    import torch
+    torch = _modules["torch"]
     m, n, ld = _rows_of("out", out, (torch.float32, torch.bfloat16))
     if (m, n) != (a.rows, b.rows):
         raise ValueError(f"out is {[m, n]}, the product {[a.rows, b.rows]}")
@@ -652,7 +653,7 @@ def weight_grad_tensors(dy, x: CodeMatrix, dw, db=None, accumulate: bool = False
     """az_codes_weight_grad: dw [n][x.cols] (float32 or bfloat16) and db (float32 [n]) from dy
     (bfloat16 [x.rows][n]) and the layer's saved input x.  A workspace is made for the call
     (torch's allocator, on the call's stream) unless a tensor is given."""
-    import torch
+    torch = _modules["torch"]
     m, n, ldy = _rows_of("dy", dy, (torch.bfloat16,))
     if m != x.rows:
         raise ValueError(f"dy has {m} rows, x {x.rows}")
@@ -674,7 +675,7 @@ def policy_tensors(logits, out, mask=None, bias=None, history=None, lengths=None
     allowed) or int32 [rows][ceil(vocab / 32)] of bits; bias: float32 [vocab], [1][vocab] or
     [rows][vocab]; history: int32 [rows][entries] with lengths int32 [rows] (default: all) and penalties
     float32 [rows][3] (repetition, frequency, presence)."""
-    import torch
+    torch = _modules["torch"]
     b, v, ld = _rows_of("logits", logits, (torch.float32, torch.bfloat16))
     ob, ov, ldo = _rows_of("out", out, (torch.float32,))
     if (ob, ov) != (b, v):
@@ -729,7 +730,7 @@ def _like(name, t, like, rows, cols, ld):
 def norm_tensors(x, y=None, q: CodeMatrix = None, residual=None, sum=None, weight=None, eps: float = 1e-6, stream=None) -> int:
     """az_rms_norm of x (float32 or bfloat16 [rows][cols]) plus residual, with weight (float32 [cols]), into y and the
     coded matrix q; sum receives x + residual (it may be either's own tensor).  residual, sum and y are like x."""
-    import torch
+    torch = _modules["torch"]
     rows, cols, ld = _rows_of("x", x, (torch.float32, torch.bfloat16))
     pr, ldr = _like("residual", residual, x, rows, cols, ld)
     ps, lds = _like("sum", sum, x, rows, cols, ld)
@@ -749,7 +750,7 @@ def norm_grad_tensors(dy, h, dx=None, dsum=None, weight=None, dw=None, eps: floa
     """az_rms_norm_grad: dx (the gradient of x and of the residual) and dw (float32 [cols]) from dy and h (float32 or bfloat16
     [rows][cols]), h the sum that the norm gave; dsum: what else reaches h.  dy, dsum and dx are like
     h.  A workspace is made for the call (torch's allocator, on the call's stream) unless a tensor is given."""
-    import torch
+    torch = _modules["torch"]
     rows, cols, ld = _rows_of("h", h, (torch.float32, torch.bfloat16))
     pd, ldd = _like("dy", dy, h, rows, cols, ld)
     pr, ldr = _like("dsum", dsum, h, rows, cols, ld)
@@ -769,7 +770,7 @@ def sample_tensors(logits, u, out, prob=None, temperature=None, top_k=None, top_
     """az_logits_sample: an entry of each row of logits (float32 or bfloat16 [rows][vocab]) into out (int32 [rows]) and its
     probability into prob (float32 [rows]), from random numbers u in [0, 1); u, temperature, top_p and min_p
     float32 [rows], top_k int32 [rows]."""
-    import torch
+    torch = _modules["torch"]
     b, v, ld = _rows_of("logits", logits, (torch.float32, torch.bfloat16))
     for name, t, dtype in (("u", u, torch.float32), ("out", out, torch.int32), ("prob", prob, torch.float32),
                            ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
