@@ -145,6 +145,18 @@ def test_special_rows(vocab, dtype):
     assert got[0] == vocab // 2 and abs(prob[0] - 1.0 / vocab) < 1e-7 / vocab + 1e-12
 
 
+@pytest.mark.parametrize("vocab", [100, 4672, 20001])
+@pytest.mark.parametrize("temperature", [float("inf"), 3e38, 1e-38])
+def test_temperatures_at_the_ends_with_filters(vocab, temperature):
+    """The filters keep their beginning where all weights are alike, or all but one nothing."""
+    rng = _rng(vocab, 8)
+    t = _logits(rng, 10, vocab, "f32")
+    t[5:, 7:] = float("-inf")                  # fewer allowed than top_k asks for
+    u, heat = rng.random(10), np.full(10, temperature)
+    for kw in ({}, {"top_k": np.full(10, 33)}, {"top_p": np.full(10, 0.6)}, {"top_k": np.full(10, 50), "top_p": np.full(10, 0.41), "min_p": np.full(10, 0.5)}):
+        _check(t, u, temperature=heat, **kw)
+
+
 def test_frequencies():
     """Equally spaced u give every entry its share, to one draw."""
     import torch
