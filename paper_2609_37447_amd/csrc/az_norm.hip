@@ -1,9 +1,10 @@
 // Root-mean-square norm of rows with a residual's addition, into e4m3 codes or a dense matrix, and its gradients.
 //
-// Both are one pass over memory and bound by it: a row stays in registers between its sums and its results, and the
-// next row of the same threads is on its way meanwhile.  Sums over a row are fp64 (its rate is fp32's on this
-// chip, and no finite row overflows); everything after them is fp32, rounded once.  A block of 128 columns is 16
-// neighbouring lanes, which find its scale by lane exchanges.
+// Both are one pass over memory and bound by it: a row stays in registers between its sums and its results.  Rows of the norm
+// overlap as workgroups of one row each (a persistent grid with the next row on its way: 127 us for 87 at 16384 x 4096);
+// the gradient's workgroups keep sums over many rows, and fetch the next one meanwhile.  Sums over a row are fp64 (its
+// rate is fp32's on this chip, and no finite row overflows); everything after them is fp32, rounded once.  A block of
+// 128 columns is 16 neighbouring lanes, which find its scale by lane exchanges.
 #include <math.h>
 
 #include "az_codes_common.h"
