@@ -50,11 +50,11 @@ struct DirectStep {
   }
 };
 
-// 16 rows of a step, straight into 2 KB of LDS: a lane one chunk of row lane / 8 (`row` bytes in) and
+// 16 rows of a step, straight into 2 KB of LDS: a lane one chunk of row lane / 8 (`off` bytes in) and
 // of the row eight below, whose chunks are exchanged by 4 more.
-__device__ __forceinline__ void direct_copy(__amdgpu_buffer_rsrc_t rows, int ld, uint32_t row, int chunk, int at, lds_bytes* to) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to, 16, row + chunk * 16, at, 0, 0);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to + 1024, 16, row + (chunk ^ 4) * 16, at + 8 * ld, 0, 0);
+__device__ __forceinline__ void direct_copy(__amdgpu_buffer_rsrc_t rows, const uint32_t (&off)[2], int at, lds_bytes* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to, 16, off[0], at, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to + 1024, 16, off[1], at, 0, 0);
 }
 
 // EXACT: products on the bf16 instruction, fp32 out; otherwise on the e4m3 one, bf16 out.
@@ -69,13 +69,16 @@ __global__ __launch_bounds__(DW * 64) void az_matmul_direct(CodeView a, CodeView
   const int whole = a.cols / CB, width = (a.cols + 15) & ~15;
   const int am = min(m0 + r, a.rows - 1), bn = min(n0 + r, b.rows - 1);
   const uint8_t *as = a.scales + (int64_t)(am >> a.shift) * a.nb, *bs = b.scales + (int64_t)(bn >> b.shift) * b.nb;
-  // Chunks are exchanged by the row, as in the tiles below; rows past the matrix read as zeros.
-  const int crow = lane >> 3, chunk = (lane & 7) ^ ((crow >> 1) & 7);
-  const uint32_t arow = (uint32_t)crow * (uint32_t)a.ld, brow = (uint32_t)crow * (uint32_t)b.ld;
-  const __amdgpu_buffer_rsrc_t abuf =
-      __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, (min(a.rows - m0, 16) - 1) * (int)a.ld + width, 0x00027000);
-  const __amdgpu_buffer_rsrc_t bbuf =
-      __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, (min(b.rows - n0, 16) - 1) * (int)b.ld + width, 0x00027000);
+  // Chunks are exchanged by the row, as in the tiles below; for a row past the matrix, of no result, its last one is read.
+  const int crow = lane >> 3, chunk = (lane & 7) ^ ((crow >> 1) & 7), ms = min(a.rows - m0, 16), ns = min(b.rows - n0, 16);
+  uint32_t aoff[2], boff[2];
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    aoff[i] = (uint32_t)min(crow + 8 * i, ms - 1) * (uint32_t)a.ld + (chunk ^ 4 * i) * 16;
+    boff[i] = (uint32_t)min(crow + 8 * i, ns - 1) * (uint32_t)b.ld + (chunk ^ 4 * i) * 16;
+  }
+  const __amdgpu_buffer_rsrc_t abuf = __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, (ms - 1) * (int)a.ld + width, 0x00027000);
+  const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, (ns - 1) * (int)b.ld + width, 0x00027000);
   const int sw = (r >> 1) & 7, c0 = (g ^ sw) * 16, c1 = ((g + 4) ^ sw) * 16;  // (any columns do, if a and b agree)
   cm_f32x4 acc = {0, 0, 0, 0};
   for (int kb = wave; kb < whole; kb += DW * DU) {
@@ -83,8 +86,8 @@ __global__ __launch_bounds__(DW * 64) void az_matmul_direct(CodeView a, CodeView
 #pragma unroll
     for (int u = 0; u < DU; u++) {
       const int k = min(kb + u * DW, whole - 1);
-      direct_copy(abuf, (int)a.ld, arow, chunk, k * CB, (lds_bytes*)&tiles[wave][u][0][0]);
-      direct_copy(bbuf, (int)b.ld, brow, chunk, k * CB, (lds_bytes*)&tiles[wave][u][1][0]);
+      direct_copy(abuf, aoff, k * CB, (lds_bytes*)&tiles[wave][u][0][0]);
+      direct_copy(bbuf, boff, k * CB, (lds_bytes*)&tiles[wave][u][1][0]);
       s[u].sa = as[k];
       s[u].sb = bs[k];
     }
@@ -152,13 +155,12 @@ struct Tiled {
     cm_i32x8 a[FA], b[FB];
   };
 
-  // A thread's chunks of a step, one of each ROWS rows: `off` within the step's first rows, `at`
-  // the step's place in the tile.
+  // A thread's chunks of a step, one of each ROWS rows: `off` in the tile's first step, `at` the step's
+  // place in a row.
   template <int CHUNKS>
-  static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, int ld, uint32_t off, int at, lds_bytes* to) {
+  static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t tile, const uint32_t* off, int at, lds_bytes* to) {
 #pragma unroll
-    for (int j = 0; j < CHUNKS; j++)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * ROWS * CB, 16, off, at + j * ROWS * ld, 0, 0);
+    for (int j = 0; j < CHUNKS; j++) __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, to + j * ROWS * CB, 16, off[j], at, 0, 0);
   }
   static __device__ __forceinline__ void scale_words(__amdgpu_buffer_rsrc_t words, lds_bytes* to, uint32_t at) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(words, to, 4, at, 0, 0, 0);
@@ -224,10 +226,15 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(Co
   const int m0 = max(min(tm * K::TM, a.rows - K::TM), 0), n0 = max(min(tn * K::TN, b.rows - K::TN), 0);
   const int ms = min(a.rows, K::TM), ns = min(b.rows, K::TN);
 
-  // Copying: wave w of instruction j takes rows 32 j + 8 w .. + 7, a lane one chunk of one row.  Rows
-  // past the matrix are out of the buffer's range and read as zeros.
+  // Copying: wave w of instruction j takes rows 32 j + 8 w .. + 7, a lane one chunk of one row; for a
+  // row past the matrix, of no result, its last one, so that no copy of codes leaves the matrix whatever a
+  // buffer's range counts.
   const int crow = 8 * wave + (lane >> 3), chunk = (lane & 7) ^ ((crow >> 1) & 7);
-  const uint32_t aoff = (uint32_t)crow * (uint32_t)a.ld + chunk * 16, boff = (uint32_t)crow * (uint32_t)b.ld + chunk * 16;
+  uint32_t aoff[K::TM / 32], boff[K::TN / 32];
+#pragma unroll
+  for (int j = 0; j < K::TM / 32; j++) aoff[j] = (uint32_t)min(32 * j + crow, ms - 1) * (uint32_t)a.ld + chunk * 16;
+#pragma unroll
+  for (int j = 0; j < K::TN / 32; j++) boff[j] = (uint32_t)min(32 * j + crow, ns - 1) * (uint32_t)b.ld + chunk * 16;
   const int width = (a.cols + 15) & ~15;
   const __amdgpu_buffer_rsrc_t abuf = __builtin_amdgcn_make_buffer_rsrc(a.codes + m0 * a.ld, 0, (ms - 1) * (int)a.ld + width, 0x00027000);
   const __amdgpu_buffer_rsrc_t bbuf = __builtin_amdgcn_make_buffer_rsrc(b.codes + n0 * b.ld, 0, (ns - 1) * (int)b.ld + width, 0x00027000);
@@ -248,8 +255,8 @@ __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(Co
   auto fetch = [&](int kb) {
     const int stage = (kb & 1) * K::STAGE;
     kb = min(kb, whole - 1);
-    K::template copy<K::TM / 32>(abuf, (int)a.ld, aoff, kb * CB, lds0 + stage);
-    K::template copy<K::TN / 32>(bbuf, (int)b.ld, boff, kb * CB, lds0 + stage + K::ASTEP);
+    K::template copy<K::TM / 32>(abuf, aoff, kb * CB, lds0 + stage);
+    K::template copy<K::TN / 32>(bbuf, boff, kb * CB, lds0 + stage + K::ASTEP);
 #pragma unroll
     for (int i = 0; i < TURNS; i++)
       if ((K::SA + K::TN) % 256 == 0 || i * 4 + wave < (K::SA + K::TN) / 64)
