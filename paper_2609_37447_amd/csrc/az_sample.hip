@@ -344,8 +344,9 @@ struct Row {
     }
     __syncthreads();
   }
-  // Bin of a logit by its distance from the largest; the last bin holds what has no weight.
-  __device__ __forceinline__ int bin_of(float l) const { return (int)fminf((top - l) * step, (float)(S::BINS - 1)); }
+  // Bin of a logit by its distance from the largest; the last bin holds what has no weight.  (Of half the distance, which
+  // no two finite logits have past fp32.)
+  __device__ __forceinline__ int bin_of(float l) const { return (int)fminf(fmaf(-0.5f, l, 0.5f * top) * (2.0f * step), (float)(S::BINS - 1)); }
   // The keys of a bin: bin_of falls as the key rises.
   __device__ __forceinline__ void bin_keys(int bin, uint32_t& lo, uint32_t& hi) const {
     auto first_at_most = [&](int b) {  // the smallest key whose bin is at most b

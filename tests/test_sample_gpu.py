@@ -157,6 +157,36 @@ def test_temperatures_at_the_ends_with_filters(vocab, temperature):
         _check(t, u, temperature=heat, **kw)
 
 
+@pytest.mark.parametrize("vocab", [3, 100, 4672, 20001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temperature", [1e37, 9e37, 3e38, float("inf")])
+def test_logits_as_far_apart_as_they_can_be(vocab, dtype, temperature):
+    """Distances past the largest fp32 number, at temperatures for which they still have a weight."""
+    import torch
+    rng = _rng(vocab, 9)
+    t = torch.from_numpy(rng.uniform(-3.3e38, 3.3e38, (10, vocab)).astype(np.float32))
+    t[:, 1] = 3.35e38
+    t[5:, vocab // 2 + 1:] = float("-inf")
+    t = t.to(torch.bfloat16) if dtype == "bf16" else t
+    u, heat, k = rng.random(10), np.full(10, temperature), max(1, vocab // 3)
+    for kw in ({}, {"top_k": np.full(10, k)}, {"top_p": rng.uniform(0.3, 0.999, 10)}, {"min_p": np.full(10, 0.013)},
+               {"top_k": np.full(10, k), "top_p": np.full(10, 0.91371), "min_p": np.full(10, 0.0017)}):
+        _check(t, u, temperature=heat, **kw)
+
+
+def test_a_distance_past_fp32_keeps_its_weight():
+    import torch
+    big = 3e38
+    t = torch.tensor([[big, -big], [big, -big]])
+    got, prob = _run(t, [0.99, 0.5], temperature=[big, big], top_p=[0.95, 0.95])  # weights 1 and exp(-2)
+    assert got.tolist() == [1, 0] and np.all(np.abs(prob - np.array([0.1192029, 0.8807971])) <= 1e-6)
+    t = torch.tensor([[big, -big, -3.1e38], [-3.1e38, -big, big]])
+    got, prob = _run(t, [1.0, 0.0], temperature=[1e38, 1e38], top_k=[2, 2])       # weights 1, exp(-6), and one that goes
+    assert got.tolist() == [1, 1] and np.all(np.abs(prob - 0.002472623) <= 1e-6 * 0.002472623 + 1e-9)
+    got, prob = _run(t, [1.0, 0.0], temperature=[1e38, 1e38], top_p=[0.99999, 0.99999])  # the last has 0.0022
+    assert got.tolist() == [2, 0]
+
+
 def test_frequencies():
     """Equally spaced u give every entry its share, to one draw."""
     import torch
