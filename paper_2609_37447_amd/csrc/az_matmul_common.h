@@ -84,24 +84,25 @@ __device__ __forceinline__ void write_tile(const cm_f32x16 (&acc)[K::FA][K::FB],
   }
 }
 
-// out from the sums over parts of the columns, in the order of the parts.  A thread takes four neighbouring columns of a
-// row at a time; blockIdx.y goes over the rows.  Four parts of 333 x 1880: 4.2 us (4.7 with a
-// division for each result).
+// Whether rows of n results are joined four neighbouring columns a thread.
+__host__ __device__ inline bool join_by_four(int64_t n) { return n % 4 == 0 && n >= 256; }
+
+// out from the sums over parts of the columns, in the order of the parts.  Wide rows by four neighbouring columns of a
+// row a thread, blockIdx.y over the rows: four parts of 333 x 1880 2.6-2.7 us, each result for itself with its division 3.3-3.4.  Rows
+// that are narrow or end inside a group of four each result for itself: eight parts of 3431 x 17 2.6 (by four columns 5.7, five of
+// 256 threads at work), of 100 x 130 2.5 (4.0); four parts of 200 x 3001 3.3-3.4 (3.3-3.6).
 template <bool F32>
 __global__ __launch_bounds__(256) void az_join_products(const float* __restrict__ parts, int count, int m, int n,
                                                         const float* __restrict__ bias, void* __restrict__ out, int64_t ldo) {
-  const int64_t total = (int64_t)m * n, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (c >= n) return;
-  const int left = (int)min((int64_t)n - c, (int64_t)4);
-  float add[4] = {};
-  if (bias) {
-#pragma unroll
-    for (int e = 0; e < 4; e++) add[e] = bias[c + min(e, left - 1)];
-  }
-  for (int64_t r = blockIdx.y; r < m; r += gridDim.y) {
-    const float* from = parts + r * n + c;
-    float v[4] = {};
-    if (left == 4) {
+  const int64_t total = (int64_t)m * n;
+  if (join_by_four(n)) {
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (c >= n) return;
+    float add[4] = {};
+    if (bias) __builtin_memcpy(add, bias + c, 16);
+    for (int64_t r = blockIdx.y; r < m; r += gridDim.y) {
+      const float* from = parts + r * n + c;
+      float v[4] = {};
 #pragma unroll 4
       for (int p = 0; p < count; p++) {
         float x[4];
@@ -109,15 +110,25 @@ __global__ __launch_bounds__(256) void az_join_products(const float* __restrict_
 #pragma unroll
         for (int e = 0; e < 4; e++) v[e] += x[e];
       }
-    } else {
-      for (int p = 0; p < count; p++)
-        for (int e = 0; e < left; e++) v[e] += from[p * total + e];
+      put<!F32, 4, EVEN>(out, r * ldo, (int)c, n, {v[0] + add[0], v[1] + add[1], v[2] + add[2], v[3] + add[3]});
     }
-    put<!F32, 4>(out, r * ldo, (int)c, n, {v[0] + add[0], v[1] + add[1], v[2] + add[2], v[3] + add[3]});
+  } else {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+      float v = 0.0f;
+      for (int p = 0; p < count; p++) v += parts[p * total + i];
+      const int64_t r = i / n, c = i - r * n;
+      if (bias) v += bias[c];
+      if constexpr (F32) ((float*)out)[r * ldo + c] = v;
+      else ((uint16_t*)out)[r * ldo + c] = bf16_of(v);
+    }
   }
 }
 
 // The workgroups that join results of m x n.
-inline dim3 join_grid(int64_t m, int64_t n) { return dim3((unsigned)((n + 1023) / 1024), (unsigned)(m < 65535 ? m : 65535)); }
+inline dim3 join_grid(int64_t m, int64_t n) {
+  if (join_by_four(n)) return dim3((unsigned)((n + 1023) / 1024), (unsigned)(m < 65535 ? m : 65535));
+  const int64_t groups = (m * n + 255) / 256;
+  return dim3((unsigned)(groups < 8192 ? groups : 8192));
+}
 
 }  // namespace

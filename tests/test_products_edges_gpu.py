@@ -1,5 +1,5 @@
-"""Products of matrices that end inside a tile, on whole numbers whose sums are exact (as in test_codes_kernels_gpu.py): results are
-compared for equality.
+"""Products of matrices that end inside a tile, and the join of parts by either of its ways, on whole numbers whose sums are exact
+(as in test_codes_kernels_gpu.py): results are compared for equality.
 """
 
 import pytest
@@ -68,3 +68,26 @@ def test_few_rows_that_lie_far_apart(a, b, shape):
     ran = _launched(lambda: az.matmul_tensors(p, q, o))
     assert "direct" in ran[0][0]
     assert torch.equal(o, _dot(x, w).float())
+
+
+# rows of results on both sides of the rule for four columns a thread (a multiple of four, 256 or more)
+@pytest.mark.parametrize("m,n,k", [(1100, 252, 9001), (1100, 255, 9001), (1100, 256, 9001), (1100, 258, 9001), (1100, 260, 9001),
+                                   (100, 1024, 20000), (100, 1027, 20000), (100, 1028, 20000), (100, 1880, 20000), (2985, 19, 29715)])
+@pytest.mark.parametrize("a,b", [("e2m1", "e2m1"), ("e4m3", "e2m1"), ("e4m3", "e4m3")])
+@pytest.mark.parametrize("out,pad,bias", [("f32", 0, True), ("bf16", 3, True), ("bf16", 0, False), ("f32", 5, False)])
+def test_joined_parts(m, n, k, a, b, out, pad, bias):
+    az, torch = _az()
+    g = _generator(m, n, k, 3)
+    x, w = _whole(g, m, k), _whole(g, n, k)
+    p, q = _operand(a, x), _operand(b, w)
+    bs = _whole(g, 1, n + 1)[0, 1:] if bias else None  # (four bytes past an aligned address)
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    o, whole = _rows(m, n, dt, n + pad, pad)
+    ran = _launched(lambda: az.matmul_tensors(p, q, o, bias=bs))
+    assert [r[0] for r in ran[1:]] == [f"az_join_products<{str(out == 'f32').lower()}>"]
+    want = _dot(x, w)
+    if bias:
+        want += bs.double()
+    assert torch.equal(o, want.float().to(dt))
+    o.fill_(7.0)
+    assert bool((whole == 7.0).all())
