@@ -157,6 +157,53 @@ def test_norm_grad(rows, cols, dtype, weight, dsum, pad, offset):
     assert torch.equal(only, dx)
 
 
+@pytest.mark.parametrize("rows,cols", SHAPES + [(600, 1030), (400, 8199)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("weight,pad,offset", [(True, 0, 0), (False, 3, 1), (True, 16, 5)])
+def test_results_in_their_inputs_place(rows, cols, dtype, weight, pad, offset):
+    """y in x's, the sum in x's and in the residual's, dx in dsum's and in dy's, padded rows too: the same bits as elsewhere, and
+    nothing between the rows is written."""
+    az, torch = _az()
+    rng = _rng(rows, cols, 12)
+    x, r, d = (_data(rng, rows, cols, dtype) for _ in range(3))
+    w = torch.from_numpy((1 + 0.3 * rng.standard_normal(cols)).astype(np.float32)).cuda() if weight else None
+
+    def place(t):
+        v, whole = _strided(t, pad, fill=7.0, offset=offset)
+        return v, whole
+
+    def beside(v, whole):
+        v.fill_(7.0)
+        return bool((whole == 7.0).all())
+
+    xd, rd, dd = (place(t)[0] for t in (x, r, d))
+    y, y2, s, dx, dx2 = (place(torch.zeros_like(x))[0] for _ in range(5))
+    az.norm_tensors(xd, y=y, weight=w)
+    az.norm_tensors(xd, y=y2, residual=rd, sum=s, weight=w)
+    az.norm_grad_tensors(dd, xd, dx, dsum=rd, weight=w)
+    az.norm_grad_tensors(dd, xd, dx2, weight=w)
+    a, whole = place(x)
+    az.norm_tensors(a, y=a, weight=w)
+    assert torch.equal(a, y) and beside(a, whole)
+    a, whole = place(x)
+    az.norm_tensors(a, y=a, residual=rd, sum=s.zero_(), weight=w)
+    assert torch.equal(a, y2) and beside(a, whole)
+    for t in (x, r):
+        a, whole = place(t)
+        out = place(torch.zeros_like(x))[0]
+        az.norm_tensors(a if t is x else xd, y=out, residual=rd if t is x else a, sum=a, weight=w)
+        assert torch.equal(a, s) and torch.equal(out, y2) and beside(a, whole)
+    a, whole = place(r)
+    az.norm_grad_tensors(dd, xd, a, dsum=a, weight=w)
+    assert torch.equal(a, dx) and beside(a, whole)
+    a, whole = place(d)
+    az.norm_grad_tensors(a, xd, a, dsum=rd, weight=w)
+    assert torch.equal(a, dx) and beside(a, whole)
+    a, whole = place(d)
+    az.norm_grad_tensors(a, xd, a, weight=w)
+    assert torch.equal(a, dx2) and beside(a, whole)
+
+
 def test_norm_grad_against_differences():
     """Central differences of the kernel's own loss, sum(dy * y) in fp64: with a step t its error is t^2 f''' / 6 and E |y| dy / t."""
     az, torch = _az()

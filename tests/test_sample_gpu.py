@@ -187,6 +187,24 @@ def test_a_distance_past_fp32_keeps_its_weight():
     assert got.tolist() == [2, 0]
 
 
+@pytest.mark.parametrize("vocab", [100, 4672, 131072, 1 << 24])
+@pytest.mark.parametrize("filters", [{}, {"top_p": [1.0 - 2.0 ** -24]}])
+def test_a_peak_over_a_flat_tail(vocab, filters):
+    """Each weight is off by at most half a step 2^-S of the largest, S = 62 - ceil(log2 vocab) and at most 51: a tail of equal entries just
+    below half a step has none, and one of one and a half steps counts as two."""
+    import torch
+    s = min(62 - int(np.ceil(np.log2(vocab))), 51)
+    for tail, step in ((0.4999, 0), (1.5001, 2), (3.0, 3)):
+        l = torch.full((1, vocab), float(np.float32(np.log(tail) - s * np.log(2.0))), device="cuda")
+        l[0, vocab // 2] = 0.0
+        got, prob = _run(l, [0.5], **filters)
+        assert got[0] == vocab // 2
+        true = 1.0 / (1.0 + (vocab - 1) * np.exp(float(l[0, 0])))
+        # (half a step of fp32, and at most 2^-24 of the sum that top_p leaves out)
+        assert abs(prob[0] - 1.0 / (1.0 + (vocab - 1) * step * 2.0 ** -s)) <= 2.0 ** -23
+        assert abs(prob[0] - true) <= vocab * 2.0 ** -(s + 1) + 2.0 ** -23
+
+
 def test_frequencies():
     """Equally spaced u give every entry its share, to one draw."""
     import torch
