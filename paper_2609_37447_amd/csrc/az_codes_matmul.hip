@@ -211,7 +211,7 @@ struct Tiled {
   }
 };
 
-// 8192^3: 460-482 us (2,280-2,390 TFLOP/s); 333 x 1880 x 10240 with exact products, four parts: 28 us.
+// 8192^3: 460-489 us (2,250-2,390 TFLOP/s); 333 x 1880 x 10240 with exact products, four parts: 28 us.
 template <int FA, int FB, int WM, int WN, bool EXACT, bool F32>
 __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_matmul_tiled(CodeView a, CodeView b, const float* __restrict__ bias,
                                                                               void* __restrict__ out, int64_t ldo, int mt, int nt,

@@ -65,7 +65,8 @@ __device__ __forceinline__ void store_nibbles(uint8_t* row, int c, int cols, uin
   }
 }
 
-// Two lanes take a block, 16 columns each, eight lanes 128 columns.  64 x 10240 bf16: 2.8 us.
+// Two lanes take a block, 16 columns each, eight lanes 128 columns.  64 x 10240 bf16: 2.8 us; 16384 x 4096 bf16 31.1, 4672 x 8192
+// fp32 32.1 (5.4 TB/s, a copy's rate).
 template <bool BF16>
 __global__ __launch_bounds__(NT) void az_nibble_rows(const void* __restrict__ x, int64_t ldx, NibbleView q) {
   const uint32_t nb = ((uint32_t)q.cols + 127) / 128, total = (uint32_t)q.rows * nb, lane8 = threadIdx.x & 7;

@@ -265,8 +265,8 @@ struct Tiled {
   }
 };
 
-// 8192^3: 272-278 us in 4 bits (3,960-4,040 TFLOP/s, matrix unit busy 45%: two steps on their way cannot hide the copies' way),
-// 430 with an e4m3 a.
+// 8192^3: 272-294 us in 4 bits by card and heat (3,740-4,040 TFLOP/s, matrix unit busy 46%: two steps on their way cannot hide
+// the copies' way), 441-452 with an e4m3 a.
 template <int A, int FA, int FB, int WM, int WN, bool EXACT, bool F32>
 __global__ __launch_bounds__(256, FA * FB == 16 ? 1 : 2) void az_nibble_tiled(LeftView a, NibbleView b, const float* __restrict__ bias,
                                                                               void* __restrict__ out, int64_t ldo, int mt, int nt,
@@ -477,7 +477,8 @@ enum Mode { FOURS = 0, MIXED = 1, EXACT = 2 };
 // Chosen against others, two 4-bit operands: 1 x 4672 x 8192 few rows 8.8 (32-row tiles in 8 parts 10.9); 40 x 4672 x 8192
 // 32-row tiles in 4 parts 13.4 (few rows 19); 333 x 1880 x 10240 64-row in 4 parts 19.2 (32-row in one 27); 1024 x 4672 x 8192
 // 128-row 37.7 (64-row 51.9, 256-row 59.9); 4096^3 256-row 43.7 (128-row 48.9).  The 256-row tile is not used in parts, where it
-// was never the best by more than the noise, nor for fp32 results of an e4m3 a (4096^3: 110, 128-row 115).
+// was never the best by more than the noise, and not built for fp32 results of an e4m3 a, where it gains at whole rounds (4096^3
+// 108, 128-row 113; 8192^3 770 for 827) and loses between them (8192 x 4672 x 8192 548 for 498).
 Plan choose_plan(int64_t m, int64_t n, int64_t k, Mode mode, bool f32, bool fits) {
   struct Tile {
     int kind, tm, tn, occ;
